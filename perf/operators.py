@@ -191,7 +191,9 @@ def _run_own(s):
         return ctx.logprobs(s["logits"], s["tokens"], n_top=s["top"], temperature=s["temp"])
     if s["op"] == "logprobs_grad":
         return ctx.logprobs_grad(s["logits"], s["tokens"], s["g_logprob"], s["g_entropy"], temperature=s["temp"])
-    return ctx.distill(s["logits"], s["ids"], s["teacher"], tail=s["tail"], temperature=s["temp"], weight=s["weight"],
+    from paper_2603_03333_b200 import binding
+    tail = binding.TAIL_BUCKET if s["tail"] == "bucket" else binding.TAIL_RENORM
+    return ctx.distill(s["logits"], s["ids"], s["teacher"], tail=tail, temperature=s["temp"], weight=s["weight"],
                        grad=s["grad"])
 
 
