@@ -23,8 +23,8 @@
  *     synchronise, never allocate and never free.
  *     The context-based verify calls (dropmatch_verify, _batched, _tree, _batched_next, _js)
  *     can therefore be captured into a CUDA graph; the seed and all sizes are then fixed.
- *   - The library allocates device memory only in dm_create, dm_set_head and
- *     dm_enable_js (its workspace) and frees it in dm_set_head / dm_destroy.
+ *   - The library allocates device memory only in dm_create, dm_set_head,
+ *     dm_enable_js and dm_enable_score (its workspace) and frees it in dm_set_head / dm_destroy.
  *   - Every function returns DM_OK or a negative status; nothing throws, aborts
  *     or prints.  A CUDA error raised by earlier asynchronous work is reported by
  *     the next call as DM_ECUDA.  A kernel that gives up on an internal wait sets
@@ -63,6 +63,8 @@ enum { DM_F32 = 0, DM_BF16 = 1 };             /* storage type of W and H (accumu
 enum { DM_RULE_NAIVE = 0, DM_RULE_MAJORITY = 1 };
 enum { DM_IMPL_AUTO = 0, DM_IMPL_SIMT = 1, DM_IMPL_TCGEN05 = 2 };
 enum { DM_MASK_PER_POSITION = 0, DM_MASK_PER_PATH = 1 };
+enum { DM_TAIL_RENORM = 0, DM_TAIL_BUCKET = 1 };   /* what a teacher's mass outside its given tokens becomes (dropmatch_distill) */
+#define DM_MAX_TOP 128                             /* alternatives, and teacher tokens, per row */
 
 /* Create a context on CUDA device `device` (must be sm_100).  *out is set on success. */
 int dm_create(dm_ctx** out, int device);
@@ -207,6 +209,83 @@ int dropmatch_verify_js(dm_ctx* ctx, const void* H, const int32_t* draft, const 
                         int K, float p, uint64_t seed, uint64_t seq_base, int32_t* out_tokens,
                         int32_t* out_counts, float* out_js, int32_t* out_js_ok, int32_t* out_accept_len,
                         void* stream);
+
+/* ---- log-probabilities, and training the draft model ---------------------------------------------
+ * The paper decides on tokens; an engine around it also wants their log-probabilities, and a draft
+ * model whose tokens get accepted has to be trained towards the target.  The three calls below cover
+ * that: dropmatch_score reads the target's head (and gives a teacher's top tokens), dropmatch_distill
+ * trains the draft's logits towards them, dropmatch_logprobs and its gradient work on any logits.
+ *
+ * Definitions, for a row of logits l[0..V) and a temperature T > 0:
+ *   z = l / T;  lse = log sum_v exp(z[v]);  log p[v] = z[v] - lse;  entropy = - sum_v p[v] log p[v].
+ * Natural logarithms.  Outputs (float32, one per row, each may be NULL):
+ *   out_logprob   log p[tokens[r]]; 0 where tokens[r] is outside [0,V) (a row without a token);
+ *                 needs `tokens`
+ *   out_lse, out_entropy
+ *   out_top_ids, out_top_logprob [rows, n_top]   the n_top largest entries in decreasing order, equal
+ *                 entries: smaller id first.  Both or, with n_top = 0, neither.  n_top <= min(V, DM_MAX_TOP)
+ * Masked entries: -inf has probability 0 (log p = -inf) and never yields a NaN; a large negative
+ * number is just a number.  A row of nothing but -inf: lse = -inf, entropy 0, every log p = -inf.
+ * A row that holds a NaN or +inf: lse, entropy and every log-probability of the row are NaN (top ids
+ * list NaN first).  Sums are fp32; they are kept without the row's largest entry, so that
+ * log-probabilities close to 0 keep their relative precision. */
+
+/* Score hidden rows against the context's head, without dropout: l = H W^T (Eq. 3).
+ * dm_enable_score reserves, after dm_set_head, the workspace for calls of up to max_rows rows and
+ * max_top alternatives (fp32 logits of at most 512 rows at a time).  Allocates; synchronises the
+ * device; a later dm_set_head drops the buffers.
+ *   H[n_rows,d]      storage type of the head, 16-byte aligned
+ *   tokens[n_rows]   device, may be NULL (then out_logprob must be NULL)
+ * n_rows = 0 is allowed and does nothing.  DM_EWORKSPACE beyond what dm_enable_score reserved.
+ * Sharded heads (dm_set_vocab_offset) are not supported: DM_EUNSUPPORTED.  Like every context-based
+ * call it uses the context's workspace: order the calls (and captured graphs) of one context.
+ * If a kernel gives up on a wait (dm_device_error), the outputs are NaN and ids -1. */
+int dm_enable_score(dm_ctx* ctx, int max_rows, int max_top);
+int dropmatch_score(dm_ctx* ctx, const void* H, const int32_t* tokens, int n_rows, int n_top, float temperature,
+                    float* out_logprob, float* out_lse, float* out_entropy, int32_t* out_top_ids,
+                    float* out_top_logprob, void* stream);
+
+/* The same on logits in memory.  Needs no head and no workspace: calls of one context may overlap.
+ *   logits[n_rows][ld]   dtype DM_F32 or DM_BF16, row stride ld >= V entries, aligned to one entry
+ *                        (16-byte aligned rows of the same alignment are the fastest)
+ * n_rows = 0 is allowed and does nothing.  V <= 2^30. */
+int dropmatch_logprobs(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
+                       const int32_t* tokens, int n_top, float temperature, float* out_logprob, float* out_lse,
+                       float* out_entropy, int32_t* out_top_ids, float* out_top_logprob, void* stream);
+
+/* Gradient of sum_r ( g_logprob[r] * logprob[r] + g_entropy[r] * entropy[r] ) with respect to the
+ * logits:  dl[v] = (1/T) ( g_logprob (1[v = token] - p[v]) - g_entropy p[v] (log p[v] + entropy) ).
+ *   g_logprob, g_entropy [n_rows]   float32; either may be NULL (zero); `tokens` is needed with g_logprob
+ *   out_grad[n_rows][ld_grad]       same type as the logits, rounded once; may be the logits themselves
+ *                                   (same pointer, ld_grad = ld), else must not overlap them.
+ *                                   Entries V..ld_grad of a row are left as they are
+ * A row whose two factors are 0 (or that has no token and g_entropy = 0) gets a gradient of 0 whatever
+ * its logits hold; so does a row of nothing but -inf.  Recomputes the row's sums: one read of the
+ * logits, one write. */
+int dropmatch_logprobs_grad(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
+                            const int32_t* tokens, float temperature, const float* g_logprob,
+                            const float* g_entropy, void* out_grad, int64_t ld_grad, void* stream);
+
+/* Distillation of a teacher that is known by k tokens per row: loss[r] = KL(teacher || student) and the
+ * gradient of sum_r weight[r] * loss[r] with respect to the student's logits, in one pass.
+ *   teacher_ids[n_rows,k], teacher_logprob[n_rows,k]   1 <= k <= DM_MAX_TOP.  An id outside [0,V) is an
+ *       absent entry.  Values are taken at the teacher's temperature: dropmatch_score at temperature T
+ *       gives them for a student temperature T.  -inf is probability 0.  An id that occurs twice counts
+ *       with both values.
+ *   tail  DM_TAIL_RENORM: q = Softmax(teacher_logprob) over the present entries (any common offset cancels:
+ *         logits / T will do);   loss = sum q (log q - log p)
+ *         DM_TAIL_BUCKET: q = exp(teacher_logprob) and the rest q_t = max(0, 1 - sum q) is matched as one
+ *         outcome against the student's mass p_t outside the teacher's tokens:
+ *         loss = sum q (log q - log p) + q_t (log q_t - log p_t)   (no rest where the tokens cover V)
+ *   weight[n_rows]   float32 or NULL (1): a mask, 1/n, or the upstream gradient of loss[r]
+ *   out_loss[n_rows] float32 (without the weight) or NULL;  out_grad as above, or NULL; not both NULL
+ *   dl[v] = weight / T * ( M p[v] - q[v] - [v is no teacher token] q_t p[v] / p_t ),  M = sum q + q_t
+ * No factor T^2 is applied.  A row without a present entry: loss 0 (and gradient 0).  A teacher token
+ * the student gives probability 0: loss +inf.  A row of nothing but -inf: gradient 0.  A row of weight 0
+ * gets a gradient of 0 whatever it holds.  DM_EUNSUPPORTED beyond V of about 12 million (bucket). */
+int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
+                      const int32_t* teacher_ids, const float* teacher_logprob, int k, int tail, float temperature,
+                      const float* weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream);
 
 /* Vocabulary-sharded heads (the deployment of Sec. 4.1 is tensor-parallel: every GPU holds a
  * slice of the LM head).  A context whose head is rows [offset, offset+V) of the full head reports

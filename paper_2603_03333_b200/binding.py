@@ -17,11 +17,13 @@ F32, BF16 = 0, 1
 RULE_NAIVE, RULE_MAJORITY = 0, 1
 IMPL_AUTO, IMPL_SIMT, IMPL_TCGEN05 = 0, 1, 2
 MASK_PER_POSITION, MASK_PER_PATH = 0, 1
+TAIL_RENORM, TAIL_BUCKET = 0, 1
+MAX_TOP = 128
 
 _LIB_PATH = Path(__file__).resolve().parent / "libdropmatch.so"
 _lib = None
 
-_vp, _ci, _cf, _u64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint64
+_vp, _ci, _cf, _u64, _i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint64, ctypes.c_int64
 
 # name -> (restype, argtypes); mirrors include/dropmatch.h declaration by declaration
 SIGNATURES = {
@@ -45,6 +47,11 @@ SIGNATURES = {
                                               _vp, _vp, _vp, _vp, _vp]),
     "dm_enable_js": (_ci, [_vp, _ci, _ci]),
     "dropmatch_verify_js": (_ci, [_vp, _vp, _vp, _vp, _ci, _ci, _ci, _cf, _u64, _u64, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dm_enable_score": (_ci, [_vp, _ci, _ci]),
+    "dropmatch_score": (_ci, [_vp, _vp, _vp, _ci, _ci, _cf, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dropmatch_logprobs": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _ci, _cf, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dropmatch_logprobs_grad": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _cf, _vp, _vp, _vp, _i64, _vp]),
+    "dropmatch_distill": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _vp, _ci, _ci, _cf, _vp, _vp, _vp, _i64, _vp]),
     "dropmatch_verify_tree": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
                                     _vp, _vp, _vp, _vp, _vp, _vp]),
     "dropmatch_verify_tree_next": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
@@ -98,6 +105,8 @@ def _ptr(t):
     # c_void_p object per argument would cost more than the rest of the marshalling together
     return None if t is None else t.data_ptr()
 
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}   # of tensors of logits
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -311,6 +320,128 @@ class Context:
                                          _ptr(out["tokens"]), _ptr(out["counts"]), _ptr(out["js"]), _ptr(out["js_ok"]),
                                          _ptr(out["accept_len"]), _stream(self.device)), "dropmatch_verify_js")
         return out
+
+    # -- dm_enable_score / dropmatch_score
+    def enable_score(self, max_rows: int, max_top: int = 0):
+        _check(lib().dm_enable_score(self._h, max_rows, max_top), "dm_enable_score")
+
+    def score(self, H, tokens=None, n_top=0, temperature=1.0):
+        """H[...,d] through the head, without dropout; tokens[...] int32 or None.  -> dict of float32
+        tensors of the leading shape: lse, entropy, logprob (with tokens), and for n_top > 0
+        top_ids[...,n_top] (int32) and top_logprob[...,n_top]."""
+        self._on_device(_dev(H, self._tdtype(), "H"), "H")
+        if H.dim() < 2 or H.shape[-1] != self.d:
+            raise TypeError("H must have shape [..., d]")
+        out = self._row_outputs(H.shape[:-1], tokens, n_top)
+        _check(lib().dropmatch_score(self._h, _ptr(H), _ptr(tokens), H.numel() // self.d, n_top, temperature,
+                                     *self._row_pointers(out), _stream(self.device)), "dropmatch_score")
+        return out
+
+    # -- dropmatch_logprobs / dropmatch_logprobs_grad / dropmatch_distill
+    def logprobs(self, logits, tokens=None, n_top=0, temperature=1.0):
+        """The outputs of `score` for logits[...,V] in memory (float32 or bfloat16; the last dimension
+        dense, one stride between rows)."""
+        rows, ld = self._rows(logits, "logits")
+        out = self._row_outputs(logits.shape[:-1], tokens, n_top)
+        _check(lib().dropmatch_logprobs(self._h, _ptr(logits), _DTYPES[logits.dtype], ld, rows, logits.shape[-1],
+                                        _ptr(tokens), n_top, temperature, *self._row_pointers(out),
+                                        _stream(self.device)), "dropmatch_logprobs")
+        return out
+
+    def logprobs_grad(self, logits, tokens, grad_logprob, grad_entropy=None, temperature=1.0, out=None):
+        """-> gradient of sum(grad_logprob * logprob + grad_entropy * entropy) for the logits, in their
+        dtype.  Either factor may be None; `out` may be the logits themselves."""
+        rows, ld = self._rows(logits, "logits")
+        lead = logits.shape[:-1]
+        self._per_row(tokens, torch.int32, lead, "tokens")
+        self._per_row(grad_logprob, torch.float32, lead, "grad_logprob")
+        self._per_row(grad_entropy, torch.float32, lead, "grad_entropy")
+        out, ld_out = self._grad_target(logits, out)
+        _check(lib().dropmatch_logprobs_grad(self._h, _ptr(logits), _DTYPES[logits.dtype], ld, rows, logits.shape[-1],
+                                             _ptr(tokens), temperature, _ptr(grad_logprob), _ptr(grad_entropy),
+                                             _ptr(out), ld_out, _stream(self.device)), "dropmatch_logprobs_grad")
+        return out
+
+    def distill(self, logits, teacher_ids, teacher_logprob, tail=TAIL_RENORM, temperature=1.0, weight=None, loss=True,
+                grad=False, out=None):
+        """KL(teacher || student) per row of logits[...,V] for teacher_ids[...,k] (int32, outside [0,V):
+        absent) and teacher_logprob[...,k] (float32).  -> dict: loss[...] (unless loss=False) and, with
+        `grad`, the gradient of sum(weight * loss) for the logits, in their dtype, into `out` if given
+        (which may be the logits themselves)."""
+        rows, ld = self._rows(logits, "logits")
+        lead = logits.shape[:-1]
+        k = teacher_ids.shape[-1]
+        self._per_row(teacher_ids, torch.int32, (*lead, k), "teacher_ids")
+        self._per_row(teacher_logprob, torch.float32, (*lead, k), "teacher_logprob")
+        self._per_row(weight, torch.float32, lead, "weight")
+        if not grad and out is not None:
+            raise TypeError("out is the gradient's: it needs grad=True")
+        res = {}
+        if loss:
+            res["loss"] = torch.empty(lead, dtype=torch.float32, device=self.device)
+        ld_out = 0
+        if grad:
+            res["grad"], ld_out = self._grad_target(logits, out)
+        _check(lib().dropmatch_distill(self._h, _ptr(logits), _DTYPES[logits.dtype], ld, rows, logits.shape[-1],
+                                       _ptr(teacher_ids), _ptr(teacher_logprob), k, tail, temperature, _ptr(weight),
+                                       _ptr(res.get("loss")), _ptr(res.get("grad")), ld_out, _stream(self.device)),
+               "dropmatch_distill")
+        return res
+
+    def _on_device(self, t, what):
+        if t.device != self.device:
+            raise TypeError(f"{what} must be on the context's device {self.device}")
+        return t
+
+    def _rows(self, t, what):
+        """(rows, row stride) of a tensor [..., V] whose rows lie one stride apart."""
+        if not t.is_cuda or t.dtype not in _DTYPES or t.dim() < 2:
+            raise TypeError(f"{what} must be a CUDA tensor [..., V] of float32 or bfloat16")
+        self._on_device(t, what)
+        V = t.shape[-1]
+        if V > 1 and t.stride(-1) != 1:
+            raise TypeError(f"{what} must be dense along the last dimension")
+        rows, ld = 1, None
+        for n, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+            if n != 1:
+                if ld is None:
+                    ld = stride
+                elif stride != ld * rows:
+                    raise TypeError(f"{what} must have one stride between rows")
+            rows *= n
+        ld = V if ld is None else ld
+        if rows > 1 and ld < V:
+            raise TypeError(f"{what} must not have overlapping rows")
+        return rows, max(ld, V)
+
+    def _per_row(self, t, dtype, shape, what):
+        if t is None:
+            return
+        self._on_device(_dev(t, dtype, what), what)
+        if tuple(t.shape) != tuple(shape):
+            raise TypeError(f"{what} must have shape {tuple(shape)}")
+
+    def _grad_target(self, logits, out):
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        if out.shape != logits.shape or out.dtype != logits.dtype:
+            raise TypeError("out must have the logits' shape and dtype")
+        return out, self._rows(out, "out")[1]
+
+    def _row_outputs(self, lead, tokens, n_top):
+        self._per_row(tokens, torch.int32, lead, "tokens")
+        f32 = dict(dtype=torch.float32, device=self.device)
+        out = dict(lse=torch.empty(lead, **f32), entropy=torch.empty(lead, **f32))
+        if tokens is not None:
+            out["logprob"] = torch.empty(lead, **f32)
+        if n_top > 0:
+            out["top_ids"] = torch.empty((*lead, n_top), dtype=torch.int32, device=self.device)
+            out["top_logprob"] = torch.empty((*lead, n_top), **f32)
+        return out
+
+    @staticmethod
+    def _row_pointers(out):
+        return [_ptr(out.get(name)) for name in ("logprob", "lse", "entropy", "top_ids", "top_logprob")]
 
     # -- dropmatch_verify_tree
     def verify_tree(self, H, node_token, node_parent, node_hrow, K, p, seed, seq_base=0, rule=RULE_NAIVE):

@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "dm_internal.h"
+#include "dm_rows.cuh"
 
 using namespace dm;
 
@@ -44,6 +45,9 @@ struct dm_ctx {
     float* js_logits = nullptr;              // [js_max_rows][V]
     float* js_ws = nullptr;
     int js_max_rows = 0, js_max_hidden = 0;
+    // dropmatch_score (dm_enable_score): logits of up to score_chunk rows at a time
+    float* score_logits = nullptr;           // [score_chunk][V]
+    int score_max_rows = 0, score_max_top = 0, score_chunk = 0;
     // optional timing of the head kernel alone (dm_profile_head)
     bool profile = false;
     std::vector<cudaEvent_t> prof_events;    // begin/end pairs, grown on demand
@@ -53,6 +57,7 @@ struct dm_ctx {
 namespace {
 
 constexpr size_t kMaxProfileEvents = 8192;
+constexpr int kScoreChunk = 512;   // rows of dropmatch_score whose logits exist at a time
 
 struct DeviceGuard {
     int prev = -1;
@@ -77,6 +82,8 @@ void free_workspace(dm_ctx* c) {
     cudaFree(c->js_logits); c->js_logits = nullptr;
     cudaFree(c->js_ws); c->js_ws = nullptr;
     c->js_max_rows = c->js_max_hidden = 0;
+    cudaFree(c->score_logits); c->score_logits = nullptr;
+    c->score_max_rows = c->score_max_top = c->score_chunk = 0;
     c->ws_bytes = 0;
 }
 
@@ -194,6 +201,61 @@ int check_common(const dm_ctx* c, const void* H, int B, int T, int K) {
     if (B < 1 || T < 1 || K < 1 || K > kMaxK) return DM_EINVAL;
     if ((long long)B * T * K > 0x3FFFFFFFll) return DM_EINVAL;
     return DM_OK;
+}
+
+// Checks and fields that all calls on rows of logits share.
+int rows_common(RowsParams* rp, int dtype, int64_t ld, int n_rows, int V, float temperature) {
+    if (dtype != DM_F32 && dtype != DM_BF16) return DM_EINVAL;
+    if (n_rows < 0 || V < 1 || ld < V) return DM_EINVAL;
+    if (!(temperature > 0.0f) || !(temperature < 1e30f) || !(temperature > 1e-30f)) return DM_EINVAL;
+    if (V > kRowsMaxV) return DM_EUNSUPPORTED;
+    rp->ld = ld;
+    rp->V = V;
+    rp->rows = n_rows;
+    rp->inv_temp_d = 1.0 / (double)temperature;
+    rp->inv_temp = (float)rp->inv_temp_d;
+    rp->c = (float)(1.4426950408889634074 / (double)temperature);   // log2(e) / T
+    return DM_OK;
+}
+
+int rows_outputs(RowsParams* rp, const int32_t* tokens, int n_top, float* out_logprob, float* out_lse, float* out_entropy,
+                 int32_t* out_top_ids, float* out_top_logprob) {
+    if (n_top < 0 || n_top > DM_MAX_TOP || n_top > rp->V) return DM_EINVAL;
+    if (rp->rows > 0) {
+        if (n_top > 0 && (out_top_ids == nullptr || out_top_logprob == nullptr)) return DM_EINVAL;
+        if (out_logprob != nullptr && tokens == nullptr) return DM_EINVAL;
+    }
+    rp->tokens = out_logprob != nullptr ? tokens : nullptr;
+    rp->n_top = n_top;
+    rp->out_logprob = out_logprob; rp->out_lse = out_lse; rp->out_entropy = out_entropy;
+    rp->out_top_ids = out_top_ids; rp->out_top_logprob = out_top_logprob;
+    return DM_OK;
+}
+
+// Rows [r0, r0 + rows) of a call: per-row inputs and outputs move along.
+RowsParams rows_from(const RowsParams& rp, int r0, int rows) {
+    RowsParams p = rp;
+    p.rows = rows;
+    if (p.tokens) p.tokens += r0;
+    if (p.out_logprob) p.out_logprob += r0;
+    if (p.out_lse) p.out_lse += r0;
+    if (p.out_entropy) p.out_entropy += r0;
+    if (p.n_top > 0) { p.out_top_ids += (size_t)r0 * p.n_top; p.out_top_logprob += (size_t)r0 * p.n_top; }
+    return p;
+}
+
+bool aligned_to_entry(const void* p, int dtype) {
+    return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (dtype == DM_F32 ? 3u : 1u)) == 0;
+}
+
+// The gradient may take the logits' place entry by entry, or must lie clear of them.
+bool grad_target_ok(const void* logits, int64_t ld, const void* grad, int64_t ld_grad, int n_rows, int V, int dtype) {
+    if (!aligned_to_entry(grad, dtype) || ld_grad < V) return false;
+    if (grad == logits) return ld_grad == ld || n_rows == 1;
+    const uintptr_t elem = dtype == DM_F32 ? 4 : 2;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits), a1 = a0 + ((uintptr_t)(n_rows - 1) * (uintptr_t)ld + (uintptr_t)V) * elem;
+    const uintptr_t b0 = reinterpret_cast<uintptr_t>(grad), b1 = b0 + ((uintptr_t)(n_rows - 1) * (uintptr_t)ld_grad + (uintptr_t)V) * elem;
+    return a1 <= b0 || b1 <= a0;
 }
 
 }  // namespace
@@ -632,6 +694,139 @@ int dropmatch_verify_js(dm_ctx* c, const void* H, const int32_t* draft, const fl
     if (st != DM_OK) return st;
     c->last_launches += js_launches;
     return DM_OK;
+}
+
+int dm_enable_score(dm_ctx* c, int max_rows, int max_top) {
+    if (c == nullptr) return DM_EINVAL;
+    if (!c->has_head) return DM_ENOHEAD;
+    if (max_rows < 1 || max_rows > c->max_rows || max_top < 0 || max_top > DM_MAX_TOP || max_top > c->head.V) return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    if (c->score_logits != nullptr) c->ws_bytes -= (size_t)c->score_chunk * c->head.V * sizeof(float);
+    cudaFree(c->score_logits); c->score_logits = nullptr;
+    c->score_max_rows = c->score_max_top = c->score_chunk = 0;
+    const int chunk = max_rows < kScoreChunk ? max_rows : kScoreChunk;
+    const size_t n_logits = (size_t)chunk * c->head.V * sizeof(float);
+    if (cudaMalloc(&c->score_logits, n_logits) != cudaSuccess) {
+        cudaGetLastError();
+        c->score_logits = nullptr;
+        return DM_ECUDA;
+    }
+    c->score_max_rows = max_rows;
+    c->score_max_top = max_top;
+    c->score_chunk = chunk;
+    c->ws_bytes += n_logits;
+    return DM_OK;
+}
+
+int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows, int n_top, float temperature,
+                    float* out_logprob, float* out_lse, float* out_entropy, int32_t* out_top_ids,
+                    float* out_top_logprob, void* stream) {
+    if (c == nullptr || n_rows < 0 || n_top < 0) return DM_EINVAL;
+    if (!c->has_head) return DM_ENOHEAD;
+    RowsParams rp{};
+    int st = rows_common(&rp, DM_F32, c->head.V, n_rows, c->head.V, temperature);
+    if (st != DM_OK) return st;
+    st = rows_outputs(&rp, tokens, n_top, out_logprob, out_lse, out_entropy, out_top_ids, out_top_logprob);
+    if (st != DM_OK) return st;
+    if (c->head.v_offset != 0) return DM_EUNSUPPORTED;
+    if (n_rows == 0) return DM_OK;
+    if (H == nullptr || (reinterpret_cast<uintptr_t>(H) & 15u) != 0) return DM_EINVAL;
+    if (c->score_logits == nullptr || n_rows > c->score_max_rows || n_top > c->score_max_top) return DM_EWORKSPACE;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    MaskKey mk;
+    make_mask_key(0.0f, 0, &mk);   // no dropout: one path per row that keeps every element
+    int impl, launches_total = 0;
+    st = pick_impl(c, n_rows, &impl);
+    if (st != DM_OK) return st;
+    const size_t row_bytes = (size_t)c->head.d * (c->head.dtype == DM_F32 ? 4 : 2);
+    for (int r0 = 0; r0 < n_rows; r0 += c->score_chunk) {
+        const int rows = n_rows - r0 < c->score_chunk ? n_rows - r0 : c->score_chunk;
+        const void* Hc = static_cast<const unsigned char*>(H) + (size_t)r0 * row_bytes;
+        RowMap map{nullptr, 1, rows, 1, 0u, DM_MASK_PER_POSITION};
+        int n_slices = 0, launches = 1;
+        if (impl == DM_IMPL_TCGEN05)
+            st = fused_launch(c->fused, c->head, Hc, rows, rows, map, mk, &n_slices, c->partials, c->score_logits, c->err, s,
+                              &launches, nullptr, nullptr, nullptr, nullptr, nullptr, c->wait_limit, c->pdl);
+        else
+            st = launch_simt(c->head, Hc, rows, map, mk, &n_slices, c->partials, c->score_logits, c->err, s);
+        if (st != DM_OK) return st;
+        RowsParams part = rows_from(rp, r0, rows);
+        part.logits = c->score_logits;
+        part.err = c->err;
+        st = launch_rows_logprobs(part, DM_F32, s);
+        if (st != DM_OK) return st;
+        launches_total += launches + 1;
+    }
+    c->last_impl = impl;
+    c->last_launches = launches_total;
+    return DM_OK;
+}
+
+int dropmatch_logprobs(dm_ctx* c, const void* logits, int dtype, int64_t ld, int n_rows, int V, const int32_t* tokens,
+                       int n_top, float temperature, float* out_logprob, float* out_lse, float* out_entropy,
+                       int32_t* out_top_ids, float* out_top_logprob, void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    RowsParams rp{};
+    int st = rows_common(&rp, dtype, ld, n_rows, V, temperature);
+    if (st != DM_OK) return st;
+    st = rows_outputs(&rp, tokens, n_top, out_logprob, out_lse, out_entropy, out_top_ids, out_top_logprob);
+    if (st != DM_OK) return st;
+    if (n_rows == 0) return DM_OK;
+    if (!aligned_to_entry(logits, dtype)) return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    rp.logits = logits;
+    return launch_rows_logprobs(rp, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_logprobs_grad(dm_ctx* c, const void* logits, int dtype, int64_t ld, int n_rows, int V, const int32_t* tokens,
+                            float temperature, const float* g_logprob, const float* g_entropy, void* out_grad,
+                            int64_t ld_grad, void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    RowsParams rp{};
+    int st = rows_common(&rp, dtype, ld, n_rows, V, temperature);
+    if (st != DM_OK) return st;
+    if (n_rows == 0) return DM_OK;
+    if (g_logprob != nullptr && tokens == nullptr) return DM_EINVAL;
+    if (!aligned_to_entry(logits, dtype) || !grad_target_ok(logits, ld, out_grad, ld_grad, n_rows, V, dtype)) return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    rp.logits = logits;
+    rp.tokens = tokens;
+    rp.g_logprob = g_logprob; rp.g_entropy = g_entropy;
+    rp.out_grad = out_grad; rp.ld_grad = ld_grad;
+    return launch_rows_grad(rp, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_distill(dm_ctx* c, const void* logits, int dtype, int64_t ld, int n_rows, int V, const int32_t* teacher_ids,
+                      const float* teacher_logprob, int k, int tail, float temperature, const float* weight,
+                      float* out_loss, void* out_grad, int64_t ld_grad, void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    RowsParams rp{};
+    int st = rows_common(&rp, dtype, ld, n_rows, V, temperature);
+    if (st != DM_OK) return st;
+    if (k < 1 || k > DM_MAX_TOP || (tail != DM_TAIL_RENORM && tail != DM_TAIL_BUCKET)) return DM_EINVAL;
+    if (n_rows == 0) return DM_OK;
+    if (teacher_ids == nullptr || teacher_logprob == nullptr || (out_loss == nullptr && out_grad == nullptr)) return DM_EINVAL;
+    if (!aligned_to_entry(logits, dtype)) return DM_EINVAL;
+    if (out_grad != nullptr && !grad_target_ok(logits, ld, out_grad, ld_grad, n_rows, V, dtype)) return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    rp.logits = logits;
+    rp.t_ids = teacher_ids; rp.t_logprob = teacher_logprob;
+    rp.k = k; rp.tail = tail;
+    rp.weight = weight;
+    rp.out_loss = out_loss;
+    rp.out_grad = out_grad; rp.ld_grad = ld_grad;
+    return launch_rows_distill(rp, dtype, static_cast<cudaStream_t>(stream));
 }
 
 int dropmatch_verify_tree(dm_ctx* c, const void* H, const int32_t* node_token, const int32_t* node_parent,

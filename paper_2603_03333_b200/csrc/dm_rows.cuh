@@ -1,0 +1,42 @@
+// Arguments of the row operators (dm_rows.cu), shared with the C ABI.
+#pragma once
+#include "dm_internal.h"
+
+namespace dm {
+
+constexpr int kRowsMaxTop = DM_MAX_TOP;   // alternatives, and teacher tokens, of a row
+constexpr int kRowsMaxCluster = 8;        // CTAs that share a row
+constexpr int kRowsMaxV = 1 << 30;
+
+struct RowsParams {
+    const void* logits;   // [rows][ld], entries 0..V-1 of a row
+    long long ld;
+    int V, rows;
+    float inv_temp;       // 1 / T
+    float c;              // log2(e) / T
+    double inv_temp_d;
+    int stash_vecs;       // 16-byte vectors of a CTA's share kept in shared memory (gradient kernels; set by the launch)
+    const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
+    // logprobs
+    const int32_t* tokens;
+    int n_top;
+    float *out_logprob, *out_lse, *out_entropy, *out_top_logprob;
+    int32_t* out_top_ids;
+    // gradients
+    const float *g_logprob, *g_entropy;
+    void* out_grad;
+    long long ld_grad;
+    // distill
+    const int32_t* t_ids;
+    const float *t_logprob, *weight;
+    int k, tail;
+    float* out_loss;
+};
+
+// dtype: DM_F32 or DM_BF16 (logits and their gradient).  Only enqueue work; DM_EUNSUPPORTED where a
+// share of a row does not fit what a CTA needs to know about it in shared memory.
+int launch_rows_logprobs(const RowsParams& P, int dtype, cudaStream_t stream);
+int launch_rows_grad(const RowsParams& P, int dtype, cudaStream_t stream);
+int launch_rows_distill(const RowsParams& P, int dtype, cudaStream_t stream);
+
+}  // namespace dm
