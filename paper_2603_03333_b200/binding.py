@@ -388,8 +388,9 @@ class Context:
                "dropmatch_distill")
         return res
 
+    # the calls on rows are short: these checks are written for few Python-level operations
     def _on_device(self, t, what):
-        if t.device != self.device:
+        if t.get_device() != self.device.index:
             raise TypeError(f"{what} must be on the context's device {self.device}")
         return t
 
@@ -399,6 +400,8 @@ class Context:
             raise TypeError(f"{what} must be a CUDA tensor [..., V] of float32 or bfloat16")
         self._on_device(t, what)
         V = t.shape[-1]
+        if t.is_contiguous():
+            return (t.numel() // V if V else 0), V
         if V > 1 and t.stride(-1) != 1:
             raise TypeError(f"{what} must be dense along the last dimension")
         rows, ld = 1, None
@@ -417,31 +420,38 @@ class Context:
     def _per_row(self, t, dtype, shape, what):
         if t is None:
             return
-        self._on_device(_dev(t, dtype, what), what)
-        if tuple(t.shape) != tuple(shape):
+        if not (t.dtype is dtype and t.get_device() == self.device.index and t.is_contiguous()):
+            self._on_device(_dev(t, dtype, what), what)
+        if t.shape != shape:
             raise TypeError(f"{what} must have shape {tuple(shape)}")
 
     def _grad_target(self, logits, out):
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
+            return out, logits.shape[-1]
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise TypeError("out must have the logits' shape and dtype")
         return out, self._rows(out, "out")[1]
 
     def _row_outputs(self, lead, tokens, n_top):
         self._per_row(tokens, torch.int32, lead, "tokens")
-        f32 = dict(dtype=torch.float32, device=self.device)
-        out = dict(lse=torch.empty(lead, **f32), entropy=torch.empty(lead, **f32))
-        if tokens is not None:
-            out["logprob"] = torch.empty(lead, **f32)
+        if tokens is None:
+            lse, entropy = torch.empty((2, *lead), dtype=torch.float32, device=self.device).unbind(0)
+            out = dict(lse=lse, entropy=entropy)
+        else:
+            lse, entropy, logprob = torch.empty((3, *lead), dtype=torch.float32, device=self.device).unbind(0)
+            out = dict(lse=lse, entropy=entropy, logprob=logprob)
         if n_top > 0:
-            out["top_ids"] = torch.empty((*lead, n_top), dtype=torch.int32, device=self.device)
-            out["top_logprob"] = torch.empty((*lead, n_top), **f32)
+            shape = (*lead, n_top)
+            out["top_ids"] = torch.empty(shape, dtype=torch.int32, device=self.device)
+            out["top_logprob"] = torch.empty(shape, dtype=torch.float32, device=self.device)
         return out
 
     @staticmethod
     def _row_pointers(out):
-        return [_ptr(out.get(name)) for name in ("logprob", "lse", "entropy", "top_ids", "top_logprob")]
+        get = out.get
+        return (_ptr(get("logprob")), out["lse"].data_ptr(), out["entropy"].data_ptr(), _ptr(get("top_ids")),
+                _ptr(get("top_logprob")))
 
     # -- dropmatch_verify_tree
     def verify_tree(self, H, node_token, node_parent, node_hrow, K, p, seed, seq_base=0, rule=RULE_NAIVE):

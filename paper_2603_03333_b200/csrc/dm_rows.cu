@@ -7,10 +7,11 @@
 //                  (see distill_teacher below)
 //
 // A row belongs to one thread-block cluster; its CTAs take contiguous shares of the row, cut at
-// 16-byte boundaries.  One pass over the share keeps, per thread, a running reference, the sum of
-// 2^((x - ref) c) with c = log2(e) / T, the sum of those times their exponents (entropy) and the
-// exact maximum.  Threads meet in the block, CTAs through distributed shared memory; the sums are
-// kept WITHOUT the row's largest entry (its holder goes over its entries once more), so that
+// 16-byte boundaries.  One pass over the share keeps, per warp, the exact maximum m so far (five
+// shuffles per 1024 entries) and, per lane, the sum of e = 2^((x - m) log2(e) / T) and of e times its
+// exponent (entropy) over the entries below m; entries equal to m are counted.  A batch whose maximum
+// stays below m takes the short path: seven or eight instructions per entry.  Warps meet in the
+// block, CTAs through distributed shared memory.  Sums never contain the row's largest entry, so that
 // log(1 + rest) keeps its precision next to a near-certain token.
 //
 // Bound: memory, one read of x (and one write of the gradient).  The gradient kernels keep as much
@@ -28,12 +29,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256;
-constexpr int kUnroll = 4;             // 16-byte loads in flight per thread
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kUnroll = 4;             // vectors of a batch: 16-byte loads in flight per thread
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
-constexpr float kSlack = 20.0f;        // how far (in powers of two) an entry may lie above the running reference
+constexpr int kMaxSlots = 32;          // maxima a thread keeps of its batches (for finding the top entries again)
 constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 0 in fp32, and 0 * clamp stays 0
-constexpr int kStashVecs = 4352;       // 68 KB: three CTAs of a gradient kernel per SM
+constexpr int kStashVecs = 4224;       // 66 KB: three CTAs of a gradient kernel per SM
 constexpr size_t kRowsSmemLimit = 200 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -64,6 +66,15 @@ template <> struct RowVec<float> {
     __device__ static uint4 pack(const float (&x)[4]) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    __device__ static float vmax(const uint4 (&v)[kUnroll]) {
+        float m = neg_inf();
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            m = max_nan(m, max_nan(max_nan(__uint_as_float(v[u].x), __uint_as_float(v[u].y)),
+                                   max_nan(__uint_as_float(v[u].z), __uint_as_float(v[u].w))));
+        return m;
+    }
+    __device__ static uint4 masked() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
     __device__ static float get(const float* p) { return *p; }
     __device__ static void put(float* p, float x) { *p = x; }
 };
@@ -86,6 +97,20 @@ template <> struct RowVec<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ static float vmax(const uint4 (&v)[kUnroll]) {   // two entries per instruction, NaN kept
+        uint32_t m = 0xFF80FF80u;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            m = max2(m, max2(max2(v[u].x, v[u].y), max2(v[u].z, v[u].w)));
+        }
+        return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    }
+    __device__ static uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t y;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+        return y;
+    }
+    __device__ static uint4 masked() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
     __device__ static float get(const __nv_bfloat16* p) {
         return __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16);
     }
@@ -116,32 +141,90 @@ template <typename T> struct Share {
     }
 };
 
-// Running statistics of a thread's entries, all relative to `ref` (<= mx): s = sum 2^z, t = sum z 2^z.
+// Running statistics of a warp's entries.  Exponents are taken against rc, the rounded product m * c:
+// w(x) = fma(x, c, -rc) is then off by one rounding only; finish() moves the sums to m itself.
 struct Stats {
-    float ref, mx, s, t, tail;
-    __device__ __forceinline__ void init() { ref = mx = neg_inf(); s = t = tail = 0.0f; }
-    template <int N, bool kEntropy, bool kTail>
-    __device__ __forceinline__ void add(const float (&x)[N], float c, uint32_t top_bits) {
-        float vm = x[0];
+    float m, rc;              // the warp's maximum (all lanes alike)
+    float s, t, tail;         // this lane's sums over entries below m: 2^w, w 2^w; and 2^w outside the teacher's tokens (m included)
+    int cnt;                  // this lane's entries equal to m
+    __device__ __forceinline__ void init() { m = neg_inf(); rc = 0.0f; s = t = tail = 0.0f; cnt = 0; }
+    __device__ __forceinline__ static float product(float m, float c) { return fminf(fmaxf(m * c, -3.0e38f), 3.0e38f); }
+
+    template <typename T, bool kEntropy, bool kTail>
+    __device__ __forceinline__ void add(const uint4 (&v)[kUnroll], float lane_max, float c, const uint32_t (&top_bits)[kUnroll]) {
+        constexpr int N = RowVec<T>::N;
+        float wm = lane_max;
 #pragma unroll
-        for (int n = 1; n < N; ++n) vm = max_nan(vm, x[n]);
-        mx = max_nan(mx, vm);
-        if (vm == neg_inf()) return;             // nothing but masked entries
-        if (!((vm - ref) * c <= kSlack)) {       // rare: the first entries, or a far larger one (or NaN)
-            const float d = max_nan((ref - vm) * c, kFloorExp), f = ref == neg_inf() ? 0.0f : ex2(d);
-            t = f * fmaf(d, s, t);
-            s *= f;
-            tail *= f;
-            ref = vm;
+        for (int off = 16; off > 0; off >>= 1) wm = max_nan(wm, __shfl_xor_sync(0xFFFFFFFFu, wm, off));
+        if (wm < m) {
+            float bs = 0.0f, bt = 0.0f;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float x[N], vs = 0.0f;
+                RowVec<T>::unpack(v[u], x);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    const float w = exponent<kEntropy>(x[n], c);
+                    const float e = ex2(w);
+                    vs += e;
+                    if (kEntropy) bt = fmaf(e, w, bt);
+                    if (kTail) x[n] = e;
+                }
+                bs += vs;
+                if (kTail) tail += top_bits[u] == 0u ? vs : outside<N>(x, top_bits[u]);
+            }
+            s += bs;
+            t += bt;
+            return;
+        }
+        if (wm == neg_inf()) return;   // nothing but masked entries so far
+        if (!(wm == m)) {              // a new maximum: the old one becomes an entry like the others
+            const float rc_new = product(wm, c);
+            if (m != neg_inf()) {
+                const float d = fmaxf(rc - rc_new, kFloorExp), f = ex2(d);
+                const float w = fmaxf(fmaf(m, c, -rc_new), kFloorExp), e = (float)cnt * ex2(w);
+                t = fmaf(f, fmaf(d, s, t), e * w);
+                s = fmaf(f, s, e);
+                tail *= f;
+            }
+            m = wm;
+            rc = rc_new;
+            cnt = 0;
         }
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const float z = max_nan((x[n] - ref) * c, kFloorExp);
-            const float e = ex2(z);
-            s += e;
-            if (kEntropy) t = fmaf(e, z, t);
-            if (kTail) tail += ((top_bits >> n) & 1u) ? 0.0f : e;
+        for (int u = 0; u < kUnroll; ++u) {
+            float x[N], vs = 0.0f;
+            RowVec<T>::unpack(v[u], x);
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const float w = exponent<kEntropy>(x[n], c);
+                const float e = ex2(w);
+                const bool top = x[n] == m;
+                cnt += top ? 1 : 0;
+                vs += top ? 0.0f : e;
+                if (kEntropy) t = top ? t : fmaf(e, w, t);
+                if (kTail) x[n] = e;
+            }
+            s += vs;
+            if (kTail) tail += outside<N>(x, top_bits[u]);
         }
+    }
+    template <bool kEntropy> __device__ __forceinline__ float exponent(float x, float c) const {
+        const float w = fmaf(x, c, -rc);
+        return kEntropy ? fmaxf(w, kFloorExp) : w;   // a masked entry: 0 * kFloorExp instead of 0 * inf
+    }
+    template <int N> __device__ __forceinline__ static float outside(const float (&e)[N], uint32_t bits) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) sum += ((bits >> n) & 1u) ? 0.0f : e[n];
+        return sum;
+    }
+    __device__ __forceinline__ void finish(float c) {
+        if (m == neg_inf()) return;
+        const float d = fminf(fmaxf(fmaf(m, c, -rc), -100.0f), 100.0f), f = ex2(-d);   // rounding of rc: tiny, either sign
+        t = f * fmaf(-d, s, t);
+        s *= f;
+        tail *= f;
     }
 };
 
@@ -154,116 +237,105 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 struct RowsShared {
-    float red[3][kThreads / 32];
-    int red_cnt[kThreads / 32];
+    float w_m[kWarps], w_s[kWarps], w_t[kWarps], w_tail[kWarps];
+    int w_cnt[kWarps];
     Merged mine;                 // this CTA's statistics, read by the others of the cluster
-    int cand_n, thr_hits;
-    unsigned int scan[kThreads / 32];
-    // teacher (distill)
+    int cand_n;
+    unsigned int scan[kWarps];
+    // teacher (distill): warps 0..3 hold its entries, one per thread
     int t_id[kRowsMaxTop];
-    float t_q[kRowsMaxTop], t_x[kRowsMaxTop];
-    unsigned char t_first[kRowsMaxTop];
-    float t_mass, t_rest;        // sum of q, mass of the bucket (0: no bucket)
+    float t_q[kRowsMaxTop];
+    float t_max[kRowsMaxTop / 32];
+    double t_sum[kRowsMaxTop / 32];
+    float t_loss[kRowsMaxTop / 32];
+    int t_distinct, t_repeated;
 };
 
-// The block's statistics from its threads'.  Holders of the block's maximum go over their entries
-// once more and leave entries equal to it out of their sum, counting them instead.
-template <typename T, bool kEntropy>
-__device__ Merged block_merge(const Stats& st, const Share<T>& sh, float c, RowsShared& ss) {
-    constexpr int N = RowVec<T>::N;
+// The block's statistics from its warps'; complete in ss.mine after the next barrier.
+__device__ void block_merge(Stats& st, float c, RowsShared& ss) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float m = st.mx;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-    if (lane == 0) ss.red[0][warp] = m;
-    __syncthreads();
-    m = ss.red[0][0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 32; ++w) m = max_nan(m, ss.red[0][w]);
-    __syncthreads();
-    float s = 0.0f, t = 0.0f, tail = 0.0f;
-    int cnt = 0;
-    if (st.ref != neg_inf()) {
-        const float d = max_nan((st.ref - m) * c, kFloorExp), f = ex2(d);
-        s = st.s * f;
-        t = f * fmaf(d, st.s, st.t);
-        tail = st.tail * f;
-    }
-    if (st.mx == m && m != neg_inf()) {
-        s = t = 0.0f;
-        for (int j = sh.first + (int)threadIdx.x; j < sh.last; j += kThreads) {
-            float x[N];
-            RowVec<T>::unpack(sh.load(j), x);
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const float z = max_nan((x[n] - m) * c, kFloorExp), e = ex2(z);
-                if (x[n] == m) ++cnt;
-                else { s += e; if (kEntropy) t = fmaf(e, z, t); }
-            }
-        }
-    }
-    s = warp_sum(s);
-    if (kEntropy) t = warp_sum(t);
-    tail = warp_sum(tail);
+    st.finish(c);
+    const float s = warp_sum(st.s), t = warp_sum(st.t), tail = warp_sum(st.tail);
+    int cnt = st.cnt;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) cnt += __shfl_xor_sync(0xFFFFFFFFu, cnt, off);
-    if (lane == 0) { ss.red[0][warp] = s; ss.red[1][warp] = t; ss.red[2][warp] = tail; ss.red_cnt[warp] = cnt; }
+    if (lane == 0) { ss.w_m[warp] = st.m; ss.w_s[warp] = s; ss.w_t[warp] = t; ss.w_tail[warp] = tail; ss.w_cnt[warp] = cnt; }
     __syncthreads();
+    if (warp != 0) return;
+    const bool have = lane < kWarps;
+    const float wm = have ? ss.w_m[lane] : neg_inf();
+    float m = wm;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
     Merged r{m, 0.0f, 0.0f, 0.0f};
     cnt = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        r.rest += ss.red[0][w]; r.t += ss.red[1][w]; r.tail += ss.red[2][w]; cnt += ss.red_cnt[w];
+    if (have && wm != neg_inf()) {
+        const float ws = ss.w_s[lane], wt = ss.w_t[lane];
+        if (wm == m) {
+            r.rest = ws; r.t = wt; r.tail = ss.w_tail[lane]; cnt = ss.w_cnt[lane];
+        } else {
+            const float d = fmaxf((wm - m) * c, kFloorExp), f = ex2(d), all = ws + (float)ss.w_cnt[lane];
+            r.rest = f * all; r.t = f * fmaf(d, all, wt); r.tail = f * ss.w_tail[lane];
+        }
     }
+    r.rest = warp_sum(r.rest); r.t = warp_sum(r.t); r.tail = warp_sum(r.tail);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) cnt += __shfl_xor_sync(0xFFFFFFFFu, cnt, off);
     if (cnt > 1) r.rest += (float)(cnt - 1);
-    if (m == __uint_as_float(0x7F800000u)) r.rest = r.t = r.tail = __uint_as_float(0x7FC00000u);   // +inf: no distribution
-    return r;
+    if (!(m < __uint_as_float(0x7F800000u))) r.rest = r.t = r.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
+    if (lane == 0) ss.mine = r;
 }
 
 // The cluster's statistics from its CTAs' (already published and synchronised).
 __device__ Merged cluster_merge(cg::cluster_group& cluster, RowsShared& ss, int n_cta, float c) {
     if (n_cta == 1) return ss.mine;
-    Merged part[kRowsMaxCluster];
     float m = neg_inf();
     int base = 0;
 #pragma unroll 1
     for (int r = 0; r < n_cta; ++r) {
-        part[r] = *cluster.map_shared_rank(&ss.mine, r);
-        if (m == m && !(part[r].m <= m)) { m = part[r].m; base = r; }   // a NaN stays
+        const float pm = cluster.map_shared_rank(&ss.mine, r)->m;
+        if (m == m && !(pm <= m)) { m = pm; base = r; }   // a NaN stays
     }
-    Merged a{m, part[base].rest, part[base].t, part[base].tail};
-    if (m != m) { a.rest = m; return a; }
+    Merged a = *cluster.map_shared_rank(&ss.mine, base);
+    if (m != m) return a;
 #pragma unroll 1
     for (int r = 0; r < n_cta; ++r) {
-        if (r == base || part[r].m == neg_inf()) continue;
-        const float d = max_nan((part[r].m - m) * c, kFloorExp), f = ex2(d), s = part[r].rest + 1.0f;
-        a.rest = fmaf(f, s, a.rest);
-        a.t = fmaf(f, fmaf(d, s, part[r].t), a.t);
-        a.tail = fmaf(f, part[r].tail, a.tail);
+        const Merged part = *cluster.map_shared_rank(&ss.mine, r);
+        if (r == base || part.m == neg_inf()) continue;
+        const float d = fmaxf((part.m - m) * c, kFloorExp), f = ex2(d), all = part.rest + 1.0f;
+        a.rest = fmaf(f, all, a.rest);
+        a.t = fmaf(f, fmaf(d, all, part.t), a.t);
+        a.tail = fmaf(f, part.tail, a.tail);
     }
     return a;
 }
 
 // ---------------------------------------------------------------------------- the largest entries
-// Entries of the share with a key above `floor_key` (or not below it, with `or_equal`) go to the
-// candidate list; only threads whose maximum passes look at their entries again.
+// Entries of the share with a key of at least `key_min` go to the candidate list.  Each thread looks
+// at the maxima it kept of its batches and reads only those batches again that hold one.
 template <typename T>
-__device__ int collect(const Share<T>& sh, uint32_t my_key, uint32_t floor_key, bool or_equal, RowsShared& ss,
-                       unsigned long long* cand) {
+__device__ int collect(const Share<T>& sh, uint32_t my_key, uint32_t key_min, const uint32_t* slots, int slot_batches,
+                       RowsShared& ss, unsigned long long* cand) {
     constexpr int N = RowVec<T>::N;
     if (threadIdx.x == 0) ss.cand_n = 0;
     __syncthreads();
-    if (my_key > floor_key || (or_equal && my_key == floor_key)) {
-        for (int j = sh.first + (int)threadIdx.x; j < sh.last; j += kThreads) {
-            float x[N];
-            RowVec<T>::unpack(sh.load(j), x);
-            const int i0 = sh.entry0(j);
+    if (my_key >= key_min) {
+        int slot = 0;
+        for (int b0 = sh.first; b0 < sh.last; b0 += kUnroll * kThreads * slot_batches, ++slot) {
+            if (slots[slot * kThreads + threadIdx.x] < key_min) continue;
+            const int end = min(sh.last, b0 + kUnroll * kThreads * slot_batches);
+#pragma unroll 4
+            for (int j = b0 + (int)threadIdx.x; j < end; j += kThreads) {
+                float x[N];
+                RowVec<T>::unpack(sh.load(j), x);
+                const int i0 = sh.entry0(j);
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const uint32_t key = logit_key(x[n]);
-                if ((key > floor_key || (or_equal && key == floor_key)) && i0 + n >= 0 && i0 + n < sh.V) {
-                    const int at = atomicAdd(&ss.cand_n, 1);
-                    if (at < kCandCap) cand[at] = pack_best(key, (uint32_t)(i0 + n));
+                for (int n = 0; n < N; ++n) {
+                    const uint32_t key = logit_key(x[n]);
+                    if (key >= key_min && i0 + n >= 0 && i0 + n < sh.V) {
+                        const int at = atomicAdd(&ss.cand_n, 1);
+                        if (at < kCandCap) cand[at] = pack_best(key, (uint32_t)(i0 + n));
+                    }
                 }
             }
         }
@@ -280,6 +352,7 @@ __device__ int count_at_least(const Share<T>& sh, uint32_t key_min, RowsShared& 
     if (threadIdx.x == 0) ss.cand_n = 0;
     __syncthreads();
     int n_mine = 0;
+#pragma unroll 4
     for (int j = sh.first + (int)threadIdx.x; j < sh.last; j += kThreads) {
         float x[N];
         RowVec<T>::unpack(sh.load(j), x);
@@ -321,7 +394,7 @@ __device__ void collect_ties(const Share<T>& sh, uint32_t key, int need, int at,
         __syncthreads();
         unsigned int before = 0, total = 0;
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) { if (w < warp) before += ss.scan[w]; total += ss.scan[w]; }
+        for (int w = 0; w < kWarps; ++w) { if (w < warp) before += ss.scan[w]; total += ss.scan[w]; }
         int pos = found + (int)(before + incl - mine);
         for (int n = 0; n < N; ++n)
             if ((bits >> n) & 1u) {
@@ -339,8 +412,8 @@ __device__ void collect_ties(const Share<T>& sh, uint32_t key, int need, int at,
 // entries above it are collected, a few more than k as a rule.  Where that overflows the list (many
 // equal entries, or k large ones in few threads) the k-th largest key is found exactly.
 template <typename T>
-__device__ void top_of_share(const Share<T>& sh, float thread_max, int k, RowsShared& ss, unsigned long long* cand,
-                             unsigned long long* sorted) {
+__device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const uint32_t* slots, int slot_batches,
+                             RowsShared& ss, unsigned long long* cand, unsigned long long* sorted) {
     // a thread without an entry has key 0; padding and masked entries have the key of -inf
     const bool any = sh.first + (int)threadIdx.x < sh.last;
     const uint32_t my_key = any ? logit_key(thread_max) : 0u;
@@ -348,9 +421,9 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, RowsSh
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t c = thr | (1u << bit);
         const int n = __syncthreads_count(my_key >= c);
-        if (n >= k) { thr = c; if (n <= 2 * k) break; }
+        if (n >= k) { thr = c; if (n <= k + (k >> 1)) break; }
     }
-    int n = collect(sh, my_key, thr, true, ss, cand);
+    int n = collect(sh, my_key, thr, slots, slot_batches, ss, cand);
     if (n > kCandCap) {
         // exact: the k-th largest key of the share.  First guess: the exact k-th largest thread
         // maximum, which is it whenever fewer than k entries lie above (a row full of equal entries).
@@ -367,7 +440,7 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, RowsSh
             }
             kth = lo;
         }
-        n = kth == 0xFFFFFFFFu ? 0 : collect(sh, my_key, kth, false, ss, cand);   // fewer than k
+        n = kth == 0xFFFFFFFFu ? 0 : collect(sh, my_key, kth + 1u, slots, slot_batches, ss, cand);   // fewer than k
         collect_ties(sh, kth, k - n, n, ss, cand);
         n = k;
         __syncthreads();
@@ -377,6 +450,7 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, RowsSh
     for (int i = threadIdx.x; i < n; i += kThreads) {   // the packed words are all different: rank by counting
         const unsigned long long mine = cand[i];
         int rank = 0;
+#pragma unroll 8
         for (int o = 0; o < n; ++o) rank += cand[o] > mine ? 1 : 0;
         if (rank < k) sorted[rank] = mine;
     }
@@ -389,51 +463,10 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, RowsSh
 //   bucket  q = exp(v), the rest of the mass q_t = max(0, 1 - sum q) against the student's mass
 //           p_t outside the teacher's tokens:          L = sum q (log q - log p) + q_t (log q_t - log p_t)
 //   dL/dz_j = M p_j - q_j - [j is no teacher token] (q_t / p_t) p_j,   M = sum q + q_t;   dL/dx = dL/dz / T.
-// k values per row: fp64 throughout, so that 1 - sum q keeps what fp32 values carry.
-__device__ void distill_teacher(const RowsParams& P, int row, RowsShared& ss) {
-    const int lane = threadIdx.x & 31;
-    if (threadIdx.x < 32) {
-        double vmax = -INFINITY;
-        for (int i = lane; i < P.k; i += 32) {
-            const bool have = ss.t_id[i] >= 0;
-            if (have) vmax = fmax(vmax, (double)P.t_logprob[(long long)row * P.k + i]);
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) vmax = fmax(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, off));
-        const double shift = P.tail == DM_TAIL_RENORM && vmax > -INFINITY ? vmax : 0.0;
-        double e[kRowsMaxTop / 32], sum = 0.0;
-        int distinct = 0;
-#pragma unroll
-        for (int u = 0; u < kRowsMaxTop / 32; ++u) {
-            const int i = lane + 32 * u;
-            e[u] = 0.0;
-            if (i < P.k && ss.t_id[i] >= 0) {
-                e[u] = exp((double)P.t_logprob[(long long)row * P.k + i] - shift);
-                sum += e[u];
-                bool first = true;
-                for (int o = 0; o < i; ++o) first = first && ss.t_id[o] != ss.t_id[i];
-                ss.t_first[i] = first;
-                distinct += first;
-            } else if (i < P.k) {
-                ss.t_first[i] = 0;
-            }
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) {
-            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
-            distinct += __shfl_xor_sync(0xFFFFFFFFu, distinct, off);
-        }
-        const double scale = P.tail == DM_TAIL_RENORM ? (sum != 0.0 ? 1.0 / sum : 0.0) : 1.0;
-#pragma unroll
-        for (int u = 0; u < kRowsMaxTop / 32; ++u)
-            if (lane + 32 * u < P.k) ss.t_q[lane + 32 * u] = (float)(e[u] * scale);
-        if (lane == 0) {
-            ss.t_mass = (float)(sum * scale);
-            const double rest = 1.0 - sum;
-            ss.t_rest = P.tail == DM_TAIL_BUCKET && distinct < P.V ? (rest < 0.0 ? 0.0f : (float)rest) : 0.0f;
-        }
-    }
-}
+// One thread per entry.  q is computed and summed in fp64: 1 - sum q then keeps what the fp32 values
+// carry.  A bitmap of the share's teacher tokens serves the sum of the tail (p_t would lose its
+// precision as a difference) and tells entries that name the same token apart.
+struct TeacherEntry { int id; float v, x; bool first; double q; };
 
 // ------------------------------------------------------------------------------------ the kernel
 template <typename T, int kOp>
@@ -447,11 +480,12 @@ rows_kernel(const RowsParams P) {
     uint32_t* bitmap = reinterpret_cast<uint32_t*>(stash + P.stash_vecs);               // distill: teacher tokens of the share
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // logprobs: candidates, then the sorted list
     unsigned long long* sorted = cand + kCandCap;
-    unsigned long long* merged = sorted + kRowsMaxTop;                                  // rank 0: every CTA's list
+    uint32_t* slots = reinterpret_cast<uint32_t*>(sorted + kRowsMaxTop);                // maxima of the threads' batches
+    unsigned long long* merged = cand;                                                  // rank 0: every CTA's list (the candidates are done with)
 
     cg::cluster_group cluster = cg::this_cluster();
     const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int row = (int)(blockIdx.x / (unsigned)n_cta), tid = threadIdx.x;
+    const int row = (int)(blockIdx.x / (unsigned)n_cta), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float c = P.c;
 
     Share<T> sh;
@@ -478,27 +512,46 @@ rows_kernel(const RowsParams P) {
         g_h = P.g_entropy != nullptr ? P.g_entropy[row] : 0.0f;
         zero_grad = g_lp == 0.0f && g_h == 0.0f;
     }
+    const bool use_bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad_row != nullptr);
+    TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
     if (kOp == OP_DISTILL) {
         if (P.weight != nullptr) { const float wt = P.weight[row]; zero_grad = wt == 0.0f; w *= wt; }
-        for (int i = tid; i < P.k; i += kThreads) {
-            int id = P.t_ids[(long long)row * P.k + i];
-            if (id < 0 || id >= P.V) id = -1;
-            ss.t_id[i] = id;
-            ss.t_x[i] = id >= 0 ? RowVec<T>::get(sh.row + id) : neg_inf();
+        if (tid < P.k) {
+            te.id = P.t_ids[(long long)row * P.k + tid];
+            te.v = P.t_logprob[(long long)row * P.k + tid];
+            if (te.id < 0 || te.id >= P.V) te.id = -1;
+            if (te.id >= 0) te.x = RowVec<T>::get(sh.row + te.id);
+            ss.t_id[tid] = te.id;
         }
-        if (P.tail == DM_TAIL_BUCKET) {
-            const int n_words = (per * N + 31) / 32;
-            for (int i = tid; i < n_words; i += kThreads) bitmap[i] = 0u;
+        if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }
+        if (use_bits)
+            for (int i = tid; i < (per * N + 31) / 32; i += kThreads) bitmap[i] = 0u;
+        if (warp < kRowsMaxTop / 32) {
+            float vm = te.id >= 0 ? te.v : neg_inf();
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+            if (lane == 0) ss.t_max[warp] = vm;
         }
         __syncthreads();
-        distill_teacher(P, row, ss);
-        if (P.tail == DM_TAIL_BUCKET) {
-            for (int i = tid; i < P.k; i += kThreads) {
-                const int u = ss.t_id[i] + sh.phase - sh.first * N;     // position within the share
-                if (ss.t_id[i] >= 0 && u >= 0 && u < (sh.last - sh.first) * N) atomicOr(&bitmap[u >> 5], 1u << (u & 31));
+        if (use_bits && te.id >= 0) {
+            const int u = te.id + sh.phase - sh.first * N;     // position within the share
+            if (u >= 0 && u < (sh.last - sh.first) * N) {
+                te.first = ((atomicOr(&bitmap[u >> 5], 1u << (u & 31)) >> (u & 31)) & 1u) == 0u;
+                if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
             }
         }
         __syncthreads();
+        if (warp < kRowsMaxTop / 32) {
+            float vm = ss.t_max[0];
+#pragma unroll
+            for (int i = 1; i < kRowsMaxTop / 32; ++i) vm = fmaxf(vm, ss.t_max[i]);
+            const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
+            if (te.id >= 0) te.q = exp((double)te.v - shift);
+            double sum = te.q;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+            if (lane == 0) ss.t_sum[warp] = sum;      // read behind the barriers below
+        }
     }
 
     // A row whose gradient is zero whatever it holds is not read (unless its loss is wanted).
@@ -507,31 +560,38 @@ rows_kernel(const RowsParams P) {
     if (need_stats) {
         Stats st;
         st.init();
-        for (int j0 = sh.first + tid; j0 < sh.last; j0 += kUnroll * kThreads) {
+        float thread_max = neg_inf();
+        int batch = 0;
+        for (int b0 = sh.first; b0 < sh.last; b0 += kUnroll * kThreads, ++batch) {   // the same for the whole block
             uint4 v[kUnroll];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-                if (j0 + u * kThreads < sh.last) v[u] = sh.load(j0 + u * kThreads);
+            uint32_t bits[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                const int j = j0 + u * kThreads;
-                if (j >= sh.last) break;
-                if (kOp != OP_LOGPROBS && j - sh.first < P.stash_vecs) stash[j - sh.first] = v[u];
-                float x[N];
-                RowVec<T>::unpack(v[u], x);
-                uint32_t top_bits = 0;
-                if (kTail && P.tail == DM_TAIL_BUCKET) {
-                    const int at = (j - sh.first) * N;
-                    top_bits = bitmap[at >> 5] >> (at & 31);
-                }
-                st.add<N, kEntropy, kTail>(x, c, top_bits);
+                const int j = b0 + u * kThreads + tid;
+                v[u] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
             }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int at = b0 - sh.first + u * kThreads + tid;
+                if (kOp != OP_LOGPROBS && at < P.stash_vecs) stash[at] = v[u];   // (the stash never exceeds the share)
+                bits[u] = 0u;
+                if (kTail && P.tail == DM_TAIL_BUCKET && at < per) bits[u] = (bitmap[(at * N) >> 5] >> ((at * N) & 31)) & ((1u << N) - 1u);
+            }
+            const float lane_max = RowVec<T>::vmax(v);
+            if (kOp == OP_LOGPROBS && P.n_top > 0) {
+                const int at = batch / P.slot_batches * kThreads + tid;
+                const uint32_t key = logit_key(lane_max);
+                slots[at] = batch % P.slot_batches == 0 || key > slots[at] ? key : slots[at];
+                thread_max = max_nan(thread_max, lane_max);
+            }
+            st.add<T, kEntropy, kTail>(v, lane_max, c, bits);
         }
-        const Merged mine = block_merge<T, kEntropy>(st, sh, c, ss);
-        if (tid == 0) ss.mine = mine;
-        if (kOp == OP_LOGPROBS && P.n_top > 0) top_of_share(sh, st.mx, P.n_top, ss, cand, sorted);
+        block_merge(st, c, ss);
+        if (kOp == OP_LOGPROBS && P.n_top > 0) top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, cand, sorted);
         if (n_cta > 1) cluster.sync(); else __syncthreads();
         a = cluster_merge(cluster, ss, n_cta, c);
+    } else {
+        __syncthreads();
     }
     const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
     const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
@@ -551,13 +611,14 @@ rows_kernel(const RowsParams P) {
             // merge of sorted lists: the rank of an entry is its place in its own list plus the number
             // of larger ones in each other list
             const int k = P.n_top;
-            for (int i = tid; i < n_cta * k; i += kThreads) {
-                const unsigned long long* theirs = n_cta == 1 ? sorted : cluster.map_shared_rank(sorted, i / k);
-                merged[i] = theirs[i % k];
+            const unsigned long long* lists = sorted;
+            if (n_cta > 1) {
+                for (int i = tid; i < n_cta * k; i += kThreads) merged[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
+                __syncthreads();
+                lists = merged;
             }
-            __syncthreads();
             for (int i = tid; i < n_cta * k; i += kThreads) {
-                const unsigned long long mine = merged[i];
+                const unsigned long long mine = lists[i];
                 if (mine == 0ull) continue;
                 int place = i % k;
                 for (int r = 0; r < n_cta && place < k; ++r) {
@@ -565,7 +626,7 @@ rows_kernel(const RowsParams P) {
                     int lo = 0, hi = k;       // entries of list r that are larger
                     while (lo < hi) {
                         const int mid = (lo + hi) >> 1;
-                        if (merged[r * k + mid] > mine) lo = mid + 1; else hi = mid;
+                        if (lists[r * k + mid] > mine) lo = mid + 1; else hi = mid;
                     }
                     place += lo;
                 }
@@ -580,54 +641,79 @@ rows_kernel(const RowsParams P) {
         }
     }
 
-    float tail_factor = 0.0f;   // q_t / (sum of the tail's exponentials)
+    float mass = 0.0f, rest = 0.0f;   // sum of the teacher's q, mass of its bucket (0: no bucket)
     if (kOp == OP_DISTILL) {
-        if (ss.t_rest > 0.0f && a.tail > 0.0f) tail_factor = ss.t_rest / a.tail;
-        if (rank == 0 && P.out_loss != nullptr && tid < 32) {
-            double loss = 0.0;
-            const double log_tot = log1p((double)a.rest);
-            for (int i = tid; i < P.k; i += 32) {
-                const float q = ss.t_q[i];
-                if (ss.t_id[i] < 0 || q == 0.0f) continue;
-                const float x = ss.t_x[i];
-                const double logp = dead || x == neg_inf() ? -INFINITY : ((double)x - (double)a.m) * P.inv_temp_d - log_tot;
-                loss += (double)q * (log((double)q) - logp);
-            }
+        double sum = 0.0;
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, off);
-            if (tid == 0) {
-                const double qt = ss.t_rest;
-                if (qt > 0.0 && !(dead && ss.t_mass == 0.0f)) loss += qt * (log(qt) - (log((double)a.tail) - log_tot));
-                P.out_loss[row] = (float)loss;
+        for (int i = 0; i < kRowsMaxTop / 32; ++i) sum += ss.t_sum[i];
+        const double scale = P.tail == DM_TAIL_RENORM ? (sum != 0.0 ? 1.0 / sum : 0.0) : 1.0;
+        mass = (float)(sum * scale);
+        // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
+        if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
+        if (warp < kRowsMaxTop / 32) {
+            const float q = (float)(te.q * scale);
+            if (tid < P.k) ss.t_q[tid] = q;
+            if (rank == 0 && P.out_loss != nullptr) {
+                // log q = v - shift - log(sum): no logarithm per entry
+                float vm = ss.t_max[0];
+#pragma unroll
+                for (int i = 1; i < kRowsMaxTop / 32; ++i) vm = fmaxf(vm, ss.t_max[i]);
+                const float log_sum = P.tail == DM_TAIL_RENORM && sum > 0.0 ? logf((float)sum) : 0.0f;
+                const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + (double)log_sum : 0.0;
+                float term = 0.0f;
+                if (te.id >= 0 && !(q == 0.0f)) {
+                    const double logp = dead || te.x == neg_inf() ? -INFINITY : ((double)te.x - (double)a.m) * P.inv_temp_d - (double)log_total;
+                    term = (float)((double)q * (((double)te.v - base) - logp));
+                }
+                term = warp_sum(term);
+                if (lane == 0) ss.t_loss[warp] = term;
             }
+        }
+        __syncthreads();
+        if (rank == 0 && tid == 0 && P.out_loss != nullptr) {
+            float loss = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kRowsMaxTop / 32; ++i) loss += ss.t_loss[i];
+            if (rest != 0.0f && !(dead && mass == 0.0f)) loss += rest * (logf(rest) - (logf(a.tail) - log_total));
+            P.out_loss[row] = loss;
         }
     }
 
     if (kOp != OP_LOGPROBS && grad_row != nullptr) {
-        // logprobs: dx = p (A + B z), z in powers of two;  distill: dx = p A, less the bucket's share outside the top
-        float A = 0.0f, B = 0.0f, A_top = 0.0f;
+        // with w = (x - m) c in powers of two:  logprobs  dx = 2^w (A + B w);  distill  dx = 2^w A, A taking
+        // the bucket's share off every entry (the teacher's tokens are written over below)
         const bool none = zero_grad || dead;
+        float A, B = 0.0f, A_top = 0.0f;
         if (kOp == OP_GRAD) {
             A = -w * inv_total * fmaf(g_h, entropy - log_total, g_lp);
             B = -w * inv_total * g_h * kLn2;
         } else {
-            const float mass = ss.t_mass + ss.t_rest;
-            A_top = w * mass * inv_total;
-            A = w * fmaf(mass, inv_total, -tail_factor);
+            const float tail_factor = rest > 0.0f && a.tail > 0.0f ? rest / a.tail : 0.0f;   // q_t / (sum of the tail's exponentials)
+            A_top = w * (mass + rest) * inv_total;
+            A = w * fmaf(mass + rest, inv_total, -tail_factor);
         }
         const bool same_phase = (int)((reinterpret_cast<uintptr_t>(grad_row) & 15u) / sizeof(T)) == sh.phase;
+#pragma unroll 4
         for (int j = sh.first + tid; j < sh.last; j += kThreads) {
             float x[N];
-            if (!none) RowVec<T>::unpack(j - sh.first < P.stash_vecs ? stash[j - sh.first] : sh.load(j), x);
+            if (none) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                if (none) { x[n] = 0.0f; continue; }
-                const float z = max_nan((x[n] - a.m) * c, kFloorExp);
-                x[n] = kOp == OP_GRAD ? ex2(z) * fmaf(B, z, A) : ex2(z) * A;
+                for (int n = 0; n < N; ++n) x[n] = 0.0f;
+            } else {
+                RowVec<T>::unpack(j - sh.first < P.stash_vecs ? stash[j - sh.first] : sh.load(j), x);
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    if (kOp == OP_GRAD) {
+                        const float z = fmaxf((x[n] - a.m) * c, kFloorExp);
+                        x[n] = ex2(z) * fmaf(B, z, A);
+                    } else {
+                        x[n] = ex2((x[n] - a.m) * c) * A;
+                    }
+                }
             }
             const int i0 = sh.entry0(j);
             if (sh.whole(j) && same_phase) {
-                *reinterpret_cast<uint4*>(grad_row + i0) = RowVec<T>::pack(x);
+                __stcs(reinterpret_cast<uint4*>(grad_row + i0), RowVec<T>::pack(x));
             } else {
 #pragma unroll
                 for (int n = 0; n < N; ++n)
@@ -639,21 +725,20 @@ rows_kernel(const RowsParams P) {
             const int lo = sh.entry0(sh.first), hi = sh.entry0(sh.last);   // this share's entries
             if (kOp == OP_GRAD) {
                 if (tid == 0 && tok >= 0 && tok >= lo && tok < hi) {   // (entries below 0 are the padding of the first vector)
-                    const float z = max_nan((tok_x - a.m) * c, kFloorExp), e = ex2(z);
+                    const float z = fmaxf((tok_x - a.m) * c, kFloorExp), e = ex2(z);
                     // 1 - p of the largest entry is rest / total, without cancellation
                     const float one_less = tok_x == a.m ? a.rest * inv_total : 1.0f - e * inv_total;
                     const float by_entropy = -w * g_h * inv_total * e * fmaf(kLn2, z, entropy - log_total);
                     RowVec<T>::put(grad_row + tok, fmaf(w * g_lp, one_less, by_entropy));
                 }
-            } else {
-                for (int i = tid; i < P.k; i += kThreads) {
-                    const int id = ss.t_id[i];
-                    if (id < 0 || id < lo || id >= hi || !ss.t_first[i]) continue;
-                    float q = 0.0f;
-                    for (int o = i; o < P.k; ++o) q += ss.t_id[o] == id ? ss.t_q[o] : 0.0f;
-                    const float e = ex2(max_nan((ss.t_x[i] - a.m) * c, kFloorExp));
-                    RowVec<T>::put(grad_row + id, fmaf(A_top, e, -w * q));
+            } else if (te.first) {                       // (set only for tokens of this share)
+                float q = ss.t_q[tid];
+                if (ss.t_repeated) {
+                    q = 0.0f;
+                    for (int o = 0; o < P.k; ++o) q += ss.t_id[o] == te.id ? ss.t_q[o] : 0.0f;
                 }
+                const float e = ex2((te.x - a.m) * c);
+                RowVec<T>::put(grad_row + te.id, fmaf(A_top, e, -w * q));
             }
         }
     }
@@ -674,7 +759,7 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
     // CTAs per row: enough of them to fill the GPU where rows are few, not less than one vector per
     // thread; gradient kernels cut a row until a share fits their part of shared memory.
     int cluster = 1;
-    while (cluster < kRowsMaxCluster && (long long)P.rows * cluster < 4ll * sms && n_vec > cluster * kThreads) cluster *= 2;
+    while (cluster < kRowsMaxCluster && (long long)P.rows * cluster < 3ll * sms && n_vec > cluster * kThreads) cluster *= 2;
     if (grad)
         while (cluster < kRowsMaxCluster && (n_vec + cluster - 1) / cluster > kStashVecs) cluster *= 2;
     auto kern = rows_kernel<T, kOp>;
@@ -683,9 +768,13 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
         const int per = (n_vec + cluster - 1) / cluster;
         P.stash_vecs = grad ? (per < kStashVecs ? per : kStashVecs) : 0;
         smem = (size_t)P.stash_vecs * 16;
-        if (kOp == OP_DISTILL && P.tail == DM_TAIL_BUCKET) smem += ((size_t)per * N + 31) / 32 * 4;
-        if (kOp == OP_LOGPROBS && P.n_top > 0)
-            smem += (size_t)(kCandCap + kRowsMaxTop + cluster * P.n_top) * sizeof(unsigned long long);
+        if (kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad)) smem += ((size_t)per * N + 31) / 32 * 4;
+        if (kOp == OP_LOGPROBS && P.n_top > 0) {
+            const int batches = (per + kUnroll * kThreads - 1) / (kUnroll * kThreads);
+            P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
+            const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
+            smem += (size_t)(kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + (size_t)n_slots * kThreads * sizeof(uint32_t);
+        }
         if (smem <= kRowsSmemLimit) break;
         if (cluster >= kRowsMaxCluster) return DM_EUNSUPPORTED;
     }

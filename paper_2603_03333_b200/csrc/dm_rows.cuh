@@ -16,6 +16,7 @@ struct RowsParams {
     float c;              // log2(e) / T
     double inv_temp_d;
     int stash_vecs;       // 16-byte vectors of a CTA's share kept in shared memory (gradient kernels; set by the launch)
+    int slot_batches;     // batches of a thread that share one remembered maximum (set by the launch)
     const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
     // logprobs
     const int32_t* tokens;
