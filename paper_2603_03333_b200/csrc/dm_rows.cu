@@ -25,18 +25,28 @@
 
 namespace dm {
 
+#ifndef DM_ROWS_THREADS
+#define DM_ROWS_THREADS 256
+#endif
+#ifndef DM_ROWS_MINB
+#define DM_ROWS_MINB 4
+#endif
+#ifndef DM_ROWS_MINR
+#define DM_ROWS_MINR 3
+#endif
+
 namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = DM_ROWS_THREADS;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;             // vectors of a batch: 16-byte loads in flight per thread
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
 constexpr int kMaxSlots = 32;          // maxima a thread keeps of its batches (for finding the top entries again)
 constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 0 in fp32, and 0 * clamp stays 0
-constexpr int kStashVecs = 4224;       // 66 KB: three CTAs of a gradient kernel per SM
-constexpr size_t kRowsSmemLimit = 200 * 1024;
+constexpr int kStashVecs = 4096;       // share of a gradient kernel's CTA up to which a row is cut: 64 KB, three CTAs per SM
+constexpr size_t kRowsSmemLimit = 216 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
 enum { OP_LOGPROBS = 0, OP_GRAD = 1, OP_DISTILL = 2 };
@@ -50,6 +60,34 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
     float y;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
+}
+// Two fp32 values in one 64-bit register pair: sm_100 has packed fp32 arithmetic, two entries per instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+    f32x2 p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ void unpair(f32x2 p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum2(f32x2 p) {
+    float lo, hi;
+    unpair(p, lo, hi);
+    return lo + hi;
 }
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
 
@@ -66,6 +104,19 @@ template <> struct RowVec<float> {
     __device__ static uint4 pack(const float (&x)[4]) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    __device__ static void pairs(const uint4& v, f32x2 (&x)[2]) {
+        x[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+        x[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+    }
+    __device__ static uint4 pack_pairs(const f32x2 (&x)[2]) {
+        uint4 v;
+        asm("mov.b64 {%0, %1}, %2;" : "=r"(v.x), "=r"(v.y) : "l"(x[0]));
+        asm("mov.b64 {%0, %1}, %2;" : "=r"(v.z), "=r"(v.w) : "l"(x[1]));
+        return v;
+    }
+    static constexpr bool kFloorsEntries = false;   // exponents are clamped one by one
+    __device__ static uint32_t floor_word(float) { return 0u; }
+    __device__ static void raise(uint4&, uint32_t) {}
     __device__ static float vmax(const uint4 (&v)[kUnroll]) {
         float m = neg_inf();
 #pragma unroll
@@ -75,6 +126,15 @@ template <> struct RowVec<float> {
         return m;
     }
     __device__ static uint4 masked() { return make_uint4(0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u); }
+    // Which entries equal m (one bit each); they become -inf.
+    __device__ static uint32_t take(uint4& v, float m) {
+        uint32_t eq = 0;
+        if (__uint_as_float(v.x) == m) { eq |= 1u; v.x = 0xFF800000u; }
+        if (__uint_as_float(v.y) == m) { eq |= 2u; v.y = 0xFF800000u; }
+        if (__uint_as_float(v.z) == m) { eq |= 4u; v.z = 0xFF800000u; }
+        if (__uint_as_float(v.w) == m) { eq |= 8u; v.w = 0xFF800000u; }
+        return eq;
+    }
     __device__ static float get(const float* p) { return *p; }
     __device__ static void put(float* p, float x) { *p = x; }
 };
@@ -97,6 +157,33 @@ template <> struct RowVec<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    __device__ static void pairs(const uint4& v, f32x2 (&x)[4]) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int n = 0; n < 4; ++n) x[n] = pair(__uint_as_float(w[n] << 16), __uint_as_float(w[n] & 0xFFFF0000u));
+    }
+    __device__ static uint4 pack_pairs(const f32x2 (&x)[4]) {   // the one rounding of a bf16 gradient, to nearest
+        uint32_t w[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            float lo, hi;
+            unpair(x[n], lo, hi);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+            w[n] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static constexpr bool kFloorsEntries = true;    // entries are raised to a floor, two per instruction, before they are unpacked
+    __device__ static uint32_t floor_word(float x) {
+        const __nv_bfloat16 f = __float2bfloat16_rd(fmaxf(x, -3.3e38f));
+        return (uint32_t)*reinterpret_cast<const unsigned short*>(&f) * 0x10001u;
+    }
+    __device__ static void raise(uint4& v, uint32_t floor2) {
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(floor2));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(floor2));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(v.z) : "r"(floor2));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(v.w) : "r"(floor2));
+    }
     __device__ static float vmax(const uint4 (&v)[kUnroll]) {   // two entries per instruction, NaN kept
         uint32_t m = 0xFF80FF80u;
 #pragma unroll
@@ -111,11 +198,34 @@ template <> struct RowVec<__nv_bfloat16> {
         return y;
     }
     __device__ static uint4 masked() { return make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+    __device__ static uint32_t take_pair(uint32_t& v, uint32_t mm) {
+        uint32_t eq;   // all ones in the halves that compare equal
+        asm("set.eq.u32.bf16x2 %0, %1, %2;" : "=r"(eq) : "r"(v), "r"(mm));
+        v = (v & ~eq) | (0xFF80FF80u & eq);
+        return (eq & 1u) | ((eq >> 15) & 2u);
+    }
+    __device__ static uint32_t take(uint4& v, float m) {   // m is a bf16 value
+        const uint32_t mm = (__float_as_uint(m) >> 16) * 0x10001u;
+        return take_pair(v.x, mm) | (take_pair(v.y, mm) << 2) | (take_pair(v.z, mm) << 4) | (take_pair(v.w, mm) << 6);
+    }
     __device__ static float get(const __nv_bfloat16* p) {
         return __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16);
     }
     __device__ static void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
+
+// Asynchronous 16-byte copies global -> shared memory, one group per batch; a thread waits for its own.
+__device__ __forceinline__ void copy_async(uint4* dst, const uint4* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait(int newer) {   // all but the `newer` latest groups have landed (or more)
+    if (newer <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else if (newer == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (newer == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else asm volatile("cp.async.wait_group 4;" ::: "memory");
+}
 
 // A CTA's share of a row: 16-byte vectors [first, last) of the row, vector j holding entries
 // j*N - phase .. j*N - phase + N-1 (phase: entries between the 16-byte boundary below the row's
@@ -123,105 +233,135 @@ template <> struct RowVec<__nv_bfloat16> {
 template <typename T> struct Share {
     const T* row;
     int V, phase, first, last;
+    int whole_lo, whole_hi;   // vectors of the row that hold N of its entries
     __device__ __forceinline__ int entry0(int j) const { return j * RowVec<T>::N - phase; }
-    __device__ __forceinline__ bool whole(int j) const {
-        const int i0 = entry0(j);
-        return i0 >= 0 && i0 + RowVec<T>::N <= V;
-    }
+    __device__ __forceinline__ bool whole(int j) const { return j >= whole_lo && j < whole_hi; }
+    __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(row - phase); }
     // Loads go to L2 (ld.global.cg): the row may be overwritten in place by this very kernel, each
     // entry by the thread that read it.
     __device__ __forceinline__ uint4 load(int j) const {
         constexpr int N = RowVec<T>::N;
-        if (whole(j)) return __ldcg(reinterpret_cast<const uint4*>(row + (long long)j * N - phase));
+        if (whole(j)) return __ldcg(vectors() + j);
         float x[N];
         const int i0 = entry0(j);
 #pragma unroll
         for (int n = 0; n < N; ++n) x[n] = (i0 + n >= 0 && i0 + n < V) ? RowVec<T>::get(row + i0 + n) : neg_inf();
         return RowVec<T>::pack(x);
     }
+    // one batch: vectors b0 + u * kThreads + thread, masked past the end of the share
+    __device__ __forceinline__ void load_batch(int b0, uint4 (&v)[kUnroll]) const {
+        const int j = b0 + (int)threadIdx.x;
+        if (b0 >= whole_lo && b0 + kUnroll * kThreads <= min(last, whole_hi)) {
+            const uint4* p = vectors() + j;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) v[u] = __ldcg(p + u * kThreads);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) v[u] = j + u * kThreads < last ? load(j + u * kThreads) : RowVec<T>::masked();
+        }
+    }
 };
 
 // Running statistics of a warp's entries.  Exponents are taken against rc, the rounded product m * c:
-// w(x) = fma(x, c, -rc) is then off by one rounding only; finish() moves the sums to m itself.
+// w(x) = fma(x, ce, -rc) is then off by one rounding only; finish() moves the sums to m itself.  Where
+// |m| c is beyond 1e37 (a row of nothing but the type's lowest value, say) every other entry is
+// thousands of powers of two below m and adds nothing: ce = 0 says so.
 struct Stats {
-    float m, rc;              // the warp's maximum (all lanes alike)
+    float m, rc, ce;          // the warp's maximum (all lanes alike), and how exponents are taken
+    uint32_t floor2;          // bf16: entries below this are raised to it (250 powers of two below m)
     float s, t, tail;         // this lane's sums over entries below m: 2^w, w 2^w; and 2^w outside the teacher's tokens (m included)
     int cnt;                  // this lane's entries equal to m
-    __device__ __forceinline__ void init() { m = neg_inf(); rc = 0.0f; s = t = tail = 0.0f; cnt = 0; }
-    __device__ __forceinline__ static float product(float m, float c) { return fminf(fmaxf(m * c, -3.0e38f), 3.0e38f); }
+    __device__ __forceinline__ void init() {
+        m = neg_inf(); rc = ce = 0.0f; s = t = tail = 0.0f; cnt = 0; floor2 = 0u;
+    }
+    __device__ __forceinline__ float of_maximum() const { return ce != 0.0f ? ex2(fmaf(m, ce, -rc)) : 1.0f; }
 
+    // Exponents are taken against `top` from here on (the sums are not moved).
+    template <typename T> __device__ __forceinline__ void set_maximum(float top, float c) {
+        m = top;
+        rc = top * c;
+        ce = fabsf(rc) <= 1e37f ? c : 0.0f;
+        floor2 = RowVec<T>::floor_word(top - 250.0f / c);
+        cnt = 0;
+    }
+    // Entries equal to the maximum are counted and taken out of the batch.
+    template <typename T, bool kTail>
+    __device__ __forceinline__ void take(uint4 (&v)[kUnroll], const uint32_t (&top_bits)[kUnroll]) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const uint32_t eq = RowVec<T>::take(v[u], m);
+            cnt += __popc(eq);
+            if (kTail) tail = fmaf((float)__popc(eq & ~top_bits[u]), of_maximum(), tail);
+        }
+    }
+    // A batch of entries below the maximum.
     template <typename T, bool kEntropy, bool kTail>
-    __device__ __forceinline__ void add(const uint4 (&v)[kUnroll], float lane_max, float c, const uint32_t (&top_bits)[kUnroll]) {
+    __device__ __forceinline__ void sum(uint4 (&v)[kUnroll], const uint32_t (&top_bits)[kUnroll]) {
         constexpr int N = RowVec<T>::N;
+        const f32x2 c2 = pair(ce, ce), rc2 = pair(-rc, -rc);
+        f32x2 bs = 0ull, bt = 0ull;
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (kEntropy) RowVec<T>::raise(v[u], floor2);
+            f32x2 x[N / 2], vs = 0ull;
+            RowVec<T>::pairs(v[u], x);
+#pragma unroll
+            for (int n = 0; n < N / 2; ++n) {
+                float lo, hi;
+                unpair(fma2(x[n], c2, rc2), lo, hi);
+                if (kEntropy && !RowVec<T>::kFloorsEntries) { lo = fmaxf(lo, kFloorExp); hi = fmaxf(hi, kFloorExp); }
+                const f32x2 e = pair(ex2(lo), ex2(hi));
+                if (kTail) { vs = add2(vs, e); x[n] = e; } else { bs = add2(bs, e); }
+                if (kEntropy) bt = fma2(e, pair(lo, hi), bt);   // (a masked entry: 0 * a finite exponent)
+            }
+            if (kTail) {
+                bs = add2(bs, vs);
+                tail += top_bits[u] == 0u ? sum2(vs) : outside<N>(x, top_bits[u]);
+            }
+        }
+        s += sum2(bs);
+        t += sum2(bt);
+    }
+    // A batch of whatever entries, with the maximum so far kept exactly.
+    template <typename T, bool kEntropy, bool kTail>
+    __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, const uint32_t (&top_bits)[kUnroll]) {
         float wm = lane_max;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) wm = max_nan(wm, __shfl_xor_sync(0xFFFFFFFFu, wm, off));
-        if (wm < m) {
-            float bs = 0.0f, bt = 0.0f;
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                float x[N], vs = 0.0f;
-                RowVec<T>::unpack(v[u], x);
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const float w = exponent<kEntropy>(x[n], c);
-                    const float e = ex2(w);
-                    vs += e;
-                    if (kEntropy) bt = fmaf(e, w, bt);
-                    if (kTail) x[n] = e;
+        if (!(wm < m && ce != 0.0f)) {
+            if (wm == neg_inf()) return;   // nothing but masked entries so far
+            if (!(wm <= m)) {              // a new maximum: the old one becomes an entry like the others
+                const Stats old = *this;
+                set_maximum<T>(wm, c);
+                if (old.ce != 0.0f && ce != 0.0f) {
+                    const float d = fmaxf(old.rc - rc, kFloorExp), f = ex2(d);
+                    const float w = fmaxf(fmaf(old.m, c, -rc), kFloorExp), e = (float)old.cnt * ex2(w);
+                    t = fmaf(f, fmaf(d, s, t), e * w);
+                    s = fmaf(f, s, e);
+                    tail *= f;
+                } else {
+                    s = t = tail = 0.0f;
                 }
-                bs += vs;
-                if (kTail) tail += top_bits[u] == 0u ? vs : outside<N>(x, top_bits[u]);
             }
-            s += bs;
-            t += bt;
-            return;
+            take<T, kTail>(v, top_bits);
+            if (ce == 0.0f) return;
         }
-        if (wm == neg_inf()) return;   // nothing but masked entries so far
-        if (!(wm == m)) {              // a new maximum: the old one becomes an entry like the others
-            const float rc_new = product(wm, c);
-            if (m != neg_inf()) {
-                const float d = fmaxf(rc - rc_new, kFloorExp), f = ex2(d);
-                const float w = fmaxf(fmaf(m, c, -rc_new), kFloorExp), e = (float)cnt * ex2(w);
-                t = fmaf(f, fmaf(d, s, t), e * w);
-                s = fmaf(f, s, e);
-                tail *= f;
-            }
-            m = wm;
-            rc = rc_new;
-            cnt = 0;
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            float x[N], vs = 0.0f;
-            RowVec<T>::unpack(v[u], x);
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const float w = exponent<kEntropy>(x[n], c);
-                const float e = ex2(w);
-                const bool top = x[n] == m;
-                cnt += top ? 1 : 0;
-                vs += top ? 0.0f : e;
-                if (kEntropy) t = top ? t : fmaf(e, w, t);
-                if (kTail) x[n] = e;
-            }
-            s += vs;
-            if (kTail) tail += outside<N>(x, top_bits[u]);
-        }
+        sum<T, kEntropy, kTail>(v, top_bits);
     }
-    template <bool kEntropy> __device__ __forceinline__ float exponent(float x, float c) const {
-        const float w = fmaf(x, c, -rc);
-        return kEntropy ? fmaxf(w, kFloorExp) : w;   // a masked entry: 0 * kFloorExp instead of 0 * inf
-    }
-    template <int N> __device__ __forceinline__ static float outside(const float (&e)[N], uint32_t bits) {
+    template <int N> __device__ __forceinline__ static float outside(const f32x2 (&e)[N / 2], uint32_t bits) {
         float sum = 0.0f;
 #pragma unroll
-        for (int n = 0; n < N; ++n) sum += ((bits >> n) & 1u) ? 0.0f : e[n];
+        for (int n = 0; n < N / 2; ++n) {
+            float lo, hi;
+            unpair(e[n], lo, hi);
+            sum += ((bits >> (2 * n)) & 1u) ? 0.0f : lo;
+            sum += ((bits >> (2 * n + 1)) & 1u) ? 0.0f : hi;
+        }
         return sum;
     }
-    __device__ __forceinline__ void finish(float c) {
-        if (m == neg_inf()) return;
-        const float d = fminf(fmaxf(fmaf(m, c, -rc), -100.0f), 100.0f), f = ex2(-d);   // rounding of rc: tiny, either sign
+    __device__ __forceinline__ void finish() {
+        if (ce == 0.0f) return;
+        const float d = fminf(fmaxf(fmaf(m, ce, -rc), -100.0f), 100.0f), f = ex2(-d);   // rounding of rc: tiny, either sign
         t = f * fmaf(-d, s, t);
         s *= f;
         tail *= f;
@@ -240,7 +380,10 @@ struct RowsShared {
     float w_m[kWarps], w_s[kWarps], w_t[kWarps], w_tail[kWarps];
     int w_cnt[kWarps];
     Merged mine;                 // this CTA's statistics, read by the others of the cluster
+    Merged all;                  // the row's
+    float log_total, inv_total;  // log(1 + rest), 1 / (1 + rest)
     int cand_n;
+    uint32_t threshold;
     unsigned int scan[kWarps];
     // teacher (distill): warps 0..3 hold its entries, one per thread
     int t_id[kRowsMaxTop];
@@ -254,7 +397,7 @@ struct RowsShared {
 // The block's statistics from its warps'; complete in ss.mine after the next barrier.
 __device__ void block_merge(Stats& st, float c, RowsShared& ss) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    st.finish(c);
+    st.finish();
     const float s = warp_sum(st.s), t = warp_sum(st.t), tail = warp_sum(st.tail);
     int cnt = st.cnt;
 #pragma unroll
@@ -286,28 +429,35 @@ __device__ void block_merge(Stats& st, float c, RowsShared& ss) {
     if (lane == 0) ss.mine = r;
 }
 
-// The cluster's statistics from its CTAs' (already published and synchronised).
-__device__ Merged cluster_merge(cg::cluster_group& cluster, RowsShared& ss, int n_cta, float c) {
-    if (n_cta == 1) return ss.mine;
-    float m = neg_inf();
-    int base = 0;
-#pragma unroll 1
-    for (int r = 0; r < n_cta; ++r) {
-        const float pm = cluster.map_shared_rank(&ss.mine, r)->m;
-        if (m == m && !(pm <= m)) { m = pm; base = r; }   // a NaN stays
+// The row's statistics from its CTAs' (published and synchronised), one lane per CTA; warp 0 only.
+__device__ void cluster_merge(cg::cluster_group& cluster, RowsShared& ss, int n_cta, float c) {
+    const int lane = threadIdx.x & 31;
+    Merged a;
+    if (n_cta == 1) {
+        a = ss.mine;
+    } else {
+        Merged part{neg_inf(), 0.0f, 0.0f, 0.0f};
+        if (lane < n_cta) part = *cluster.map_shared_rank(&ss.mine, lane);
+        float m = part.m;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+        const unsigned int holders = __ballot_sync(0xFFFFFFFFu, part.m == m);
+        if (m != neg_inf() && lane != __ffs(holders) - 1) {   // everybody but one holder of the maximum adds all of its entries
+            const float d = fmaxf((part.m - m) * c, kFloorExp), f = ex2(d), all = part.m == neg_inf() ? 0.0f : part.rest + 1.0f;
+            part.rest = f * all;
+            part.t = f * fmaf(d, all, part.t);
+            part.tail *= f;
+        }
+        a.m = m;
+        a.rest = warp_sum(part.rest);
+        a.t = warp_sum(part.t);
+        a.tail = warp_sum(part.tail);
     }
-    Merged a = *cluster.map_shared_rank(&ss.mine, base);
-    if (m != m) return a;
-#pragma unroll 1
-    for (int r = 0; r < n_cta; ++r) {
-        const Merged part = *cluster.map_shared_rank(&ss.mine, r);
-        if (r == base || part.m == neg_inf()) continue;
-        const float d = fmaxf((part.m - m) * c, kFloorExp), f = ex2(d), all = part.rest + 1.0f;
-        a.rest = fmaf(f, all, a.rest);
-        a.t = fmaf(f, fmaf(d, all, part.t), a.t);
-        a.tail = fmaf(f, part.tail, a.tail);
+    if (lane == 0) {
+        ss.all = a;
+        ss.log_total = log1pf(a.rest);
+        ss.inv_total = 1.0f / (1.0f + a.rest);
     }
-    return a;
 }
 
 // ---------------------------------------------------------------------------- the largest entries
@@ -417,12 +567,25 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
     // a thread without an entry has key 0; padding and masked entries have the key of -inf
     const bool any = sh.first + (int)threadIdx.x < sh.last;
     const uint32_t my_key = any ? logit_key(thread_max) : 0u;
-    uint32_t thr = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t c = thr | (1u << bit);
-        const int n = __syncthreads_count(my_key >= c);
-        if (n >= k) { thr = c; if (n <= k + (k >> 1)) break; }
+    uint32_t* keys = reinterpret_cast<uint32_t*>(cand);   // (not yet in use)
+    keys[threadIdx.x] = my_key;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        uint32_t mine[kWarps];
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) mine[i] = keys[32 * i + threadIdx.x];
+        uint32_t t = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t c = t | (1u << bit);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) n += __popc(__ballot_sync(0xFFFFFFFFu, mine[i] >= c));
+            if (n >= k) { t = c; if (n <= k + (k >> 1)) break; }   // any lower bound will do; a close one leaves few candidates
+        }
+        if (threadIdx.x == 0) ss.threshold = t;
     }
+    __syncthreads();
+    const uint32_t thr = ss.threshold;
     int n = collect(sh, my_key, thr, slots, slot_batches, ss, cand);
     if (n > kCandCap) {
         // exact: the k-th largest key of the share.  First guess: the exact k-th largest thread
@@ -469,15 +632,18 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
 struct TeacherEntry { int id; float v, x; bool first; double q; };
 
 // ------------------------------------------------------------------------------------ the kernel
-template <typename T, int kOp>
-__global__ void __launch_bounds__(kThreads)
+// kResident: the row's gradient is wanted and a share fits in shared memory.  All of it is fetched at
+// once by asynchronous copies (each thread waits for its own); one pass over shared memory finds the
+// maximum, one sums, one writes the gradient.  Otherwise batches stream through registers.
+template <typename T, int kOp, bool kResident>
+__global__ void __launch_bounds__(kThreads, kResident ? DM_ROWS_MINR : DM_ROWS_MINB)
 rows_kernel(const RowsParams P) {
     constexpr int N = RowVec<T>::N;
     constexpr bool kEntropy = kOp != OP_DISTILL, kTail = kOp == OP_DISTILL;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowsShared ss;
     uint4* stash = reinterpret_cast<uint4*>(smem);                                      // [stash_vecs], vector first + x
-    uint32_t* bitmap = reinterpret_cast<uint32_t*>(stash + P.stash_vecs);               // distill: teacher tokens of the share
+    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);     // distill: teacher tokens of the share, a byte per vector
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // logprobs: candidates, then the sorted list
     unsigned long long* sorted = cand + kCandCap;
     uint32_t* slots = reinterpret_cast<uint32_t*>(sorted + kRowsMaxTop);                // maxima of the threads' batches
@@ -495,7 +661,23 @@ rows_kernel(const RowsParams P) {
     const int n_vec = (sh.phase + P.V + N - 1) / N, per = (n_vec + n_cta - 1) / n_cta;
     sh.first = min(n_vec, rank * per);
     sh.last = min(n_vec, sh.first + per);
+    sh.whole_lo = sh.phase != 0 ? 1 : 0;
+    sh.whole_hi = (sh.phase + P.V) / N;
     T* grad_row = kOp != OP_LOGPROBS && P.out_grad != nullptr ? static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad : nullptr;
+
+    constexpr int kBatch = kUnroll * kThreads;
+    const int n_share = sh.last - sh.first, n_batches = (n_share + kBatch - 1) / kBatch;
+    if (kResident) {   // on its way before anything else is looked at; the last batch is filled up with masked entries
+        for (int b = 0, at = tid; b < n_batches; ++b) {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u, at += kThreads) {
+                const int j = sh.first + at;
+                if (j < sh.last && sh.whole(j)) copy_async(stash + at, sh.vectors() + j);
+                else stash[at] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
+            }
+            copy_commit();
+        }
+    }
 
     float w = P.inv_temp;   // factor of the gradient
     int tok = -1;
@@ -525,7 +707,7 @@ rows_kernel(const RowsParams P) {
         }
         if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }
         if (use_bits)
-            for (int i = tid; i < (per * N + 31) / 32; i += kThreads) bitmap[i] = 0u;
+            for (int i = tid; i < n_batches * kBatch / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
         if (warp < kRowsMaxTop / 32) {
             float vm = te.id >= 0 ? te.v : neg_inf();
 #pragma unroll
@@ -534,9 +716,10 @@ rows_kernel(const RowsParams P) {
         }
         __syncthreads();
         if (use_bits && te.id >= 0) {
-            const int u = te.id + sh.phase - sh.first * N;     // position within the share
-            if (u >= 0 && u < (sh.last - sh.first) * N) {
-                te.first = ((atomicOr(&bitmap[u >> 5], 1u << (u & 31)) >> (u & 31)) & 1u) == 0u;
+            const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
+            if (at >= 0 && at < sh.last - sh.first) {
+                const uint32_t bit = 1u << (8 * (at & 3) + (te.id + sh.phase) % N);
+                te.first = (atomicOr(reinterpret_cast<uint32_t*>(bitmap) + (at >> 2), bit) & bit) == 0u;
                 if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
             }
         }
@@ -556,45 +739,88 @@ rows_kernel(const RowsParams P) {
 
     // A row whose gradient is zero whatever it holds is not read (unless its loss is wanted).
     const bool need_stats = !(zero_grad && (kOp == OP_GRAD || P.out_loss == nullptr));
-    Merged a{0.0f, 0.0f, 0.0f, 0.0f};
     if (need_stats) {
         Stats st;
         st.init();
+        const bool bucket = kTail && P.tail == DM_TAIL_BUCKET;
         float thread_max = neg_inf();
-        int batch = 0;
-        for (int b0 = sh.first; b0 < sh.last; b0 += kUnroll * kThreads, ++batch) {   // the same for the whole block
-            uint4 v[kUnroll];
-            uint32_t bits[kUnroll];
+        if (kResident) {
+            for (int b = 0; b < n_batches; ++b) {
+                uint4 v[kUnroll];
+                copy_wait(n_batches - 1 - b);
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int j = b0 + u * kThreads + tid;
-                v[u] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
+                for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
+                thread_max = max_nan(thread_max, RowVec<T>::vmax(v));
             }
+            float m = thread_max;
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int at = b0 - sh.first + u * kThreads + tid;
-                if (kOp != OP_LOGPROBS && at < P.stash_vecs) stash[at] = v[u];   // (the stash never exceeds the share)
-                bits[u] = 0u;
-                if (kTail && P.tail == DM_TAIL_BUCKET && at < per) bits[u] = (bitmap[(at * N) >> 5] >> ((at * N) & 31)) & ((1u << N) - 1u);
+            for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+            if (lane == 0) ss.w_m[warp] = m;
+            __syncthreads();
+            m = ss.w_m[0];
+#pragma unroll
+            for (int i = 1; i < kWarps; ++i) m = max_nan(m, ss.w_m[i]);
+            st.set_maximum<T>(m, c);
+            const bool holder = __any_sync(0xFFFFFFFFu, thread_max == m && m != neg_inf());
+            __syncthreads();   // (w_m is written again below)
+            for (int b = 0; b < n_batches && (holder || st.ce != 0.0f); ++b) {
+                uint4 v[kUnroll];
+                uint32_t bits[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    v[u] = stash[b * kBatch + u * kThreads + tid];
+                    bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
+                }
+                if (holder) st.take<T, kTail>(v, bits);
+                if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, bits);
             }
-            const float lane_max = RowVec<T>::vmax(v);
-            if (kOp == OP_LOGPROBS && P.n_top > 0) {
-                const int at = batch / P.slot_batches * kThreads + tid;
-                const uint32_t key = logit_key(lane_max);
-                slots[at] = batch % P.slot_batches == 0 || key > slots[at] ? key : slots[at];
-                thread_max = max_nan(thread_max, lane_max);
+        } else {
+            uint4 next[kUnroll];
+            sh.load_batch(sh.first, next);
+            uint32_t* slot = slots + tid;
+            uint32_t slot_key = 0u;
+            int in_slot = 0;
+            for (int b = 0; b < n_batches; ++b) {   // the same for the whole block; one batch ahead in registers
+                uint4 v[kUnroll];
+                uint32_t bits[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    v[u] = next[u];
+                    bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
+                }
+                sh.load_batch(sh.first + (b + 1) * kBatch, next);
+                const float lane_max = RowVec<T>::vmax(v);
+                if (kOp == OP_LOGPROBS && P.n_top > 0) {
+                    thread_max = max_nan(thread_max, lane_max);
+                    slot_key = max(slot_key, logit_key(lane_max));
+                    if (++in_slot == P.slot_batches || b == n_batches - 1) {
+                        *slot = slot_key;
+                        slot += kThreads;
+                        slot_key = 0u;
+                        in_slot = 0;
+                    }
+                }
+                st.add<T, kEntropy, kTail>(v, lane_max, c, bits);
             }
-            st.add<T, kEntropy, kTail>(v, lane_max, c, bits);
         }
         block_merge(st, c, ss);
         if (kOp == OP_LOGPROBS && P.n_top > 0) top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, cand, sorted);
-        if (n_cta > 1) cluster.sync(); else __syncthreads();
-        a = cluster_merge(cluster, ss, n_cta, c);
+        if (n_cta > 1) cluster.sync();
+        if (warp == 0) {
+            __syncwarp();
+            cluster_merge(cluster, ss, n_cta, c);
+        }
     } else {
-        __syncthreads();
+        if (kResident) copy_wait(0);
+        if (tid == 0) {
+            ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
+            ss.log_total = ss.inv_total = 0.0f;
+        }
     }
+    __syncthreads();
+    const Merged a = ss.all;
     const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
-    const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
+    const float log_total = ss.log_total, inv_total = ss.inv_total;
     const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
 
     if (kOp == OP_LOGPROBS) {
@@ -693,31 +919,47 @@ rows_kernel(const RowsParams P) {
             A = w * fmaf(mass + rest, inv_total, -tail_factor);
         }
         const bool same_phase = (int)((reinterpret_cast<uintptr_t>(grad_row) & 15u) / sizeof(T)) == sh.phase;
-#pragma unroll 4
-        for (int j = sh.first + tid; j < sh.last; j += kThreads) {
-            float x[N];
-            if (none) {
+        const f32x2 m2 = pair(-a.m, -a.m), c2 = pair(c, c), A2 = pair(A, A), B2 = pair(B, B);
+        const auto convert = [&](uint4 v) {
+            f32x2 x[N / 2];
+            RowVec<T>::pairs(v, x);
 #pragma unroll
-                for (int n = 0; n < N; ++n) x[n] = 0.0f;
-            } else {
-                RowVec<T>::unpack(j - sh.first < P.stash_vecs ? stash[j - sh.first] : sh.load(j), x);
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    if (kOp == OP_GRAD) {
-                        const float z = fmaxf((x[n] - a.m) * c, kFloorExp);
-                        x[n] = ex2(z) * fmaf(B, z, A);
-                    } else {
-                        x[n] = ex2((x[n] - a.m) * c) * A;
-                    }
+            for (int n = 0; n < N / 2; ++n) {
+                float lo, hi;
+                unpair(mul2(add2(x[n], m2), c2), lo, hi);
+                if (kOp == OP_GRAD) {
+                    lo = fmaxf(lo, kFloorExp);
+                    hi = fmaxf(hi, kFloorExp);
+                    x[n] = mul2(pair(ex2(lo), ex2(hi)), fma2(B2, pair(lo, hi), A2));
+                } else {
+                    x[n] = mul2(pair(ex2(lo), ex2(hi)), A2);
                 }
             }
-            const int i0 = sh.entry0(j);
-            if (sh.whole(j) && same_phase) {
-                __stcs(reinterpret_cast<uint4*>(grad_row + i0), RowVec<T>::pack(x));
-            } else {
+            return RowVec<T>::pack_pairs(x);
+        };
+        // whole vectors that are in the stash and land on a 16-byte boundary: the bulk of a row
+        int j = sh.first + tid;
+        if (same_phase && !none) {
+            if (j < sh.whole_lo) j += kThreads;
+            const int end = kResident ? min(sh.last, sh.whole_hi) : j;
+            uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase);
+#pragma unroll 4
+            for (; j < end; j += kThreads) __stcs(dst + j, convert(stash[j - sh.first]));
+        }
+        for (int edge = same_phase && !none && sh.first + tid < sh.whole_lo; edge >= 0; --edge) {   // ... and what is left
+            for (int i = edge ? sh.first + tid : j; i < (edge ? sh.whole_lo : sh.last); i += kThreads) {
+                const uint4 v = none ? make_uint4(0u, 0u, 0u, 0u)
+                                     : convert(kResident ? stash[i - sh.first] : sh.load(i));
+                const int i0 = sh.entry0(i);
+                if (sh.whole(i) && same_phase) {
+                    __stcs(reinterpret_cast<uint4*>(grad_row + i0), v);
+                } else {
+                    float x[N];
+                    RowVec<T>::unpack(v, x);
 #pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (i0 + n >= 0 && i0 + n < P.V) RowVec<T>::put(grad_row + i0 + n, x[n]);
+                    for (int n = 0; n < N; ++n)
+                        if (i0 + n >= 0 && i0 + n < P.V) RowVec<T>::put(grad_row + i0 + n, x[n]);
+                }
             }
         }
         __syncthreads();   // the entries that differ are written over by one thread each
@@ -745,9 +987,12 @@ rows_kernel(const RowsParams P) {
     if (n_cta > 1) cluster.sync();   // nobody leaves while another CTA may still read its shared memory
 }
 
+template <typename T, int kOp, bool kResident>
+int launch_kernel(const RowsParams& P, int dev, int cluster, size_t smem, cudaStream_t stream);
+
 template <typename T, int kOp>
 int launch_rows(RowsParams P, cudaStream_t stream) {
-    constexpr int N = RowVec<T>::N;
+    constexpr int N = RowVec<T>::N, kBatch = kUnroll * kThreads;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
@@ -757,27 +1002,29 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
     const bool grad = kOp != OP_LOGPROBS && P.out_grad != nullptr;
     const int n_vec = (P.V + 2 * N - 2) / N;          // at most, whatever the row's alignment
     // CTAs per row: enough of them to fill the GPU where rows are few, not less than one vector per
-    // thread; gradient kernels cut a row until a share fits their part of shared memory.
+    // thread; gradient kernels cut a row until three shares fit an SM's shared memory.
     int cluster = 1;
     while (cluster < kRowsMaxCluster && (long long)P.rows * cluster < 3ll * sms && n_vec > cluster * kThreads) cluster *= 2;
     if (grad)
         while (cluster < kRowsMaxCluster && (n_vec + cluster - 1) / cluster > kStashVecs) cluster *= 2;
-    auto kern = rows_kernel<T, kOp>;
-    size_t smem = 0;
-    for (;; cluster *= 2) {
-        const int per = (n_vec + cluster - 1) / cluster;
-        P.stash_vecs = grad ? (per < kStashVecs ? per : kStashVecs) : 0;
-        smem = (size_t)P.stash_vecs * 16;
-        if (kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad)) smem += ((size_t)per * N + 31) / 32 * 4;
-        if (kOp == OP_LOGPROBS && P.n_top > 0) {
-            const int batches = (per + kUnroll * kThreads - 1) / (kUnroll * kThreads);
-            P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
-            const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
-            smem += (size_t)(kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + (size_t)n_slots * kThreads * sizeof(uint32_t);
-        }
-        if (smem <= kRowsSmemLimit) break;
-        if (cluster >= kRowsMaxCluster) return DM_EUNSUPPORTED;
+    const int per = (n_vec + cluster - 1) / cluster, batches = (per + kBatch - 1) / kBatch;
+    const size_t bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad) ? (size_t)batches * kBatch : 0;
+    const bool resident = grad && (size_t)batches * kBatch * 16 + bits <= kRowsSmemLimit;
+    P.stash_vecs = resident ? batches * kBatch : 0;
+    size_t smem = (size_t)P.stash_vecs * 16 + bits;
+    if (kOp == OP_LOGPROBS && P.n_top > 0) {
+        P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
+        const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
+        smem += (size_t)(kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + (size_t)n_slots * kThreads * sizeof(uint32_t);
     }
+    if (smem > kRowsSmemLimit) return DM_EUNSUPPORTED;
+    if (kOp != OP_LOGPROBS && resident) return launch_kernel<T, kOp, kOp != OP_LOGPROBS>(P, dev, cluster, smem, stream);
+    return launch_kernel<T, kOp, false>(P, dev, cluster, smem, stream);
+}
+
+template <typename T, int kOp, bool kResident>
+int launch_kernel(const RowsParams& P, int dev, int cluster, size_t smem, cudaStream_t stream) {
+    auto kern = rows_kernel<T, kOp, kResident>;
     static std::atomic<unsigned long long> prepared{0};   // devices whose limit has been raised, one bit each
     if (dev >= 64 || !((prepared.load() >> dev) & 1ull)) {
         if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRowsSmemLimit) != cudaSuccess) {
