@@ -31,6 +31,9 @@ namespace dm {
 #ifndef DM_ROWS_MINB
 #define DM_ROWS_MINB 4
 #endif
+#ifndef DM_ROWS_RING
+#define DM_ROWS_RING 2
+#endif
 #ifndef DM_ROWS_MINR
 #define DM_ROWS_MINR 3
 #endif
@@ -42,8 +45,9 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = DM_ROWS_THREADS;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;             // vectors of a batch: 16-byte loads in flight per thread
+constexpr int kRing = DM_ROWS_RING;    // batches in flight where rows stream
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
-constexpr int kMaxSlots = 32;          // maxima a thread keeps of its batches (for finding the top entries again)
+constexpr int kMaxSlots = 16;          // maxima a thread keeps of its batches (for finding the top entries again)
 constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 0 in fp32, and 0 * clamp stays 0
 constexpr int kStashVecs = 4096;       // share of a gradient kernel's CTA up to which a row is cut: 64 KB, three CTAs per SM
 constexpr size_t kRowsSmemLimit = 216 * 1024;
@@ -61,34 +65,13 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
-// Two fp32 values in one 64-bit register pair: sm_100 has packed fp32 arithmetic, two entries per instruction.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pair(float lo, float hi) {
-    f32x2 p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
-    return p;
-}
-__device__ __forceinline__ void unpair(f32x2 p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ float sum2(f32x2 p) {
-    float lo, hi;
-    unpair(p, lo, hi);
-    return lo + hi;
-}
+// Two entries per instruction: sm_100 has packed fp32 arithmetic.
+typedef float2 f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) { return make_float2(lo, hi); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float sum2(f32x2 p) { return p.x + p.y; }
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
 
 // Ordered key of a logit; NaN sorts above everything.  Keys of numbers are never 0.
@@ -109,10 +92,7 @@ template <> struct RowVec<float> {
         x[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
     }
     __device__ static uint4 pack_pairs(const f32x2 (&x)[2]) {
-        uint4 v;
-        asm("mov.b64 {%0, %1}, %2;" : "=r"(v.x), "=r"(v.y) : "l"(x[0]));
-        asm("mov.b64 {%0, %1}, %2;" : "=r"(v.z), "=r"(v.w) : "l"(x[1]));
-        return v;
+        return make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
     }
     static constexpr bool kFloorsEntries = false;   // exponents are clamped one by one
     __device__ static uint32_t floor_word(float) { return 0u; }
@@ -166,9 +146,7 @@ template <> struct RowVec<__nv_bfloat16> {
         uint32_t w[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-            float lo, hi;
-            unpair(x[n], lo, hi);
-            const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+            const __nv_bfloat162 b = __float22bfloat162_rn(x[n]);
             w[n] = *reinterpret_cast<const uint32_t*>(&b);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
@@ -248,17 +226,23 @@ template <typename T> struct Share {
         for (int n = 0; n < N; ++n) x[n] = (i0 + n >= 0 && i0 + n < V) ? RowVec<T>::get(row + i0 + n) : neg_inf();
         return RowVec<T>::pack(x);
     }
-    // one batch: vectors b0 + u * kThreads + thread, masked past the end of the share
-    __device__ __forceinline__ void load_batch(int b0, uint4 (&v)[kUnroll]) const {
+    // Sends one batch (vectors b0 + u * kThreads + thread) on its way to the thread's slots of shared
+    // memory; slots past the end of the share are filled with masked entries.
+    __device__ __forceinline__ void fetch_batch(int b0, uint4* slot) const {
         const int j = b0 + (int)threadIdx.x;
         if (b0 >= whole_lo && b0 + kUnroll * kThreads <= min(last, whole_hi)) {
             const uint4* p = vectors() + j;
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) v[u] = __ldcg(p + u * kThreads);
+            for (int u = 0; u < kUnroll; ++u) copy_async(slot + u * kThreads, p + u * kThreads);
         } else {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) v[u] = j + u * kThreads < last ? load(j + u * kThreads) : RowVec<T>::masked();
+            for (int u = 0; u < kUnroll; ++u) {
+                const int i = j + u * kThreads;
+                if (i < last && whole(i)) copy_async(slot + u * kThreads, vectors() + i);
+                else slot[u * kThreads] = i < last ? load(i) : RowVec<T>::masked();
+            }
         }
+        copy_commit();
     }
 };
 
@@ -299,20 +283,19 @@ struct Stats {
     __device__ __forceinline__ void sum(uint4 (&v)[kUnroll], const uint32_t (&top_bits)[kUnroll]) {
         constexpr int N = RowVec<T>::N;
         const f32x2 c2 = pair(ce, ce), rc2 = pair(-rc, -rc);
-        f32x2 bs = 0ull, bt = 0ull;
+        f32x2 bs = pair(0.0f, 0.0f), bt = bs;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (kEntropy) RowVec<T>::raise(v[u], floor2);
-            f32x2 x[N / 2], vs = 0ull;
+            f32x2 x[N / 2], vs = pair(0.0f, 0.0f);
             RowVec<T>::pairs(v[u], x);
 #pragma unroll
             for (int n = 0; n < N / 2; ++n) {
-                float lo, hi;
-                unpair(fma2(x[n], c2, rc2), lo, hi);
-                if (kEntropy && !RowVec<T>::kFloorsEntries) { lo = fmaxf(lo, kFloorExp); hi = fmaxf(hi, kFloorExp); }
-                const f32x2 e = pair(ex2(lo), ex2(hi));
+                f32x2 w = fma2(x[n], c2, rc2);
+                if (kEntropy && !RowVec<T>::kFloorsEntries) { w.x = fmaxf(w.x, kFloorExp); w.y = fmaxf(w.y, kFloorExp); }
+                const f32x2 e = pair(ex2(w.x), ex2(w.y));
                 if (kTail) { vs = add2(vs, e); x[n] = e; } else { bs = add2(bs, e); }
-                if (kEntropy) bt = fma2(e, pair(lo, hi), bt);   // (a masked entry: 0 * a finite exponent)
+                if (kEntropy) bt = fma2(e, w, bt);   // (a masked entry: 0 * a finite exponent)
             }
             if (kTail) {
                 bs = add2(bs, vs);
@@ -352,10 +335,8 @@ struct Stats {
         float sum = 0.0f;
 #pragma unroll
         for (int n = 0; n < N / 2; ++n) {
-            float lo, hi;
-            unpair(e[n], lo, hi);
-            sum += ((bits >> (2 * n)) & 1u) ? 0.0f : lo;
-            sum += ((bits >> (2 * n + 1)) & 1u) ? 0.0f : hi;
+            sum += ((bits >> (2 * n)) & 1u) ? 0.0f : e[n].x;
+            sum += ((bits >> (2 * n + 1)) & 1u) ? 0.0f : e[n].y;
         }
         return sum;
     }
@@ -640,13 +621,14 @@ __global__ void __launch_bounds__(kThreads, kResident ? DM_ROWS_MINR : DM_ROWS_M
 rows_kernel(const RowsParams P) {
     constexpr int N = RowVec<T>::N;
     constexpr bool kEntropy = kOp != OP_DISTILL, kTail = kOp == OP_DISTILL;
+    constexpr int kBatch = kUnroll * kThreads;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowsShared ss;
     uint4* stash = reinterpret_cast<uint4*>(smem);                                      // [stash_vecs], vector first + x
     unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);     // distill: teacher tokens of the share, a byte per vector
     unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // logprobs: candidates, then the sorted list
     unsigned long long* sorted = cand + kCandCap;
-    uint32_t* slots = reinterpret_cast<uint32_t*>(sorted + kRowsMaxTop);                // maxima of the threads' batches
+    uint32_t* slots = reinterpret_cast<uint32_t*>(stash + kRing * kBatch);              // maxima of the threads' batches (the lists take the ring's place)
     unsigned long long* merged = cand;                                                  // rank 0: every CTA's list (the candidates are done with)
 
     cg::cluster_group cluster = cg::this_cluster();
@@ -665,19 +647,9 @@ rows_kernel(const RowsParams P) {
     sh.whole_hi = (sh.phase + P.V) / N;
     T* grad_row = kOp != OP_LOGPROBS && P.out_grad != nullptr ? static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad : nullptr;
 
-    constexpr int kBatch = kUnroll * kThreads;
     const int n_share = sh.last - sh.first, n_batches = (n_share + kBatch - 1) / kBatch;
-    if (kResident) {   // on its way before anything else is looked at; the last batch is filled up with masked entries
-        for (int b = 0, at = tid; b < n_batches; ++b) {
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u, at += kThreads) {
-                const int j = sh.first + at;
-                if (j < sh.last && sh.whole(j)) copy_async(stash + at, sh.vectors() + j);
-                else stash[at] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
-            }
-            copy_commit();
-        }
-    }
+    // on its way before anything else is looked at: the share, or its first batches
+    for (int b = 0; b < (kResident ? n_batches : kRing); ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
 
     float w = P.inv_temp;   // factor of the gradient
     int tok = -1;
@@ -737,7 +709,7 @@ rows_kernel(const RowsParams P) {
         }
     }
 
-    // A row whose gradient is zero whatever it holds is not read (unless its loss is wanted).
+    // A row whose gradient is zero whatever it holds is not looked at (unless its loss is wanted).
     const bool need_stats = !(zero_grad && (kOp == OP_GRAD || P.out_loss == nullptr));
     if (need_stats) {
         Stats st;
@@ -775,20 +747,21 @@ rows_kernel(const RowsParams P) {
                 if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, bits);
             }
         } else {
-            uint4 next[kUnroll];
-            sh.load_batch(sh.first, next);
             uint32_t* slot = slots + tid;
             uint32_t slot_key = 0u;
             int in_slot = 0;
-            for (int b = 0; b < n_batches; ++b) {   // the same for the whole block; one batch ahead in registers
+            uint4* ring = stash + tid;
+            for (int b = 0; b < n_batches; ++b) {   // the same for the whole block; kRing batches in flight
                 uint4 v[kUnroll];
                 uint32_t bits[kUnroll];
+                copy_wait(kRing - 1);
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) {
-                    v[u] = next[u];
+                    v[u] = ring[u * kThreads];
                     bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
                 }
-                sh.load_batch(sh.first + (b + 1) * kBatch, next);
+                sh.fetch_batch(sh.first + (b + kRing) * kBatch, ring);
+                ring = ring == stash + tid + (kRing - 1) * kBatch ? stash + tid : ring + kBatch;
                 const float lane_max = RowVec<T>::vmax(v);
                 if (kOp == OP_LOGPROBS && P.n_top > 0) {
                     thread_max = max_nan(thread_max, lane_max);
@@ -803,6 +776,7 @@ rows_kernel(const RowsParams P) {
                 st.add<T, kEntropy, kTail>(v, lane_max, c, bits);
             }
         }
+        if (!kResident) copy_wait(0);   // (what is still in flight are empty batches)
         block_merge(st, c, ss);
         if (kOp == OP_LOGPROBS && P.n_top > 0) top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, cand, sorted);
         if (n_cta > 1) cluster.sync();
@@ -811,7 +785,7 @@ rows_kernel(const RowsParams P) {
             cluster_merge(cluster, ss, n_cta, c);
         }
     } else {
-        if (kResident) copy_wait(0);
+        copy_wait(0);
         if (tid == 0) {
             ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
             ss.log_total = ss.inv_total = 0.0f;
@@ -925,14 +899,13 @@ rows_kernel(const RowsParams P) {
             RowVec<T>::pairs(v, x);
 #pragma unroll
             for (int n = 0; n < N / 2; ++n) {
-                float lo, hi;
-                unpair(mul2(add2(x[n], m2), c2), lo, hi);
+                f32x2 z = mul2(add2(x[n], m2), c2);
                 if (kOp == OP_GRAD) {
-                    lo = fmaxf(lo, kFloorExp);
-                    hi = fmaxf(hi, kFloorExp);
-                    x[n] = mul2(pair(ex2(lo), ex2(hi)), fma2(B2, pair(lo, hi), A2));
+                    z.x = fmaxf(z.x, kFloorExp);
+                    z.y = fmaxf(z.y, kFloorExp);
+                    x[n] = mul2(pair(ex2(z.x), ex2(z.y)), fma2(B2, z, A2));
                 } else {
-                    x[n] = mul2(pair(ex2(lo), ex2(hi)), A2);
+                    x[n] = mul2(pair(ex2(z.x), ex2(z.y)), A2);
                 }
             }
             return RowVec<T>::pack_pairs(x);
@@ -1001,21 +974,21 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
     }
     const bool grad = kOp != OP_LOGPROBS && P.out_grad != nullptr;
     const int n_vec = (P.V + 2 * N - 2) / N;          // at most, whatever the row's alignment
-    // CTAs per row: enough of them to fill the GPU where rows are few, not less than one vector per
-    // thread; gradient kernels cut a row until three shares fit an SM's shared memory.
+    // CTAs per row: as many as run at once where rows are few, not less than one vector per thread; gradient kernels cut a row until three shares fit an SM's shared memory.
     int cluster = 1;
-    while (cluster < kRowsMaxCluster && (long long)P.rows * cluster < 3ll * sms && n_vec > cluster * kThreads) cluster *= 2;
+    while (cluster < kRowsMaxCluster && 2ll * P.rows * cluster <= (grad ? 3ll : 4ll) * sms && n_vec > cluster * kThreads) cluster *= 2;
     if (grad)
         while (cluster < kRowsMaxCluster && (n_vec + cluster - 1) / cluster > kStashVecs) cluster *= 2;
     const int per = (n_vec + cluster - 1) / cluster, batches = (per + kBatch - 1) / kBatch;
     const size_t bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad) ? (size_t)batches * kBatch : 0;
     const bool resident = grad && (size_t)batches * kBatch * 16 + bits <= kRowsSmemLimit;
-    P.stash_vecs = resident ? batches * kBatch : 0;
+    P.stash_vecs = (resident ? batches : kRing) * kBatch;
     size_t smem = (size_t)P.stash_vecs * 16 + bits;
     if (kOp == OP_LOGPROBS && P.n_top > 0) {
         P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
         const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
-        smem += (size_t)(kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + (size_t)n_slots * kThreads * sizeof(uint32_t);
+        smem += (size_t)n_slots * kThreads * sizeof(uint32_t);
+        static_assert((kCandCap + kRowsMaxTop) * sizeof(unsigned long long) <= (size_t)kRing * kBatch * 16, "the lists fit the ring");
     }
     if (smem > kRowsSmemLimit) return DM_EUNSUPPORTED;
     if (kOp != OP_LOGPROBS && resident) return launch_kernel<T, kOp, kOp != OP_LOGPROBS>(P, dev, cluster, smem, stream);

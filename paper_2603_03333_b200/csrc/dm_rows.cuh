@@ -15,7 +15,7 @@ struct RowsParams {
     float inv_temp;       // 1 / T
     float c;              // log2(e) / T
     double inv_temp_d;
-    int stash_vecs;       // 16-byte vectors of a CTA's share kept in shared memory (gradient kernels; set by the launch)
+    int stash_vecs;       // 16-byte vectors in shared memory: a CTA's share, or the ring it streams through (set by the launch)
     int slot_batches;     // batches of a thread that share one remembered maximum (set by the launch)
     const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
     // logprobs
