@@ -7,6 +7,7 @@
 
 #include "dm_internal.h"
 #include "dm_rows.cuh"
+#include "dm_score.h"
 
 using namespace dm;
 
@@ -45,8 +46,10 @@ struct dm_ctx {
     float* js_logits = nullptr;              // [js_max_rows][V]
     float* js_ws = nullptr;
     int js_max_rows = 0, js_max_hidden = 0;
-    // dropmatch_score (dm_enable_score): logits of up to score_chunk rows at a time
-    float* score_logits = nullptr;           // [score_chunk][V]
+    // dropmatch_score (dm_enable_score): records, and logits where they are needed, of up to score_chunk
+    // rows at a time; laid out by score_workspace, or logits [score_chunk][V] for the CUDA-core kernel
+    unsigned char* score_ws = nullptr;
+    size_t score_bytes = 0;
     int score_max_rows = 0, score_max_top = 0, score_chunk = 0;
     // optional timing of the head kernel alone (dm_profile_head)
     bool profile = false;
@@ -57,7 +60,6 @@ struct dm_ctx {
 namespace {
 
 constexpr size_t kMaxProfileEvents = 8192;
-constexpr int kScoreChunk = 512;   // rows of dropmatch_score whose logits exist at a time
 
 struct DeviceGuard {
     int prev = -1;
@@ -82,7 +84,8 @@ void free_workspace(dm_ctx* c) {
     cudaFree(c->js_logits); c->js_logits = nullptr;
     cudaFree(c->js_ws); c->js_ws = nullptr;
     c->js_max_rows = c->js_max_hidden = 0;
-    cudaFree(c->score_logits); c->score_logits = nullptr;
+    cudaFree(c->score_ws); c->score_ws = nullptr;
+    c->score_bytes = 0;
     c->score_max_rows = c->score_max_top = c->score_chunk = 0;
     c->ws_bytes = 0;
 }
@@ -703,20 +706,27 @@ int dm_enable_score(dm_ctx* c, int max_rows, int max_top) {
     DeviceGuard g(c->device);
     if (!g.ok) return DM_ECUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
-    if (c->score_logits != nullptr) c->ws_bytes -= (size_t)c->score_chunk * c->head.V * sizeof(float);
-    cudaFree(c->score_logits); c->score_logits = nullptr;
+    c->ws_bytes -= c->score_bytes;
+    cudaFree(c->score_ws); c->score_ws = nullptr;
+    c->score_bytes = 0;
     c->score_max_rows = c->score_max_top = c->score_chunk = 0;
     const int chunk = max_rows < kScoreChunk ? max_rows : kScoreChunk;
-    const size_t n_logits = (size_t)chunk * c->head.V * sizeof(float);
-    if (cudaMalloc(&c->score_logits, n_logits) != cudaSuccess) {
+    // either kernel family may be asked for by a later dm_set_impl: the larger of the two, except that
+    // the CUDA-core kernel's logits are not reserved for a call without alternatives on a tensor-core head
+    size_t bytes = 0;
+    if (c->fused != nullptr) bytes = score_workspace(fused_slices(c->fused), chunk, max_top > 0).bytes;
+    const size_t logits = (size_t)chunk * c->head.V * sizeof(float);
+    if (c->fused == nullptr || c->impl == DM_IMPL_SIMT || (max_top > 0 && bytes < logits)) bytes = bytes > logits ? bytes : logits;
+    if (cudaMalloc(&c->score_ws, bytes) != cudaSuccess) {
         cudaGetLastError();
-        c->score_logits = nullptr;
+        c->score_ws = nullptr;
         return DM_ECUDA;
     }
+    c->score_bytes = bytes;
     c->score_max_rows = max_rows;
     c->score_max_top = max_top;
     c->score_chunk = chunk;
-    c->ws_bytes += n_logits;
+    c->ws_bytes += bytes;
     return DM_OK;
 }
 
@@ -733,7 +743,7 @@ int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows,
     if (c->head.v_offset != 0) return DM_EUNSUPPORTED;
     if (n_rows == 0) return DM_OK;
     if (H == nullptr || (reinterpret_cast<uintptr_t>(H) & 15u) != 0) return DM_EINVAL;
-    if (c->score_logits == nullptr || n_rows > c->score_max_rows || n_top > c->score_max_top) return DM_EWORKSPACE;
+    if (c->score_ws == nullptr || n_rows > c->score_max_rows || n_top > c->score_max_top) return DM_EWORKSPACE;
     DeviceGuard g(c->device);
     if (!g.ok) return DM_ECUDA;
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
@@ -744,23 +754,25 @@ int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows,
     st = pick_impl(c, n_rows, &impl);
     if (st != DM_OK) return st;
     const size_t row_bytes = (size_t)c->head.d * (c->head.dtype == DM_F32 ? 4 : 2);
+    if (impl == DM_IMPL_SIMT && c->score_bytes < (size_t)c->score_chunk * c->head.V * sizeof(float)) return DM_EWORKSPACE;
     for (int r0 = 0; r0 < n_rows; r0 += c->score_chunk) {
         const int rows = n_rows - r0 < c->score_chunk ? n_rows - r0 : c->score_chunk;
         const void* Hc = static_cast<const unsigned char*>(H) + (size_t)r0 * row_bytes;
-        RowMap map{nullptr, 1, rows, 1, 0u, DM_MASK_PER_POSITION};
-        int n_slices = 0, launches = 1;
-        if (impl == DM_IMPL_TCGEN05)
-            st = fused_launch(c->fused, c->head, Hc, rows, rows, map, mk, &n_slices, c->partials, c->score_logits, c->err, s,
-                              &launches, nullptr, nullptr, nullptr, nullptr, nullptr, c->wait_limit, c->pdl);
-        else
-            st = launch_simt(c->head, Hc, rows, map, mk, &n_slices, c->partials, c->score_logits, c->err, s);
-        if (st != DM_OK) return st;
         RowsParams part = rows_from(rp, r0, rows);
-        part.logits = c->score_logits;
-        part.err = c->err;
-        st = launch_rows_logprobs(part, DM_F32, s);
+        if (impl == DM_IMPL_TCGEN05) {
+            st = launch_score(c->fused, c->head, Hc, part, c->score_ws, c->err, c->wait_limit, c->pdl, s);
+        } else {
+            RowMap map{nullptr, 1, rows, 1, 0u, DM_MASK_PER_POSITION};
+            int n_slices = 0;
+            float* logits = reinterpret_cast<float*>(c->score_ws);
+            st = launch_simt(c->head, Hc, rows, map, mk, &n_slices, c->partials, logits, c->err, s);
+            if (st != DM_OK) return st;
+            part.logits = logits;
+            part.err = c->err;
+            st = launch_rows_logprobs(part, DM_F32, s);
+        }
         if (st != DM_OK) return st;
-        launches_total += launches + 1;
+        launches_total += 2;
     }
     c->last_impl = impl;
     c->last_launches = launches_total;

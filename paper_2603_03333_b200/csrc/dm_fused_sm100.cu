@@ -825,14 +825,6 @@ mask_operand_by_position_kernel(const __nv_bfloat16* __restrict__ H, __nv_bfloat
 
 // ------------------------------------------------------------------------------ host side
 
-// How the vocabulary is cut for launches that cover `row_blocks` blocks of 256 paths at once:
-// the SMs are shared out between the row blocks, so a slice is `row_blocks` times longer.
-struct SliceGeometry {
-    CUtensorMap tmap_w;     // box [64 x tile_rows]
-    int n_ctas;             // CTAs per row block = vocabulary slices
-    int tiles_per_cta, tile_rows, slice_rows;
-};
-
 struct FusedState {
     SliceGeometry geo[2];   // [0]: one row block per launch, [1]: two
     // staging buffer for the masked operand of calls with too many rows for the in-kernel
@@ -951,6 +943,19 @@ bool plan_smem(int rows, int tiles_per_cta, SmemPlan* out) {
 }
 
 }  // namespace
+
+const SliceGeometry& fused_slices(const FusedState* fs) { return fs->geo[0]; }
+
+bool tensor_map_bf16(CUtensorMap* map, const void* base, int rows, int d, int box_rows) {
+    static const EncodeTiledFn encode = encode_tiled_fn();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)d * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)kBlockK, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 bool fused_supported(const HeadDesc& head, int rows) {
     return head.dtype == DM_BF16 && head.d >= kBlockK && head.d % kBlockK == 0 && head.V >= 1 && rows >= 1;
