@@ -47,7 +47,8 @@ struct dm_ctx {
     float* js_ws = nullptr;
     int js_max_rows = 0, js_max_hidden = 0;
     // dropmatch_score (dm_enable_score): records, and logits where they are needed, of up to score_chunk
-    // rows at a time; laid out by score_workspace, or logits [score_chunk][V] for the CUDA-core kernel
+    // rows at a time; laid out by the tensor-core kernel, or logits [score_chunk][V] for the CUDA-core one
+    ScoreState* score = nullptr;             // bf16 heads of the tensor-core kernels
     unsigned char* score_ws = nullptr;
     size_t score_bytes = 0;
     int score_max_rows = 0, score_max_top = 0, score_chunk = 0;
@@ -73,6 +74,14 @@ struct DeviceGuard {
     int target = -1;
 };
 
+void free_score(dm_ctx* c) {
+    score_destroy(c->score); c->score = nullptr;
+    cudaFree(c->score_ws); c->score_ws = nullptr;
+    c->ws_bytes -= c->score_bytes;
+    c->score_bytes = 0;
+    c->score_max_rows = c->score_max_top = c->score_chunk = 0;
+}
+
 void free_workspace(dm_ctx* c) {
     cudaFree(c->partials); c->partials = nullptr;
     cudaFree(c->stage_in); c->stage_in = nullptr;
@@ -84,9 +93,7 @@ void free_workspace(dm_ctx* c) {
     cudaFree(c->js_logits); c->js_logits = nullptr;
     cudaFree(c->js_ws); c->js_ws = nullptr;
     c->js_max_rows = c->js_max_hidden = 0;
-    cudaFree(c->score_ws); c->score_ws = nullptr;
-    c->score_bytes = 0;
-    c->score_max_rows = c->score_max_top = c->score_chunk = 0;
+    free_score(c);
     c->ws_bytes = 0;
 }
 
@@ -706,20 +713,21 @@ int dm_enable_score(dm_ctx* c, int max_rows, int max_top) {
     DeviceGuard g(c->device);
     if (!g.ok) return DM_ECUDA;
     if (cudaDeviceSynchronize() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
-    c->ws_bytes -= c->score_bytes;
-    cudaFree(c->score_ws); c->score_ws = nullptr;
-    c->score_bytes = 0;
-    c->score_max_rows = c->score_max_top = c->score_chunk = 0;
+    free_score(c);
     const int chunk = max_rows < kScoreChunk ? max_rows : kScoreChunk;
-    // either kernel family may be asked for by a later dm_set_impl: the larger of the two, except that
-    // the CUDA-core kernel's logits are not reserved for a call without alternatives on a tensor-core head
-    size_t bytes = 0;
-    if (c->fused != nullptr) bytes = score_workspace(fused_slices(c->fused), chunk, max_top > 0).bytes;
+    if (c->fused != nullptr) {
+        const int st = score_create(&c->score, c->head);
+        if (st != DM_OK) return st;
+    }
+    // Either kernel family may be asked for by dm_set_impl: room for the larger of the two, except that
+    // the CUDA-core kernel's logits are not reserved for a tensor-core head without alternatives.
+    size_t bytes = c->score != nullptr ? score_workspace_bytes(c->score, chunk, max_top > 0) : 0;
     const size_t logits = (size_t)chunk * c->head.V * sizeof(float);
-    if (c->fused == nullptr || c->impl == DM_IMPL_SIMT || (max_top > 0 && bytes < logits)) bytes = bytes > logits ? bytes : logits;
+    if (c->score == nullptr || c->impl == DM_IMPL_SIMT || max_top > 0) bytes = bytes > logits ? bytes : logits;
     if (cudaMalloc(&c->score_ws, bytes) != cudaSuccess) {
         cudaGetLastError();
         c->score_ws = nullptr;
+        free_score(c);
         return DM_ECUDA;
     }
     c->score_bytes = bytes;
@@ -760,7 +768,7 @@ int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows,
         const void* Hc = static_cast<const unsigned char*>(H) + (size_t)r0 * row_bytes;
         RowsParams part = rows_from(rp, r0, rows);
         if (impl == DM_IMPL_TCGEN05) {
-            st = launch_score(c->fused, c->head, Hc, part, c->score_ws, c->err, c->wait_limit, c->pdl, s);
+            st = launch_score(c->score, c->head, Hc, part, c->score_ws, c->err, c->wait_limit, c->pdl, s);
         } else {
             RowMap map{nullptr, 1, rows, 1, 0u, DM_MASK_PER_POSITION};
             int n_slices = 0;

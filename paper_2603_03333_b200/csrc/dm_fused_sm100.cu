@@ -825,6 +825,14 @@ mask_operand_by_position_kernel(const __nv_bfloat16* __restrict__ H, __nv_bfloat
 
 // ------------------------------------------------------------------------------ host side
 
+// How the vocabulary is cut for launches that cover `row_blocks` blocks of 256 paths at once:
+// the SMs are shared out between the row blocks, so a slice is `row_blocks` times longer.
+struct SliceGeometry {
+    CUtensorMap tmap_w;     // box [64 x tile_rows]
+    int n_ctas;             // CTAs per row block = vocabulary slices
+    int tiles_per_cta, tile_rows, slice_rows;
+};
+
 struct FusedState {
     SliceGeometry geo[2];   // [0]: one row block per launch, [1]: two
     // staging buffer for the masked operand of calls with too many rows for the in-kernel
@@ -943,8 +951,6 @@ bool plan_smem(int rows, int tiles_per_cta, SmemPlan* out) {
 }
 
 }  // namespace
-
-const SliceGeometry& fused_slices(const FusedState* fs) { return fs->geo[0]; }
 
 bool tensor_map_bf16(CUtensorMap* map, const void* base, int rows, int d, int box_rows) {
     static const EncodeTiledFn encode = encode_tiled_fn();

@@ -74,14 +74,6 @@ size_t finalize_smem_bytes(int T, int K, int N);
 
 // tcgen05 tensor-core kernel (bf16 heads).  FusedState owns the TMA descriptors.
 struct FusedState;
-// How the vocabulary is cut for launches that cover `row_blocks` blocks of 256 paths at once:
-// the SMs are shared out between the row blocks, so a slice is `row_blocks` times longer.
-struct SliceGeometry {
-    CUtensorMap tmap_w;     // box [64 x tile_rows]
-    int n_ctas;             // CTAs per row block = vocabulary slices
-    int tiles_per_cta, tile_rows, slice_rows;
-};
-const SliceGeometry& fused_slices(const FusedState* fs);   // of launches over one row block
 // Tensor map over rows[rows][d] of bf16, boxes of 64 elements x box_rows rows, 128-byte swizzle.
 bool tensor_map_bf16(CUtensorMap* map, const void* base, int rows, int d, int box_rows);
 bool fused_supported(const HeadDesc& head, int rows);

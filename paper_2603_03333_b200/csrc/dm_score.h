@@ -4,14 +4,15 @@
 
 namespace dm {
 
-struct ScoreWorkspace { size_t off_tok, off_max, off_logits, bytes; };
 constexpr int kScoreChunk = 512;   // hidden rows of one launch, and rows whose logits exist at a time
 
-// Layout of the workspace for up to `rows` hidden rows per launch.
-ScoreWorkspace score_workspace(const SliceGeometry& geo, int rows, bool alternatives);
+struct ScoreState;                 // how the vocabulary is cut, and the tensor maps of W
+int score_create(ScoreState** out, const HeadDesc& head);   // bf16 heads of the tensor-core kernels
+void score_destroy(ScoreState* st);
+size_t score_workspace_bytes(const ScoreState* st, int rows, bool alternatives);   // for up to `rows` rows per launch
 
 // rp: rows (at most kScoreChunk), tokens, n_top, temperature and outputs of dropmatch_logprobs.
-int launch_score(const FusedState* fs, const HeadDesc& head, const void* H, const RowsParams& rp, unsigned char* ws, uint32_t* err,
+int launch_score(const ScoreState* st, const HeadDesc& head, const void* H, const RowsParams& rp, unsigned char* ws, uint32_t* err,
                  long long wait_limit, bool allow_pdl, cudaStream_t stream);
 
 }  // namespace dm

@@ -4,22 +4,22 @@
 //
 //   z = l / T;  lse = log sum exp z;  log p(tok) = z[tok] - lse;  entropy = -sum p log p
 //
-// score_head_kernel.  The vocabulary is cut as in the verify kernel (one slice per CTA, equal tiles
-// of at most 128 vocabulary rows, CTA pairs); a W tile is the M operand, the hidden rows are the N
-// operand, up to two blocks of 256 of them against one W tile: W crosses the HBM interface once per
-// 512 hidden rows, and of the bytes a CTA pair loads per step only half (one block) or two thirds
-// (two blocks) are hidden rows.  Hidden rows come straight from the caller's array through a tensor
-// map made for the call; rows past its end load as zeros.  Bounds: W from HBM up to some 200 rows,
-// the tensor pipe above.
+// score_head_kernel.  The hidden rows are the M operand, a tile of up to 256 vocabulary rows is the N
+// operand: accumulator lane = hidden row, column = vocabulary entry, so that an epilogue thread owns a
+// row and runs its softmax statistics in registers, without exchanges between lanes.  (With the
+// operands the other way round, as in the verify kernel, the reductions over lanes took 31 us per tile
+// of 512 rows.)  The vocabulary is cut into one slice per CTA (up to 128 rows: M = 128, N = 256) or per
+// CTA pair (above: cta_group::2, M = 256, each CTA its 128 hidden rows and half of the W tile; above 256
+// two blocks of hidden rows against one W tile, which fill TMEM), W crosses the HBM interface once per
+// 512 hidden rows.  Hidden rows come straight from the caller's array through a tensor map made for the
+// call; rows past its end load as zeros.  Bounds: W from HBM up to some 200 rows, the tensor pipe above.
 //
-// Epilogue.  32 accumulator lanes (vocabulary rows) x 16 columns (hidden rows) at a time: the
-// maximum of the 32, the sum of 2^((l - max) c) over the others (c = log2(e) / T) and the same times
-// the exponent, each column reduced over the lanes by a halving exchange (16 exchanges for 16
-// columns).  A warp merges its tiles into one record (maximum, rest, weighted sum) per column in
-// shared memory; "rest" leaves the largest entry out, so that log(1 + rest) keeps its precision.
-// If alternatives are asked for, the 32 logits and their maximum also go to global memory.
+// Epilogue.  32 columns at a time: their maximum, the sum of 2^((l - max) c) over the others
+// (c = log2(e) / T) and the same times the exponent, merged into the thread's record (maximum, rest,
+// weighted sum).  "rest" leaves the largest entry out, so that log(1 + rest) keeps its precision.  If
+// alternatives are asked for, the 32 logits and their maximum also go to global memory.
 //
-// score_finish_kernel.  One block per hidden row merges the records of all CTAs.  Alternatives: the
+// score_finish_kernel.  One block per hidden row merges the records of all slices.  Alternatives: the
 // k-th largest of the threads' maxima over the maxima of the groups of 32 is a lower bound on the
 // k-th largest logit; only groups that reach it are read (about k of 4000).
 #include <new>
@@ -35,11 +35,12 @@ namespace {
 constexpr int kThreads = 10 * 32;           // warp 0 TMA, warp 1 MMA, warps 2-9 epilogue
 constexpr int kFirstEpiWarp = 2, kEpiWarps = 8;
 constexpr int kBlockK = 64;                 // hidden-size elements per step (128 bytes of bf16)
-constexpr int kTileM = 128;
-constexpr int kWStageBytes = kTileM * kBlockK * 2;
+constexpr int kRowsM = 128;                 // hidden rows of a CTA's operand tile
+constexpr int kHBytes = kRowsM * kBlockK * 2;
 constexpr int kTmemCols = 512;
 constexpr int kMaxSteps = 12;
-constexpr int kMaxBlock = 256;              // hidden rows of one MMA (UMMA N)
+constexpr int kTileN = 256;                 // most vocabulary entries of a tile (UMMA N), accumulator columns of one
+constexpr int kDirectRows = 64;             // up to this many rows logits are stored without turning tiles around
 constexpr int kBarBytes = 512;
 constexpr int kSmemLimit = 227 * 1024;
 constexpr long long kWaitLimitCycles = 2000000000ll;
@@ -49,21 +50,22 @@ constexpr float kLn2 = 0.693147180559945309f;
 
 struct ScoreParams {
     int d, V, rows;
-    int kb_count, tiles_per_cta, tile_rows, slice_rows;
-    int n_pad, n_blk, cols;      // hidden rows of a block (multiple of 32), blocks, accumulator columns of a tile
+    int kb_count;
+    int slice, n_tiles, tile_n, last_n;  // vocabulary entries of a slice, tiles in it, entries of a tile and of the last one (multiples of 16)
+    int n_blk;                   // blocks of 256 hidden rows (pairs only)
     int n_slots, n_steps;        // accumulator slots in TMEM; stages of the ring
-    uint32_t step_bytes, b_bytes;   // bytes of a stage, and of one block's half of the hidden rows
+    uint32_t step_bytes, w_bytes, h_bytes;   // bytes of a stage, of its W part, and that one load of hidden rows brings
     int pdl;
     long long wait_limit;
     float c;                     // log2(e) / T
     const int32_t* tokens;       // [rows] or null
     float* tok_logit;            // [rows]
-    float4* records;             // [4 * CTAs][rows]
+    float4* records;             // [2 * slices][rows]
     float* group_max;            // [rows][groups] or null: no alternatives
     float* logits;               // [rows][groups][32]
-    int n_groups;                // 4 * tiles_per_cta * CTAs
+    int groups_per_tile, groups_per_slice, n_groups;
     uint32_t* err;
-    uint32_t off_rec, off_tok, off_max, off_bar;
+    uint32_t off_out, off_bar;   // alternatives: 4 KB per epilogue warp to turn a tile of logits around in
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -87,56 +89,51 @@ __device__ __forceinline__ Record merge(const Record& a, const Record& b, float 
     return r;
 }
 
-// Reduce 16 columns over 32 lanes in 16 exchanges: each round hands half of the columns to the partner
-// and keeps the other half; lanes 2x and 2x + 1 end up with column x.
-template <typename Op>
-__device__ __forceinline__ float halving16(const float (&x)[16], int lane, Op op) {
-    float a[8], b[4], e[2], y;
-    {
-        const bool up = (lane & 16) != 0;
+// Record of 32 logits of one row (at least one of them a number): relative to their maximum.
+__device__ __forceinline__ Record group_record(const float (&x)[32], float gm, float c) {
+    float2 s = make_float2(0.0f, 0.0f), t = s, ties = s;
+    const float2 m2 = make_float2(-gm, -gm), c2 = make_float2(c, c);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float give = up ? x[j] : x[j + 8], keep = up ? x[j + 8] : x[j];
-            a[j] = op(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 16));
-        }
+    for (int j = 0; j < 32; j += 2) {
+        float2 z = __fmul2_rn(__fadd2_rn(make_float2(x[j], x[j + 1]), m2), c2);
+        z.x = fmaxf(z.x, kFloorExp);      // (-inf past the end of the vocabulary)
+        z.y = fmaxf(z.y, kFloorExp);
+        // an entry equal to the maximum has z = 0 and e = 1 exactly: counted, not summed
+        const float2 top = make_float2(z.x == 0.0f ? -1.0f : 0.0f, z.y == 0.0f ? -1.0f : 0.0f);
+        const float2 e = make_float2(ex2(z.x), ex2(z.y));
+        s = __fadd2_rn(s, __fadd2_rn(e, top));
+        ties = __fadd2_rn(ties, top);
+        t = __ffma2_rn(e, z, t);
     }
-    {
-        const bool up = (lane & 8) != 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float give = up ? a[j] : a[j + 4], keep = up ? a[j + 4] : a[j];
-            b[j] = op(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 8));
-        }
-    }
-    {
-        const bool up = (lane & 4) != 0;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float give = up ? b[j] : b[j + 2], keep = up ? b[j + 2] : b[j];
-            e[j] = op(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 4));
-        }
-    }
-    {
-        const bool up = (lane & 2) != 0;
-        const float give = up ? e[0] : e[1], keep = up ? e[1] : e[0];
-        y = op(keep, __shfl_xor_sync(0xFFFFFFFFu, give, 2));
-    }
-    return op(y, __shfl_xor_sync(0xFFFFFFFFu, y, 1));
+    return Record{gm, (s.x + s.y) - (ties.x + ties.y) - 1.0f, t.x + t.y};
 }
-struct MaxOp { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct SumOp { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 
+// x[i] by five rounds of selection: an array indexed by a register would live in local memory.
+__device__ __forceinline__ float pick32(const float (&x)[32], uint32_t i) {
+    float a[16], b[8], c[4], d[2];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) a[j] = (i & 16u) ? x[j + 16] : x[j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = (i & 8u) ? a[j + 8] : a[j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = (i & 4u) ? b[j + 4] : b[j];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) d[j] = (i & 2u) ? c[j + 2] : c[j];
+    return (i & 1u) ? d[1] : d[0];
+}
+
+// kPair: clusters of two CTAs; the leader (cluster rank 0) issues cta_group::2 MMAs over both CTAs'
+// hidden rows and both halves of the W tile.  Barriers that the issuer waits on live in the leader,
+// those that it signals exist in both CTAs.
+template <bool kPair>
 __global__ void __launch_bounds__(kThreads, 1)
-score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_h,
-                  const ScoreParams P) {
+score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_w_last,
+                  const __grid_constant__ CUtensorMap tmap_h, const ScoreParams P) {
     extern __shared__ unsigned char smem_dyn[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(
         (reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t smem_base = ptx::smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float* s_rec = reinterpret_cast<float*>(smem + P.off_rec);       // [3][4][cols]: maximum, rest, weighted sum
-    int32_t* s_tok = reinterpret_cast<int32_t*>(smem + P.off_tok);   // [cols]
-    float* s_max = reinterpret_cast<float*>(smem + P.off_max);       // [8 warps][16]
     uint64_t* s_bar = reinterpret_cast<uint64_t*>(smem + P.off_bar);
     // barriers: full[n_steps] empty[n_steps] acc_full[n_slots] acc_empty[n_slots] dealloc
     const uint32_t full = smem_base + P.off_bar, empty = full + 8 * P.n_steps;
@@ -146,13 +143,15 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     uint32_t* s_tmem = reinterpret_cast<uint32_t*>(s_bar + n_bars);
     volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
     volatile int* s_never = reinterpret_cast<volatile int*>(s_tmem + 2);
-    const uint32_t rank = ptx::cluster_ctarank();
+    const uint32_t rank = kPair ? ptx::cluster_ctarank() : 0u;
+    constexpr int kCtas = kPair ? 2 : 1;
 
     if (threadIdx.x == 0) {
         ptx::prefetch_tensormap(&tmap_w);
+        ptx::prefetch_tensormap(&tmap_w_last);
         ptx::prefetch_tensormap(&tmap_h);
         for (int s = 0; s < P.n_steps; ++s) { ptx::mbar_init(full + 8 * s, 1); ptx::mbar_init(empty + 8 * s, 1); }
-        for (int s = 0; s < P.n_slots; ++s) { ptx::mbar_init(acc_full + 8 * s, 1); ptx::mbar_init(acc_empty + 8 * s, 2 * kEpiWarps); }
+        for (int s = 0; s < P.n_slots; ++s) { ptx::mbar_init(acc_full + 8 * s, 1); ptx::mbar_init(acc_empty + 8 * s, kCtas * kEpiWarps); }
         ptx::mbar_init(dealloc_bar, 1);
         *s_abort = 0;
         *s_never = 0;
@@ -160,59 +159,71 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         ptx::fence_proxy_async_smem();
     }
     if (warp == kFirstEpiWarp) {
-        ptx::tmem_alloc_pair(ptx::smem_u32(s_tmem), kTmemCols);
-        ptx::tmem_relinquish_pair();
+        if (kPair) { ptx::tmem_alloc_pair(ptx::smem_u32(s_tmem), kTmemCols); ptx::tmem_relinquish_pair(); }
+        else { ptx::tmem_alloc(ptx::smem_u32(s_tmem), kTmemCols); ptx::tmem_relinquish(); }
     }
-    for (int i = threadIdx.x; i < 4 * P.cols; i += kThreads) s_rec[i] = neg_inf();
-    for (int i = threadIdx.x; i < 8 * P.cols; i += kThreads) s_rec[4 * P.cols + i] = 0.0f;
+    if (P.h_bytes < kHBytes) {   // operand rows that no load fills stay zero
+        const int per_stage = (int)(kHBytes - P.h_bytes) / 16;
+        for (int i = threadIdx.x; i < P.n_steps * per_stage; i += kThreads)
+            *reinterpret_cast<uint4*>(smem + (uint32_t)(i / per_stage) * P.step_bytes + P.w_bytes + P.h_bytes + (uint32_t)(i % per_stage) * 16) =
+                make_uint4(0u, 0u, 0u, 0u);
+        ptx::fence_proxy_async_smem();
+    }
     ptx::tc_fence_before();
     __syncthreads();
-    ptx::cluster_sync_all();   // the other CTA's barriers are initialised before anyone signals them
+    if (kPair) ptx::cluster_sync_all();   // the other CTA's barriers are initialised before anyone signals them
     ptx::tc_fence_after();
     const uint32_t tmem_base = *s_tmem;
     if (P.pdl) ptx::griddep_launch_dependents();
 
-    const int slice = (int)blockIdx.x, v_cta0 = slice * P.slice_rows;
-    const int n_tiles = P.tiles_per_cta;   // both CTAs of a pair; rows past the end of W load as zeros and are never taken
-    const uint32_t off_b = kWStageBytes;
+    const int slice = (int)blockIdx.x / kCtas, v_slice = slice * P.slice;
+    const int n_tiles = P.n_tiles;   // entries past the end of W load as zeros and are never taken
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
         if (lane != 0) return;
-        const uint32_t step_tx = 2u * ((uint32_t)P.tile_rows * (kBlockK * 2) + (uint32_t)P.n_blk * P.b_bytes);   // both CTAs
         const uint64_t w_policy = ptx::l2_policy_evict_first();
-        const int b_row0 = (int)rank * (P.n_pad / 2);
         const int total = n_tiles * P.kb_count;
+        const uint32_t h_tx = (uint32_t)(kCtas * P.n_blk) * P.h_bytes;                       // all CTAs of the cluster
+        const uint32_t bar_map = kPair ? ptx::map_to_cta(full, 0) : full;                  // the leader's barriers
+        // cursor over (tile, hidden-size block) of the W loads
+        int x = 0, tile = 0;
+        auto load_w = [&](int stage) {
+            const bool last = tile == n_tiles - 1;
+            const int n = last ? P.last_n : P.tile_n;
+            const CUtensorMap* map = last ? &tmap_w_last : &tmap_w;
+            const int v = v_slice + tile * P.tile_n + (int)rank * (n / 2);
+            const uint32_t dst = smem_base + (uint32_t)stage * P.step_bytes;
+            if (rank == 0) ptx::mbar_arrive_expect_tx(full + 8 * stage, (uint32_t)n * (kBlockK * 2) + h_tx);
+            if (kPair) ptx::tma_load_2d_pair_hint(dst, map, x, v, bar_map + 8 * stage, w_policy);
+            else ptx::tma_load_2d_hint(dst, map, x, v, full + 8 * stage, w_policy);
+            x += kBlockK;
+            if (x == P.d) { x = 0; ++tile; }
+        };
         // W does not depend on the kernel ahead, the hidden rows may: the ring is first filled with W tiles
         const int ahead = P.pdl ? min(P.n_steps, total) : 0;
-        int x = 0, v = v_cta0;
-        for (int n = 0; n < ahead; ++n) {
-            const uint32_t bar = full + 8 * n;
-            if (rank == 0) ptx::mbar_arrive_expect_tx(bar, step_tx);
-            ptx::tma_load_2d_pair_hint(smem_base + (uint32_t)n * P.step_bytes, &tmap_w, x, v, ptx::map_to_cta(bar, 0), w_policy);
-            x += kBlockK;
-            if (x == P.d) { x = 0; v += P.tile_rows; }
-        }
+        for (int n = 0; n < ahead; ++n) load_w(n);
         if (P.pdl) ptx::griddep_wait();
-        x = 0;
-        v = v_cta0;
-        int stage = 0;
-        uint32_t parity = 1, bar = full, bar_e = empty, dst = smem_base;
+        int stage = 0, hx = 0;
+        uint32_t parity = 1;
         for (int n = 0; n < total; ++n) {
             if (n >= ahead) {
-                if (!ptx::mbar_wait<kPollNs>(bar_e, parity, s_abort, P.wait_limit)) {
+                if (!ptx::mbar_wait<kPollNs>(empty + 8 * stage, parity, s_abort, P.wait_limit)) {
                     atomicCAS(P.err, 0u, (uint32_t)ERR_WAIT_EMPTY);
                     return;
                 }
-                if (rank == 0) ptx::mbar_arrive_expect_tx(bar, step_tx);
-                ptx::tma_load_2d_pair_hint(dst, &tmap_w, x, v, ptx::map_to_cta(bar, 0), w_policy);
+                load_w(stage);
             }
-            for (int b = 0; b < P.n_blk; ++b)
-                ptx::tma_load_2d_pair(dst + off_b + (uint32_t)b * P.b_bytes, &tmap_h, x, b * P.n_pad + b_row0, ptx::map_to_cta(bar, 0));
-            x += kBlockK;
-            if (x == P.d) { x = 0; v += P.tile_rows; }
-            bar += 8; bar_e += 8; dst += P.step_bytes;
-            if (++stage == P.n_steps) { stage = 0; parity ^= 1; bar = full; bar_e = empty; dst = smem_base; }
+            const uint32_t dst = smem_base + (uint32_t)stage * P.step_bytes + P.w_bytes;
+            if (kPair) {
+                for (int b = 0; b < P.n_blk; ++b)
+                    ptx::tma_load_2d_pair(dst + (uint32_t)b * kHBytes, &tmap_h, hx, (2 * b + (int)rank) * kRowsM, bar_map + 8 * stage);
+            } else {
+                ptx::tma_load_2d(dst, &tmap_h, hx, 0, full + 8 * stage);
+            }
+            hx += kBlockK;
+            if (hx == P.d) hx = 0;
+            if (++stage == P.n_steps) { stage = 0; parity ^= 1; }
         }
         return;
     }
@@ -220,20 +231,20 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         // ------------------------------------------------------------------ MMA issuer
         // (the whole warp stays converged; one elected lane issues: see the verify kernel)
         if (rank != 0) return;
-        const uint32_t idesc = ptx::idesc_bf16_f32(2 * kTileM, P.n_pad);
-        const uint64_t a_desc0 = ptx::smem_desc_sw128(smem_base), b_desc0 = ptx::smem_desc_sw128(smem_base + off_b);
-        const uint32_t step_units = P.step_bytes >> 4, b_units = P.b_bytes >> 4;
+        const uint64_t w_desc0 = ptx::smem_desc_sw128(smem_base), h_desc0 = ptx::smem_desc_sw128(smem_base + P.w_bytes);
+        const uint32_t step_units = P.step_bytes >> 4;
         int stage = 0, slot = 0;
         uint32_t parity = 0, slot_parity = 1;
-        uint64_t a_desc = a_desc0, b_desc = b_desc0;
+        uint64_t w_desc = w_desc0, h_desc = h_desc0;
         uint32_t bar_f = full, bar_e = empty;
         for (int tile = 0; tile < n_tiles; ++tile) {
+            const uint32_t idesc = ptx::idesc_bf16_f32(kCtas * kRowsM, tile == n_tiles - 1 ? P.last_n : P.tile_n);
             if (!ptx::mbar_wait_converged<kPollNs, true>(acc_empty + 8 * slot, slot_parity, s_abort, P.wait_limit)) {
                 if (lane == 0) atomicCAS(P.err, 0u, (uint32_t)ERR_WAIT_ACC_EMPTY);
                 return;
             }
             ptx::tc_fence_after();
-            const uint32_t d_tmem = tmem_base + (uint32_t)(slot * P.cols);
+            const uint32_t d_tmem = tmem_base + (uint32_t)(slot * P.n_blk * kTileN);
             for (int kb = 0; kb < P.kb_count; ++kb) {
                 if (!ptx::mbar_wait_converged<kPollNs, true>(bar_f, parity, s_abort, P.wait_limit)) {
                     if (lane == 0) atomicCAS(P.err, 0u, (uint32_t)ERR_WAIT_FULL);
@@ -242,18 +253,19 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 ptx::tc_fence_after();
                 if (ptx::elect_one()) {
                     for (int b = 0; b < P.n_blk; ++b) {
+                        const uint64_t a_desc = h_desc + (uint32_t)b * (kHBytes >> 4);
 #pragma unroll
-                        for (int k = 0; k < kBlockK / 16; ++k)
-                            ptx::mma_f16_pair(d_tmem + (uint32_t)(b * P.n_pad), a_desc + 2 * k, b_desc + (uint32_t)b * b_units + 2 * k, idesc,
-                                              (kb | k) != 0);
+                        for (int k = 0; k < kBlockK / 16; ++k)   // 16 elements = 32 bytes = 2 descriptor units
+                            if (kPair) ptx::mma_f16_pair(d_tmem + (uint32_t)(b * kTileN), a_desc + 2 * k, w_desc + 2 * k, idesc, (kb | k) != 0);
+                            else ptx::mma_f16(d_tmem, a_desc + 2 * k, w_desc + 2 * k, idesc, (kb | k) != 0);
                     }
-                    ptx::mma_commit_pair(bar_e, 3);
+                    if (kPair) ptx::mma_commit_pair(bar_e, 3); else ptx::mma_commit(bar_e);
                 }
                 __syncwarp();
-                bar_f += 8; bar_e += 8; a_desc += step_units; b_desc += step_units;
-                if (++stage == P.n_steps) { stage = 0; parity ^= 1; bar_f = full; bar_e = empty; a_desc = a_desc0; b_desc = b_desc0; }
+                bar_f += 8; bar_e += 8; w_desc += step_units; h_desc += step_units;
+                if (++stage == P.n_steps) { stage = 0; parity ^= 1; bar_f = full; bar_e = empty; w_desc = w_desc0; h_desc = h_desc0; }
             }
-            if (ptx::elect_one()) ptx::mma_commit_pair(acc_full + 8 * slot, 3);
+            if (ptx::elect_one()) { if (kPair) ptx::mma_commit_pair(acc_full + 8 * slot, 3); else ptx::mma_commit(acc_full + 8 * slot); }
             __syncwarp();
             if (++slot == P.n_slots) { slot = 0; slot_parity ^= 1; }
         }
@@ -262,117 +274,112 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 
     // ---------------------------------------------------------------------- epilogue
     if (P.pdl) ptx::griddep_wait();       // tokens may be the kernel ahead's; global writes only after it
-    for (int i = threadIdx.x - kFirstEpiWarp * 32; i < P.cols; i += kEpiWarps * 32) {
-        const int row = i;                // columns are hidden rows: block 0, then block 1
-        s_tok[i] = P.tokens != nullptr && row < P.rows ? P.tokens[row] : -1;
+    const int quarter = warp & 3, set = (warp - kFirstEpiWarp) >> 2;   // TMEM lanes 32 * quarter ..; a set takes every other group of 32 columns
+    const int v_end = min(P.V, v_slice + P.slice);
+    float4* turn = reinterpret_cast<float4*>(smem + P.off_out) + (warp - kFirstEpiWarp) * 256;
+    Record rec[2];
+    int row[2], tok[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        row[b] = (2 * b + (int)rank) * kRowsM + quarter * 32 + lane;
+        rec[b] = Record{neg_inf(), 0.0f, 0.0f};
+        tok[b] = P.tokens != nullptr && b < P.n_blk && row[b] < P.rows ? P.tokens[row[b]] : -1;
     }
-    ptx::bar_sync(2, kEpiWarps * 32);
-    const int quarter = warp & 3, set = (warp - kFirstEpiWarp) >> 2;   // TMEM lanes 32 * quarter ..; columns are shared by two sets
-    const int m_lane = quarter * 32 + lane;
-    float* my_max = s_max + (warp - kFirstEpiWarp) * 16;
-    const int n_cols = min(P.cols, (P.rows + 15) & ~15);
-    bool alive = true;
     int slot = 0;
     uint32_t parity = 0;
     for (int tile = 0; tile < n_tiles; ++tile) {
         if (!ptx::mbar_wait_warp<kIdlePollNs>(acc_full + 8 * slot, parity, s_abort, P.wait_limit)) {
             atomicCAS(P.err, 0u, (uint32_t)ERR_WAIT_ACC_FULL);
-            alive = false;
             break;
         }
         ptx::tc_fence_after();
-        const int v = v_cta0 + tile * P.tile_rows + m_lane;
-        const bool valid = m_lane < P.tile_rows && v < P.V;
-        const int group = (slice * n_tiles + tile) * 4 + quarter;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (b >= P.n_blk || row[b] - lane >= P.rows) continue;     // (the same for the whole warp)
+            const int n_here = min(tile == n_tiles - 1 ? P.last_n : P.tile_n, v_end - (v_slice + tile * P.tile_n));
 #pragma unroll 1
-        for (int n0 = 16 * set; n0 < n_cols; n0 += 32) {
-            uint32_t acc[16];
-            ptx::tmem_ld16(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(slot * P.cols + n0), acc);
-            ptx::tmem_ld_wait();
-            float x[16], y[16];
+            for (int n0 = 32 * set; n0 < n_here; n0 += 64) {
+                uint32_t acc[32];
+                ptx::tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((slot * P.n_blk + b) * kTileN + n0), acc);
+                ptx::tmem_ld_wait();
+                const int v0 = v_slice + tile * P.tile_n + n0;
+                float x[32];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[j] = valid ? __uint_as_float(acc[j]) : neg_inf();
-            if (P.tokens != nullptr && valid) {
-                const int4* tk = reinterpret_cast<const int4*>(s_tok + n0);
+                for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(acc[j]);
+                if (n_here - n0 < 32) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int4 t4 = tk[j];
-                    if (t4.x == v) P.tok_logit[n0 + 4 * j] = x[4 * j];
-                    if (t4.y == v) P.tok_logit[n0 + 4 * j + 1] = x[4 * j + 1];
-                    if (t4.z == v) P.tok_logit[n0 + 4 * j + 2] = x[4 * j + 2];
-                    if (t4.w == v) P.tok_logit[n0 + 4 * j + 3] = x[4 * j + 3];
+                    for (int j = 0; j < 32; ++j) x[j] = n0 + j < n_here ? x[j] : neg_inf();
                 }
-            }
-            if (P.group_max != nullptr) {
-                float* out = P.logits + ((size_t)n0 * P.n_groups + group) * 32 + lane;
+                float gm = x[0];
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (n0 + j < P.rows) out[(size_t)j * P.n_groups * 32] = x[j];
-            }
-            const float gm = halving16(x, lane, MaxOp());    // lanes 2x, 2x+1: column x of the chunk
-            if ((lane & 1) == 0) my_max[lane >> 1] = gm;
-            __syncwarp();
-            float mx[16];
+                for (int j = 1; j < 32; ++j) gm = fmaxf(gm, x[j]);
+                if ((unsigned)(tok[b] - v0) < (unsigned)min(32, n_here - n0)) {   // (the rest is the next tile's)
+                    P.tok_logit[row[b]] = pick32(x, (uint32_t)(tok[b] - v0));
+                }
+                if (P.group_max != nullptr) {
+                    const size_t g = (size_t)slice * P.groups_per_slice + tile * P.groups_per_tile + (n0 >> 5);
+                    if (row[b] < P.rows) P.group_max[(size_t)row[b] * P.n_groups + g] = gm;
+                    if (P.off_out == P.off_bar) {
+                        // few rows: each thread stores its own line, and the ring has a stage more (1 to 61 rows on
+                        // the Llama-3-8B head: 161-172 us against 167-178 us)
+                        if (row[b] < P.rows) {
+                            float4* out = reinterpret_cast<float4*>(P.logits + ((size_t)row[b] * P.n_groups + g) * 32);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float4 m4 = reinterpret_cast<const float4*>(my_max)[j];
-                mx[4 * j] = m4.x; mx[4 * j + 1] = m4.y; mx[4 * j + 2] = m4.z; mx[4 * j + 3] = m4.w;
-            }
-            __syncwarp();
+                            for (int j = 0; j < 8; ++j) out[j] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                        }
+                    } else {
+                        // the warp's 32 x 32 logits go through shared memory (16-byte chunks at c ^ (row mod 8)) so that
+                        // a store covers four whole lines instead of a piece of 32 (509 rows: 432 against 775 us)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                // the first lane that holds the maximum is left out, further ones count as 1
-                const float z = fmaxf((x[j] - mx[j]) * P.c, kFloorExp);
-                const bool is_max = x[j] == mx[j];
-                const unsigned int holders = __ballot_sync(0xFFFFFFFFu, is_max);
-                const bool first = is_max && (holders & ((1u << lane) - 1u)) == 0u;
-                x[j] = first || !valid ? 0.0f : ex2(z);
-                y[j] = x[j] * (is_max ? 0.0f : z);
-            }
-            const float rest = halving16(x, lane, SumOp()), t = halving16(y, lane, SumOp());
-            if ((lane & 1) == 0) {
-                const int col = n0 + (lane >> 1), at = quarter * P.cols + col, plane = 4 * P.cols;
-                const Record old{s_rec[at], s_rec[plane + at], s_rec[2 * plane + at]};
-                const Record now = merge(old, Record{gm, rest, t}, P.c);
-                s_rec[at] = now.m; s_rec[plane + at] = now.rest; s_rec[2 * plane + at] = now.t;
-                if (P.group_max != nullptr && col < P.rows) P.group_max[(size_t)col * P.n_groups + group] = gm;
+                        for (int j = 0; j < 8; ++j)
+                            turn[lane * 8 + (j ^ (lane & 7))] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int r = 4 * i + (lane >> 3), q = row[b] - lane + r;
+                            if (q < P.rows)
+                                reinterpret_cast<float4*>(P.logits + ((size_t)q * P.n_groups + g) * 32)[lane & 7] = turn[r * 8 + ((lane & 7) ^ (r & 7))];
+                        }
+                        __syncwarp();
+                    }
+                }
+                rec[b] = merge(rec[b], group_record(x, gm, P.c), P.c);
+                __syncwarp();
             }
         }
         ptx::tc_fence_before();
         __syncwarp();
         if (lane == 0) {   // the issuer's barrier is the leader's
-            if (rank != 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(acc_empty + 8 * slot, 0));
+            if (kPair && rank != 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(acc_empty + 8 * slot, 0));
             else ptx::mbar_arrive(acc_empty + 8 * slot);
         }
         if (++slot == P.n_slots) { slot = 0; parity ^= 1; }
     }
-    if (alive) {
-        __syncwarp();
-        for (int n0 = 16 * set; n0 < n_cols; n0 += 32) {   // the records this warp has built
-            const int col = n0 + lane;
-            if (lane < 16 && col < P.rows) {
-                const int at = quarter * P.cols + col, plane = 4 * P.cols;
-                P.records[(size_t)(slice * 4 + quarter) * P.rows + col] = make_float4(s_rec[at], s_rec[plane + at], s_rec[2 * plane + at], 0.0f);
-            }
-        }
-    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+        if (b < P.n_blk && row[b] < P.rows)
+            P.records[(size_t)(slice * 2 + set) * P.rows + row[b]] = make_float4(rec[b].m, rec[b].rest, rec[b].t, 0.0f);
     // -------------------------------------------------------------------------- teardown
-    // (as in the verify kernel: after an abandoned wait the other CTA of the pair is told, and copies and
+    // (as in the verify kernel: after an abandoned wait the other CTA of a pair is told, and copies and
     // MMAs that may still be in flight are given time to finish)
     ptx::tc_fence_before();
     ptx::bar_sync(2, kEpiWarps * 32);
     if (*s_abort) {
-        if (threadIdx.x == kFirstEpiWarp * 32)
+        if (kPair && threadIdx.x == kFirstEpiWarp * 32)
             ptx::st_cluster_u32(ptx::map_to_cta(ptx::smem_u32(const_cast<int*>(s_abort)), rank ^ 1u), 1u);
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
     }
     ptx::bar_sync(2, kEpiWarps * 32);
     if (warp == kFirstEpiWarp) {
         ptx::tc_fence_after();
-        // neither CTA may free TMEM, or leave, while the other still reads accumulators or sends signals here
-        if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(dealloc_bar, rank ^ 1u));
-        ptx::mbar_wait_warp<kPollNs>(dealloc_bar, 0, s_never, 2 * max(P.wait_limit, kWaitLimitCycles));
-        ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+        if (kPair) {
+            // neither CTA may free TMEM, or leave, while the other still reads accumulators or sends signals here
+            if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(dealloc_bar, rank ^ 1u));
+            ptx::mbar_wait_warp<kPollNs>(dealloc_bar, 0, s_never, 2 * max(P.wait_limit, kWaitLimitCycles));
+            ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+        } else {
+            ptx::tmem_dealloc(tmem_base, kTmemCols);
+        }
     }
 }
 
@@ -380,9 +387,11 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 
 constexpr int kFinThreads = 256, kFinWarps = kFinThreads / 32;
 constexpr int kFinList = 1024;
+constexpr int kFinOwn = 20;     // maxima of groups a thread keeps in registers (more are read twice)
 
 struct FinishParams {
-    int rows, V, n_records, n_groups, tiles_per_cta, tile_rows, slice_rows;
+    int rows, V, n_records, groups_per_tile, n_tiles, slice, tile_n;
+    int n_groups, n_written;   // groups per row (stride), and how many of them lie within the vocabulary (the first ones)
     float c, inv_temp;
     const float4* records;
     const float *tok_logit, *group_max, *logits;
@@ -394,15 +403,15 @@ struct FinishParams {
 };
 
 __device__ __forceinline__ int group_first(const FinishParams& P, int group) {
-    const int quarter = group & 3, tile = (group >> 2) % P.tiles_per_cta, slice = (group >> 2) / P.tiles_per_cta;
-    return slice * P.slice_rows + tile * P.tile_rows + quarter * 32;
+    const int tile = group / P.groups_per_tile, slice = tile / P.n_tiles;
+    return slice * P.slice + (tile - slice * P.n_tiles) * P.tile_n + (group - tile * P.groups_per_tile) * 32;
 }
 
 __global__ void __launch_bounds__(kFinThreads)
 score_finish_kernel(const FinishParams P) {
     __shared__ Record s_part[kFinWarps];
     __shared__ Record s_all;
-    __shared__ uint32_t s_key[kFinThreads];
+    __shared__ __align__(16) uint32_t s_key[kFinThreads];
     __shared__ uint32_t s_thr;
     __shared__ int s_n, s_groups;
     __shared__ unsigned long long s_list[kFinList];
@@ -416,11 +425,16 @@ score_finish_kernel(const FinishParams P) {
 
     // the maxima of the groups and the records are fetched side by side
     const float* gm = P.group_max != nullptr ? P.group_max + (size_t)row * P.n_groups : nullptr;
+    float own[kFinOwn];
     float thread_max = neg_inf();
     if (P.n_top > 0) {
-#pragma unroll 8
-        for (int g = tid; g < P.n_groups; g += kFinThreads) thread_max = fmaxf(thread_max, gm[g]);
-        s_key[tid] = tid < P.n_groups ? float_key(thread_max) : 0u;
+#pragma unroll
+        for (int i = 0; i < kFinOwn; ++i) own[i] = i * kFinThreads + tid < P.n_written ? gm[i * kFinThreads + tid] : neg_inf();
+#pragma unroll
+        for (int i = 0; i < kFinOwn; ++i) thread_max = fmaxf(thread_max, own[i]);
+#pragma unroll 4
+        for (int g = kFinOwn * kFinThreads + tid; g < P.n_written; g += kFinThreads) thread_max = fmaxf(thread_max, gm[g]);
+        s_key[tid] = tid < P.n_written ? float_key(thread_max) : 0u;
     }
     Record r{neg_inf(), 0.0f, 0.0f};
     for (int i = tid; i < P.n_records; i += kFinThreads) {
@@ -434,7 +448,7 @@ score_finish_kernel(const FinishParams P) {
         r = (lane & off) == 0 ? merge(r, o, P.c) : merge(o, r, P.c);   // the same order on both sides
     }
     if (lane == 0) s_part[warp] = r;
-    if (tid == 0) { s_n = 0; s_groups = 0; }
+    if (tid == 0) { s_n = 0; s_groups = 0; s_thr = 0u; }
     __syncthreads();
     if (warp == 0) {
         Record a = s_part[0];
@@ -451,30 +465,31 @@ score_finish_kernel(const FinishParams P) {
     }
     if (P.n_top == 0) return;
     const int k = P.n_top;
-    if (warp == 1) {   // a key that k threads' maxima reach (0 if there are fewer than k groups)
-        uint32_t key[kFinWarps];
-#pragma unroll
-        for (int i = 0; i < kFinWarps; ++i) key[i] = s_key[32 * i + lane];
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t c = t | (1u << bit);
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kFinWarps; ++i) n += __popc(__ballot_sync(0xFFFFFFFFu, key[i] >= c));
-            if (n >= k) { t = c; if (n <= k + (k >> 1)) break; }
+    {   // the k-th largest of the threads' maxima (0 if fewer threads have one)
+        const uint32_t mine = s_key[tid];
+        int reach = 0;
+#pragma unroll 8
+        for (int i = 0; i < kFinThreads / 4; ++i) {
+            const uint4 o = reinterpret_cast<const uint4*>(s_key)[i];
+            reach += (o.x >= mine) + (o.y >= mine) + (o.z >= mine) + (o.w >= mine);
         }
-        if (lane == 0) s_thr = t;
+        if (reach >= k && mine != 0u) atomicMax(&s_thr, mine);
     }
     __syncthreads();
     const uint32_t thr = s_thr;
     const Record a = s_all;
     // groups that reach the key, then their entries, a warp per group
-    if (float_key(thread_max) >= thr)
-        for (int g = tid; g < P.n_groups; g += kFinThreads)
-            if (float_key(gm[g]) >= thr) {
-                const int at = atomicAdd(&s_groups, 1);
-                if (at < kFinList) s_group[at] = g;
-            }
+    if (float_key(thread_max) >= thr) {
+        const auto take = [&](int g) {
+            const int at = atomicAdd(&s_groups, 1);
+            if (at < kFinList) s_group[at] = g;
+        };
+#pragma unroll
+        for (int i = 0; i < kFinOwn; ++i)
+            if (i * kFinThreads + tid < P.n_written && float_key(own[i]) >= thr) take(i * kFinThreads + tid);
+        for (int g = kFinOwn * kFinThreads + tid; g < P.n_written; g += kFinThreads)
+            if (float_key(gm[g]) >= thr) take(g);
+    }
     __syncthreads();
     const float* logits = P.logits + (size_t)row * P.n_groups * 32 + lane;
     const int n_near = min(s_groups, kFinList);
@@ -498,7 +513,7 @@ score_finish_kernel(const FinishParams P) {
             __syncthreads();
             if (tid == 0) s_n = 0;
             __syncthreads();
-            for (int g = warp; g < P.n_groups; g += kFinWarps) {
+            for (int g = warp; g < P.n_written; g += kFinWarps) {
                 if (float_key(gm[g]) < (uint32_t)(c >> 32)) continue;
                 const float x = logits[(size_t)g * 32];
                 const unsigned long long word = pack_best(float_key(x), (uint32_t)(group_first(P, g) + lane));
@@ -531,56 +546,107 @@ score_finish_kernel(const FinishParams P) {
     }
 }
 
-bool plan(int rows, ScoreParams* P) {
-    const int half = rows > kMaxBlock ? 2 : 1;
-    P->n_blk = half;
-    P->n_pad = ((rows + half - 1) / half + 31) & ~31;
-    if (P->n_pad < 64) P->n_pad = 64;   // narrower pair MMAs are no faster
-    P->cols = P->n_blk * P->n_pad;
-    P->n_slots = kTmemCols / P->cols;
-    if (P->n_slots > 4) P->n_slots = 4;
-    P->b_bytes = (uint32_t)(P->n_pad / 2) * (kBlockK * 2);
-    P->step_bytes = kWStageBytes + (uint32_t)P->n_blk * P->b_bytes;
-    const uint32_t fixed = 12u * P->cols * 4u + 4u * P->cols + kEpiWarps * 16u * 4u + kBarBytes;
-    P->n_steps = (int)((kSmemLimit - 1024 - fixed) / P->step_bytes);
-    if (P->n_steps > kMaxSteps) P->n_steps = kMaxSteps;
-    P->off_rec = (uint32_t)P->n_steps * P->step_bytes;
-    P->off_tok = P->off_rec + 12u * P->cols * 4u;
-    P->off_max = P->off_tok + 4u * P->cols;
-    P->off_bar = P->off_max + kEpiWarps * 16u * 4u;
-    return P->n_steps >= 2 && P->n_slots >= 1;
-}
-
 }  // namespace
 
-int score_groups(const SliceGeometry& geo) { return 4 * geo.tiles_per_cta * ((geo.n_ctas + 1) & ~1); }
+// How the vocabulary is cut: [0] a slice per CTA, [1] a slice per CTA pair.
+struct ScoreState {
+    struct Cut {
+        CUtensorMap w, w_last;      // boxes of a full and of a slice's last tile (a CTA's part of it)
+        int slice, n_tiles, tile_n, last_n, n_slices, groups_per_tile;
+        int groups_per_slice() const { return n_tiles * groups_per_tile; }
+    } cut[2];
+};
 
-ScoreWorkspace score_workspace(const SliceGeometry& geo, int rows, bool alternatives) {
-    // records | token logits | maxima of groups | logits, each 256-byte aligned
+int score_create(ScoreState** out, const HeadDesc& head) {
+    *out = nullptr;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 2) {
+        cudaGetLastError();
+        return DM_ECUDA;
+    }
+    ScoreState* st = new (std::nothrow) ScoreState();
+    if (st == nullptr) return DM_ECUDA;
+    for (int p = 0; p < 2; ++p) {
+        ScoreState::Cut& cut = st->cut[p];
+        const int units = p ? sms / 2 : sms;
+        cut.slice = ((head.V + units - 1) / units + 15) & ~15;      // UMMA N is a multiple of 16
+        cut.n_tiles = (cut.slice + kTileN - 1) / kTileN;
+        cut.tile_n = ((cut.slice + cut.n_tiles - 1) / cut.n_tiles + 15) & ~15;   // (a short last tile would leave the ring idle)
+        cut.n_tiles = (cut.slice + cut.tile_n - 1) / cut.tile_n;
+        cut.last_n = cut.slice - (cut.n_tiles - 1) * cut.tile_n;
+        cut.n_slices = (head.V + cut.slice - 1) / cut.slice;
+        cut.groups_per_tile = (cut.tile_n + 31) / 32;
+        if (!tensor_map_bf16(&cut.w, head.W, head.V, head.d, cut.tile_n >> p) ||
+            !tensor_map_bf16(&cut.w_last, head.W, head.V, head.d, cut.last_n >> p)) {
+            delete st;
+            return DM_ECUDA;
+        }
+    }
+    if (cudaFuncSetAttribute(score_head_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess ||
+        cudaFuncSetAttribute(score_head_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) {
+        cudaGetLastError();
+        delete st;
+        return DM_ECUDA;
+    }
+    *out = st;
+    return DM_OK;
+}
+
+void score_destroy(ScoreState* st) { delete st; }
+
+namespace {
+
+struct Workspace { size_t off_tok, off_max, off_logits, bytes; };
+
+// records | token logits | maxima of groups | logits, each 256-byte aligned
+Workspace workspace(const ScoreState::Cut& cut, int rows, bool alternatives) {
     const auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
-    const size_t groups = (size_t)score_groups(geo), records = 4 * (size_t)((geo.n_ctas + 1) & ~1);
-    ScoreWorkspace w{};
-    w.off_tok = up(records * rows * sizeof(float4));
+    const size_t groups = (size_t)cut.n_slices * cut.groups_per_slice();
+    Workspace w{};
+    w.off_tok = up(2 * (size_t)cut.n_slices * rows * sizeof(float4));
     w.off_max = w.off_tok + up((size_t)rows * sizeof(float));
     w.off_logits = w.off_max + (alternatives ? up((size_t)rows * groups * sizeof(float)) : 0);
     w.bytes = w.off_logits + (alternatives ? (size_t)rows * groups * 32 * sizeof(float) : 0);
     return w;
 }
 
-int launch_score(const FusedState* fs, const HeadDesc& head, const void* H, const RowsParams& rp, unsigned char* ws, uint32_t* err,
+}  // namespace
+
+size_t score_workspace_bytes(const ScoreState* st, int rows, bool alternatives) {
+    // calls of fewer rows may use the other cut
+    const size_t one = workspace(st->cut[0], rows < kRowsM ? rows : kRowsM, alternatives).bytes;
+    const size_t two = rows > kRowsM ? workspace(st->cut[1], rows, alternatives).bytes : 0;
+    return one > two ? one : two;
+}
+
+int launch_score(const ScoreState* st, const HeadDesc& head, const void* H, const RowsParams& rp, unsigned char* ws, uint32_t* err,
                  long long wait_limit, bool allow_pdl, cudaStream_t stream) {
-    const SliceGeometry& geo = fused_slices(fs);
+    if (rp.rows > kScoreChunk) return DM_EUNSUPPORTED;
+    const bool pair = rp.rows > kRowsM;
+    const ScoreState::Cut& cut = st->cut[pair];
     ScoreParams P{};
     P.d = head.d; P.V = head.V; P.rows = rp.rows;
-    if (!plan(rp.rows, &P)) return DM_EUNSUPPORTED;
     P.kb_count = head.d / kBlockK;
-    P.tiles_per_cta = geo.tiles_per_cta; P.tile_rows = geo.tile_rows; P.slice_rows = geo.slice_rows;
+    P.slice = cut.slice; P.n_tiles = cut.n_tiles; P.tile_n = cut.tile_n; P.last_n = cut.last_n;
+    P.n_blk = rp.rows > 2 * kRowsM ? 2 : 1;
+    P.n_slots = kTmemCols / (P.n_blk * kTileN);
+    P.w_bytes = ((uint32_t)(cut.tile_n >> pair) * (kBlockK * 2) + 1023u) & ~1023u;   // swizzle atoms start on 1024-byte boundaries
+    P.step_bytes = P.w_bytes + (uint32_t)P.n_blk * kHBytes;
+    const int box = pair ? kRowsM : (rp.rows + 7) & ~7;
+    P.h_bytes = (uint32_t)box * (kBlockK * 2);
+    const uint32_t out_bytes = rp.n_top > 0 && rp.rows > kDirectRows ? kEpiWarps * 4096u : 0u;
+    P.n_steps = (int)((kSmemLimit - 1024 - kBarBytes - out_bytes) / P.step_bytes);
+    if (P.n_steps > kMaxSteps) P.n_steps = kMaxSteps;
+    P.off_out = (uint32_t)P.n_steps * P.step_bytes;
+    P.off_bar = P.off_out + out_bytes;
     P.pdl = allow_pdl ? 1 : 0;
     P.wait_limit = wait_limit > 0 ? wait_limit : kWaitLimitCycles;
     P.c = rp.c;
-    const int ctas = (geo.n_ctas + 1) & ~1;
-    P.n_groups = score_groups(geo);
-    const ScoreWorkspace w = score_workspace(geo, rp.rows, rp.n_top > 0);
+    P.groups_per_tile = cut.groups_per_tile;
+    P.groups_per_slice = cut.groups_per_slice();
+    P.n_groups = cut.n_slices * P.groups_per_slice;
+    const Workspace w = workspace(cut, rp.rows, rp.n_top > 0);
     P.tokens = rp.tokens;
     P.records = reinterpret_cast<float4*>(ws);
     P.tok_logit = reinterpret_cast<float*>(ws + w.off_tok);
@@ -590,43 +656,51 @@ int launch_score(const FusedState* fs, const HeadDesc& head, const void* H, cons
     }
     P.err = err;
     CUtensorMap tmap_h;
-    if (!tensor_map_bf16(&tmap_h, H, rp.rows, head.d, P.n_pad / 2)) return DM_ECUDA;
-    const size_t smem = P.off_bar + kBarBytes + 1024;
-    if (cudaFuncSetAttribute(score_head_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) {
-        cudaGetLastError();
-        return DM_ECUDA;
-    }
+    if (!tensor_map_bf16(&tmap_h, H, rp.rows, head.d, box)) return DM_ECUDA;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.gridDim = dim3((unsigned)(cut.n_slices << pair));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = P.off_bar + kBarBytes + 1024;
     cfg.stream = stream;
     cudaLaunchAttribute attrs[2]{};
-    attrs[0].id = cudaLaunchAttributeClusterDimension;
-    attrs[0].val.clusterDim.x = 2; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
-    attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attrs[1].val.programmaticStreamSerializationAllowed = 1;
+    int n_attrs = 0;
+    if (allow_pdl) {
+        attrs[n_attrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attrs[n_attrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (pair) {
+        attrs[n_attrs].id = cudaLaunchAttributeClusterDimension;
+        attrs[n_attrs].val.clusterDim.x = 2; attrs[n_attrs].val.clusterDim.y = 1; attrs[n_attrs++].val.clusterDim.z = 1;
+    }
     cfg.attrs = attrs;
-    cfg.numAttrs = allow_pdl ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, score_head_kernel, geo.tmap_w, tmap_h, P) != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+    cfg.numAttrs = n_attrs;
+    const cudaError_t launched = pair ? cudaLaunchKernelEx(&cfg, score_head_kernel<true>, cut.w, cut.w_last, tmap_h, P)
+                                      : cudaLaunchKernelEx(&cfg, score_head_kernel<false>, cut.w, cut.w_last, tmap_h, P);
+    if (launched != cudaSuccess || cudaGetLastError() != cudaSuccess) {
         cudaGetLastError();
         return DM_ECUDA;
     }
     FinishParams F{};
-    F.rows = rp.rows; F.V = head.V; F.n_records = 4 * ctas; F.n_groups = P.n_groups;
-    F.tiles_per_cta = geo.tiles_per_cta; F.tile_rows = geo.tile_rows; F.slice_rows = geo.slice_rows;
+    F.rows = rp.rows; F.V = head.V; F.n_records = 2 * cut.n_slices; F.n_groups = P.n_groups;
+    // groups up to the end of the vocabulary: full tiles, then the groups that the last tile reaches into
+    const int in_last = head.V - (cut.n_slices - 1) * cut.slice;
+    F.n_written = (cut.n_slices - 1) * P.groups_per_slice + in_last / cut.tile_n * cut.groups_per_tile + (in_last % cut.tile_n + 31) / 32;
+    F.groups_per_tile = cut.groups_per_tile; F.n_tiles = cut.n_tiles; F.slice = cut.slice; F.tile_n = cut.tile_n;
     F.c = rp.c; F.inv_temp = rp.inv_temp;
     F.records = P.records; F.tok_logit = P.tok_logit; F.group_max = P.group_max; F.logits = P.logits;
     F.tokens = rp.tokens; F.err = err;
     F.n_top = rp.n_top;
     F.out_logprob = rp.out_logprob; F.out_lse = rp.out_lse; F.out_entropy = rp.out_entropy;
     F.out_top_ids = rp.out_top_ids; F.out_top_logprob = rp.out_top_logprob;
+    cudaLaunchAttribute behind{};   // (what the kernel reads it waits for: griddep_wait)
+    behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    behind.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t fin{};
     fin.gridDim = dim3((unsigned)rp.rows);
     fin.blockDim = dim3(kFinThreads);
     fin.stream = stream;
-    fin.attrs = attrs + 1;
-    fin.numAttrs = 1;   // (what it reads it waits for: griddep_wait)
+    fin.attrs = &behind;
+    fin.numAttrs = 1;
     if (cudaLaunchKernelEx(&fin, score_finish_kernel, F) != cudaSuccess || cudaGetLastError() != cudaSuccess) {
         cudaGetLastError();
         return DM_ECUDA;
