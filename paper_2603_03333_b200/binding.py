@@ -108,6 +108,8 @@ def _ptr(t):
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}   # of tensors of logits
 
+_empty = torch.empty    # called with sizes, not a tuple of them: half the time
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -378,7 +380,7 @@ class Context:
             raise TypeError("out is the gradient's: it needs grad=True")
         res = {}
         if loss:
-            res["loss"] = torch.empty(lead, dtype=torch.float32, device=self.device)
+            res["loss"] = _empty(*lead, dtype=torch.float32, device=self.device)
         ld_out = 0
         if grad:
             res["grad"], ld_out = self._grad_target(logits, out)
@@ -427,24 +429,20 @@ class Context:
 
     def _grad_target(self, logits, out):
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
-            return out, logits.shape[-1]
+            return _empty(*logits.shape, dtype=logits.dtype, device=self.device), logits.shape[-1]
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise TypeError("out must have the logits' shape and dtype")
         return out, self._rows(out, "out")[1]
 
     def _row_outputs(self, lead, tokens, n_top):
-        self._per_row(tokens, torch.int32, lead, "tokens")
-        if tokens is None:
-            lse, entropy = torch.empty((2, *lead), dtype=torch.float32, device=self.device).unbind(0)
-            out = dict(lse=lse, entropy=entropy)
-        else:
-            lse, entropy, logprob = torch.empty((3, *lead), dtype=torch.float32, device=self.device).unbind(0)
-            out = dict(lse=lse, entropy=entropy, logprob=logprob)
+        dev, f32 = self.device, torch.float32
+        out = dict(lse=_empty(*lead, dtype=f32, device=dev), entropy=_empty(*lead, dtype=f32, device=dev))
+        if tokens is not None:
+            self._per_row(tokens, torch.int32, lead, "tokens")
+            out["logprob"] = _empty(*lead, dtype=f32, device=dev)
         if n_top > 0:
-            shape = (*lead, n_top)
-            out["top_ids"] = torch.empty(shape, dtype=torch.int32, device=self.device)
-            out["top_logprob"] = torch.empty(shape, dtype=torch.float32, device=self.device)
+            out["top_ids"] = _empty(*lead, n_top, dtype=torch.int32, device=dev)
+            out["top_logprob"] = _empty(*lead, n_top, dtype=f32, device=dev)
         return out
 
     @staticmethod

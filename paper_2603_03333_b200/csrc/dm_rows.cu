@@ -548,23 +548,18 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
     // a thread without an entry has key 0; padding and masked entries have the key of -inf
     const bool any = sh.first + (int)threadIdx.x < sh.last;
     const uint32_t my_key = any ? logit_key(thread_max) : 0u;
+    // the k-th largest of the threads' maxima: k threads hold an entry that large (0 if fewer have one)
     uint32_t* keys = reinterpret_cast<uint32_t*>(cand);   // (not yet in use)
     keys[threadIdx.x] = my_key;
+    if (threadIdx.x == 0) ss.threshold = 0u;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        uint32_t mine[kWarps];
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) mine[i] = keys[32 * i + threadIdx.x];
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t c = t | (1u << bit);
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) n += __popc(__ballot_sync(0xFFFFFFFFu, mine[i] >= c));
-            if (n >= k) { t = c; if (n <= k + (k >> 1)) break; }   // any lower bound will do; a close one leaves few candidates
-        }
-        if (threadIdx.x == 0) ss.threshold = t;
+    int reach = 0;
+#pragma unroll 8
+    for (int i = 0; i < kThreads / 4; ++i) {
+        const uint4 o = reinterpret_cast<const uint4*>(keys)[i];
+        reach += (o.x >= my_key) + (o.y >= my_key) + (o.z >= my_key) + (o.w >= my_key);
     }
+    if (reach >= k && my_key != 0u) atomicMax(&ss.threshold, my_key);
     __syncthreads();
     const uint32_t thr = ss.threshold;
     int n = collect(sh, my_key, thr, slots, slot_batches, ss, cand);
@@ -974,9 +969,9 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
     }
     const bool grad = kOp != OP_LOGPROBS && P.out_grad != nullptr;
     const int n_vec = (P.V + 2 * N - 2) / N;          // at most, whatever the row's alignment
-    // CTAs per row: as many as run at once where rows are few, not less than one vector per thread; gradient kernels cut a row until three shares fit an SM's shared memory.
+    // CTAs per row: as many as run at once where rows are few, not less than one batch each; gradient kernels cut a row until three shares fit an SM's shared memory.
     int cluster = 1;
-    while (cluster < kRowsMaxCluster && 2ll * P.rows * cluster <= (grad ? 3ll : 4ll) * sms && n_vec > cluster * kThreads) cluster *= 2;
+    while (cluster < kRowsMaxCluster && 2ll * P.rows * cluster <= (grad ? 3ll : 4ll) * sms && n_vec > cluster * kBatch) cluster *= 2;
     if (grad)
         while (cluster < kRowsMaxCluster && (n_vec + cluster - 1) / cluster > kStashVecs) cluster *= 2;
     const int per = (n_vec + cluster - 1) / cluster, batches = (per + kBatch - 1) / kBatch;

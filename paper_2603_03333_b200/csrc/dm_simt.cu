@@ -129,7 +129,8 @@ static int launch_simt_rc(const HeadDesc& head, const void* H, int rows, const R
     if (v_per_block < 8) v_per_block = 8;
     const int n_slices = (head.V + v_per_block - 1) / v_per_block;
     auto kern = simt_head_kernel<T, RC>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    if (smem > 48 * 1024 &&   // (a microsecond of host time that smaller launches need not spend)
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
         return DM_ECUDA;
     kern<<<n_slices, 256, smem, stream>>>(static_cast<const T*>(head.W), static_cast<const T*>(H),
                                           head.V, head.d, rows, map, mk.key0, mk.key1, mk.thr,
