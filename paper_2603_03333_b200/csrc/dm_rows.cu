@@ -47,6 +47,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;             // vectors of a batch: 16-byte loads in flight per thread
 constexpr int kRing = DM_ROWS_RING;    // batches in flight where rows stream
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
+constexpr int kHitCap = 2048;          // batches that hold them
 constexpr int kMaxSlots = 16;          // maxima a thread keeps of its batches (for finding the top entries again)
 constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 0 in fp32, and 0 * clamp stays 0
 constexpr int kStashVecs = 4096;       // share of a gradient kernel's CTA up to which a row is cut: 64 KB, three CTAs per SM
@@ -351,6 +352,10 @@ struct Stats {
 
 struct Merged { float m, rest, t, tail; };   // maximum; sums relative to it, `rest` without one maximal entry
 
+// Cluster barrier in two halves; every thread of every CTA takes both.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 __device__ __forceinline__ float warp_sum(float x) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, off);
@@ -360,10 +365,10 @@ __device__ __forceinline__ float warp_sum(float x) {
 struct RowsShared {
     float w_m[kWarps], w_s[kWarps], w_t[kWarps], w_tail[kWarps];
     int w_cnt[kWarps];
-    Merged mine;                 // this CTA's statistics, read by the others of the cluster
+    Merged part[kRowsMaxCluster];   // every CTA's statistics, each written by its CTA
     Merged all;                  // the row's
     float log_total, inv_total;  // log(1 + rest), 1 / (1 + rest)
-    int cand_n;
+    int cand_n, hit_n;
     uint32_t threshold;
     unsigned int scan[kWarps];
     // teacher (distill): warps 0..3 hold its entries, one per thread
@@ -375,8 +380,9 @@ struct RowsShared {
     int t_distinct, t_repeated;
 };
 
-// The block's statistics from its warps'; complete in ss.mine after the next barrier.
-__device__ void block_merge(Stats& st, float c, RowsShared& ss) {
+// The block's statistics from its warps', written to every CTA of the cluster (complete behind the
+// next cluster barrier: nobody reads another CTA's shared memory, so nobody waits for anybody to leave).
+__device__ void block_merge(Stats& st, float c, RowsShared& ss, cg::cluster_group& cluster, int n_cta, int rank) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     st.finish();
     const float s = warp_sum(st.s), t = warp_sum(st.t), tail = warp_sum(st.tail);
@@ -407,18 +413,20 @@ __device__ void block_merge(Stats& st, float c, RowsShared& ss) {
     for (int off = 16; off > 0; off >>= 1) cnt += __shfl_xor_sync(0xFFFFFFFFu, cnt, off);
     if (cnt > 1) r.rest += (float)(cnt - 1);
     if (!(m < __uint_as_float(0x7F800000u))) r.rest = r.t = r.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
-    if (lane == 0) ss.mine = r;
+    if (n_cta == 1) {
+        if (lane == 0) ss.part[0] = r;
+    } else if (lane < n_cta) {
+        cluster.map_shared_rank(&ss, lane)->part[rank] = r;
+    }
 }
 
-// The row's statistics from its CTAs' (published and synchronised), one lane per CTA; warp 0 only.
-__device__ void cluster_merge(cg::cluster_group& cluster, RowsShared& ss, int n_cta, float c) {
+// The row's statistics from its CTAs', one lane per CTA; warp 0 only.
+__device__ void cluster_merge(RowsShared& ss, int n_cta, float c) {
     const int lane = threadIdx.x & 31;
-    Merged a;
-    if (n_cta == 1) {
-        a = ss.mine;
-    } else {
+    Merged a = ss.part[0];
+    if (n_cta > 1) {
         Merged part{neg_inf(), 0.0f, 0.0f, 0.0f};
-        if (lane < n_cta) part = *cluster.map_shared_rank(&ss.mine, lane);
+        if (lane < n_cta) part = ss.part[lane];
         float m = part.m;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
@@ -443,31 +451,63 @@ __device__ void cluster_merge(cg::cluster_group& cluster, RowsShared& ss, int n_
 
 // ---------------------------------------------------------------------------- the largest entries
 // Entries of the share with a key of at least `key_min` go to the candidate list.  Each thread looks
-// at the maxima it kept of its batches and reads only those batches again that hold one.
+// at the maxima it kept of its batches; those that pass go to a list of hits, and the vectors behind
+// the hits are read again by all threads, one vector each (read by the thread that owned them, one
+// after the other, they took 8 to 25 thousand cycles).  More hits than the list takes count as an
+// overflow of the candidate list.
 template <typename T>
 __device__ int collect(const Share<T>& sh, uint32_t my_key, uint32_t key_min, const uint32_t* slots, int slot_batches,
-                       RowsShared& ss, unsigned long long* cand) {
+                       RowsShared& ss, int* hits, unsigned long long* cand) {
+    constexpr int N = RowVec<T>::N;
+    if (threadIdx.x == 0) ss.cand_n = ss.hit_n = 0;
+    __syncthreads();
+    const int per_slot = kUnroll * slot_batches, n_slots = (sh.last - sh.first + per_slot * kThreads - 1) / (per_slot * kThreads);
+    if (my_key >= key_min) {
+        for (int slot = 0; slot < n_slots; ++slot)
+            if (slots[slot * kThreads + threadIdx.x] >= key_min) {
+                const int at = atomicAdd(&ss.hit_n, 1);
+                if (at < kHitCap) hits[at] = slot * per_slot * kThreads + (int)threadIdx.x;   // first vector of the slot, within the share
+            }
+    }
+    __syncthreads();
+    const int n_hits = min(ss.hit_n, kHitCap);
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n_hits * per_slot; i += kThreads) {
+        const int h = i / per_slot, j = sh.first + hits[h] + (i - h * per_slot) * kThreads;
+        if (j >= sh.last) continue;
+        float x[N];
+        RowVec<T>::unpack(sh.load(j), x);
+        const int i0 = sh.entry0(j);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t key = logit_key(x[n]);
+            if (key >= key_min && i0 + n >= 0 && i0 + n < sh.V) {
+                const int at = atomicAdd(&ss.cand_n, 1);
+                if (at < kCandCap) cand[at] = pack_best(key, (uint32_t)(i0 + n));
+            }
+        }
+    }
+    __syncthreads();
+    const int n = ss.hit_n > kHitCap ? kCandCap + 1 : ss.cand_n;
+    __syncthreads();
+    return n;
+}
+// Entries with a key above `key_min` (fewer than a list takes), read again by threads that hold one.
+template <typename T>
+__device__ int collect_above(const Share<T>& sh, uint32_t my_key, uint32_t key_min, RowsShared& ss, unsigned long long* cand) {
     constexpr int N = RowVec<T>::N;
     if (threadIdx.x == 0) ss.cand_n = 0;
     __syncthreads();
-    if (my_key >= key_min) {
-        int slot = 0;
-        for (int b0 = sh.first; b0 < sh.last; b0 += kUnroll * kThreads * slot_batches, ++slot) {
-            if (slots[slot * kThreads + threadIdx.x] < key_min) continue;
-            const int end = min(sh.last, b0 + kUnroll * kThreads * slot_batches);
+    if (my_key > key_min) {
 #pragma unroll 4
-            for (int j = b0 + (int)threadIdx.x; j < end; j += kThreads) {
-                float x[N];
-                RowVec<T>::unpack(sh.load(j), x);
-                const int i0 = sh.entry0(j);
+        for (int j = sh.first + (int)threadIdx.x; j < sh.last; j += kThreads) {
+            float x[N];
+            RowVec<T>::unpack(sh.load(j), x);
+            const int i0 = sh.entry0(j);
 #pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const uint32_t key = logit_key(x[n]);
-                    if (key >= key_min && i0 + n >= 0 && i0 + n < sh.V) {
-                        const int at = atomicAdd(&ss.cand_n, 1);
-                        if (at < kCandCap) cand[at] = pack_best(key, (uint32_t)(i0 + n));
-                    }
-                }
+            for (int n = 0; n < N; ++n) {
+                const uint32_t key = logit_key(x[n]);
+                if (key > key_min && i0 + n >= 0 && i0 + n < sh.V) cand[atomicAdd(&ss.cand_n, 1)] = pack_best(key, (uint32_t)(i0 + n));
             }
         }
     }
@@ -544,25 +584,32 @@ __device__ void collect_ties(const Share<T>& sh, uint32_t key, int need, int at,
 // equal entries, or k large ones in few threads) the k-th largest key is found exactly.
 template <typename T>
 __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const uint32_t* slots, int slot_batches,
-                             RowsShared& ss, unsigned long long* cand, unsigned long long* sorted) {
+                             RowsShared& ss, int* hits, unsigned long long* cand, unsigned long long* sorted) {
     // a thread without an entry has key 0; padding and masked entries have the key of -inf
     const bool any = sh.first + (int)threadIdx.x < sh.last;
     const uint32_t my_key = any ? logit_key(thread_max) : 0u;
-    // the k-th largest of the threads' maxima: k threads hold an entry that large (0 if fewer have one)
+    // The k-th largest of the maxima of groups of threads: k groups hold an entry that large (0 if fewer
+    // have one).  At least twice as many groups as entries are wanted: a close bound at the least work.
+    const int group = k <= 16 ? 8 : k <= 32 ? 4 : k <= 64 ? 2 : 1, n_groups = kThreads / group;
     uint32_t* keys = reinterpret_cast<uint32_t*>(cand);   // (not yet in use)
-    keys[threadIdx.x] = my_key;
+    uint32_t mine = my_key;
+    for (int off = group >> 1; off > 0; off >>= 1) mine = max(mine, __shfl_xor_sync(0xFFFFFFFFu, mine, off));
+    if ((int)threadIdx.x % group == 0) keys[threadIdx.x / group] = mine;
     if (threadIdx.x == 0) ss.threshold = 0u;
     __syncthreads();
-    int reach = 0;
+    if ((int)threadIdx.x < n_groups) {
+        mine = keys[threadIdx.x];
+        int reach = 0;
 #pragma unroll 8
-    for (int i = 0; i < kThreads / 4; ++i) {
-        const uint4 o = reinterpret_cast<const uint4*>(keys)[i];
-        reach += (o.x >= my_key) + (o.y >= my_key) + (o.z >= my_key) + (o.w >= my_key);
+        for (int i = 0; i < n_groups / 4; ++i) {
+            const uint4 o = reinterpret_cast<const uint4*>(keys)[i];
+            reach += (o.x >= mine) + (o.y >= mine) + (o.z >= mine) + (o.w >= mine);
+        }
+        if (reach >= k && mine != 0u) atomicMax(&ss.threshold, mine);
     }
-    if (reach >= k && my_key != 0u) atomicMax(&ss.threshold, my_key);
     __syncthreads();
     const uint32_t thr = ss.threshold;
-    int n = collect(sh, my_key, thr, slots, slot_batches, ss, cand);
+    int n = collect(sh, my_key, thr, slots, slot_batches, ss, hits, cand);
     if (n > kCandCap) {
         // exact: the k-th largest key of the share.  First guess: the exact k-th largest thread
         // maximum, which is it whenever fewer than k entries lie above (a row full of equal entries).
@@ -579,7 +626,7 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
             }
             kth = lo;
         }
-        n = kth == 0xFFFFFFFFu ? 0 : collect(sh, my_key, kth + 1u, slots, slot_batches, ss, cand);   // fewer than k
+        n = kth == 0xFFFFFFFFu ? 0 : collect_above(sh, my_key, kth, ss, cand);   // fewer than k
         collect_ties(sh, kth, k - n, n, ss, cand);
         n = k;
         __syncthreads();
@@ -589,7 +636,7 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
     for (int i = threadIdx.x; i < n; i += kThreads) {   // the packed words are all different: rank by counting
         const unsigned long long mine = cand[i];
         int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
         for (int o = 0; o < n; ++o) rank += cand[o] > mine ? 1 : 0;
         if (rank < k) sorted[rank] = mine;
     }
@@ -619,15 +666,18 @@ rows_kernel(const RowsParams P) {
     constexpr int kBatch = kUnroll * kThreads;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowsShared ss;
-    uint4* stash = reinterpret_cast<uint4*>(smem);                                      // [stash_vecs], vector first + x
-    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);     // distill: teacher tokens of the share, a byte per vector
-    unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // logprobs: candidates, then the sorted list
-    unsigned long long* sorted = cand + kCandCap;
-    uint32_t* slots = reinterpret_cast<uint32_t*>(stash + kRing * kBatch);              // maxima of the threads' batches (the lists take the ring's place)
-    unsigned long long* merged = cand;                                                  // rank 0: every CTA's list (the candidates are done with)
-
     cg::cluster_group cluster = cg::this_cluster();
     const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    if (n_cta > 1) cluster_arrive();   // (waited for before anything is written to another CTA's shared memory)
+    uint4* stash = reinterpret_cast<uint4*>(smem);                                      // [stash_vecs], vector first + x
+    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);     // distill: teacher tokens of the share, a byte per vector
+    // logprobs: behind the ring what is kept while the row streams, in the ring's place what comes after
+    unsigned long long* merged = reinterpret_cast<unsigned long long*>(stash + kRing * kBatch);   // rank 0: every CTA's sorted list
+    uint32_t* slots = reinterpret_cast<uint32_t*>(merged + (n_cta > 1 ? n_cta * P.n_top : 0));    // maxima of the threads' batches
+    unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // candidates
+    unsigned long long* sorted = cand + kCandCap;                                       // the largest of the share, sorted
+    int* hits = reinterpret_cast<int*>(sorted + kRowsMaxTop);                           // [kHitCap]
+
     const int row = (int)(blockIdx.x / (unsigned)n_cta), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float c = P.c;
 
@@ -772,15 +822,24 @@ rows_kernel(const RowsParams P) {
             }
         }
         if (!kResident) copy_wait(0);   // (what is still in flight are empty batches)
-        block_merge(st, c, ss);
-        if (kOp == OP_LOGPROBS && P.n_top > 0) top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, cand, sorted);
-        if (n_cta > 1) cluster.sync();
-        if (warp == 0) {
-            __syncwarp();
-            cluster_merge(cluster, ss, n_cta, c);
+        if (n_cta > 1) cluster_wait();
+        block_merge(st, c, ss, cluster, n_cta, rank);
+        if (kOp == OP_LOGPROBS && P.n_top > 0) {
+            top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, hits, cand, sorted);
+            if (n_cta > 1)
+                for (int i = tid; i < P.n_top; i += kThreads) cluster.map_shared_rank(merged, 0)[rank * P.n_top + i] = sorted[i];
         }
+        if (n_cta > 1) {
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        if (warp == 0) cluster_merge(ss, n_cta, c);
     } else {
         copy_wait(0);
+        if (n_cta > 1) cluster_wait();
         if (tid == 0) {
             ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
             ss.log_total = ss.inv_total = 0.0f;
@@ -806,12 +865,7 @@ rows_kernel(const RowsParams P) {
             // merge of sorted lists: the rank of an entry is its place in its own list plus the number
             // of larger ones in each other list
             const int k = P.n_top;
-            const unsigned long long* lists = sorted;
-            if (n_cta > 1) {
-                for (int i = tid; i < n_cta * k; i += kThreads) merged[i] = cluster.map_shared_rank(sorted, i / k)[i % k];
-                __syncthreads();
-                lists = merged;
-            }
+            const unsigned long long* lists = n_cta > 1 ? merged : sorted;
             for (int i = tid; i < n_cta * k; i += kThreads) {
                 const unsigned long long mine = lists[i];
                 if (mine == 0ull) continue;
@@ -952,7 +1006,6 @@ rows_kernel(const RowsParams P) {
             }
         }
     }
-    if (n_cta > 1) cluster.sync();   // nobody leaves while another CTA may still read its shared memory
 }
 
 template <typename T, int kOp, bool kResident>
@@ -983,7 +1036,8 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
         P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
         const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
         smem += (size_t)n_slots * kThreads * sizeof(uint32_t);
-        static_assert((kCandCap + kRowsMaxTop) * sizeof(unsigned long long) <= (size_t)kRing * kBatch * 16, "the lists fit the ring");
+        if (cluster > 1) smem += (size_t)cluster * P.n_top * sizeof(unsigned long long);
+        static_assert((kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + kHitCap * sizeof(int) <= (size_t)kRing * kBatch * 16, "the lists fit the ring");
     }
     if (smem > kRowsSmemLimit) return DM_EUNSUPPORTED;
     if (kOp != OP_LOGPROBS && resident) return launch_kernel<T, kOp, kOp != OP_LOGPROBS>(P, dev, cluster, smem, stream);
