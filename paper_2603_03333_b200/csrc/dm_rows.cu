@@ -420,29 +420,22 @@ __device__ void block_merge(Stats& st, float c, RowsShared& ss, cg::cluster_grou
     }
 }
 
-// The row's statistics from its CTAs', one lane per CTA; warp 0 only.
+// The row's statistics from its CTAs', by one warp whose lanes all do the same: a few dozen dependent
+// instructions, where shuffles among lanes that have come apart cost 250 cycles each.
 __device__ void cluster_merge(RowsShared& ss, int n_cta, float c) {
-    const int lane = threadIdx.x & 31;
     Merged a = ss.part[0];
-    if (n_cta > 1) {
-        Merged part{neg_inf(), 0.0f, 0.0f, 0.0f};
-        if (lane < n_cta) part = ss.part[lane];
-        float m = part.m;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-        const unsigned int holders = __ballot_sync(0xFFFFFFFFu, part.m == m);
-        if (m != neg_inf() && lane != __ffs(holders) - 1) {   // everybody but one holder of the maximum adds all of its entries
-            const float d = fmaxf((part.m - m) * c, kFloorExp), f = ex2(d), all = part.m == neg_inf() ? 0.0f : part.rest + 1.0f;
-            part.rest = f * all;
-            part.t = f * fmaf(d, all, part.t);
-            part.tail *= f;
-        }
-        a.m = m;
-        a.rest = warp_sum(part.rest);
-        a.t = warp_sum(part.t);
-        a.tail = warp_sum(part.tail);
+#pragma unroll 1
+    for (int r = 1; r < n_cta; ++r) {
+        const Merged p = ss.part[r];
+        const bool up = !(p.m <= a.m);                     // (a NaN on either side ends up as the maximum)
+        const Merged hi = up && a.m == a.m ? p : a, lo = up && a.m == a.m ? a : p;
+        const float d = fmaxf((lo.m - hi.m) * c, kFloorExp), f = lo.m == neg_inf() ? 0.0f : ex2(d), all = lo.rest + 1.0f;
+        a.m = hi.m;
+        a.rest = fmaf(f, all, hi.rest);
+        a.t = fmaf(f, fmaf(d, all, lo.t), hi.t);
+        a.tail = fmaf(f, lo.tail, hi.tail);
     }
-    if (lane == 0) {
+    if ((threadIdx.x & 31) == 0) {
         ss.all = a;
         ss.log_total = log1pf(a.rest);
         ss.inv_total = 1.0f / (1.0f + a.rest);
