@@ -9,7 +9,7 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libdropmatch.so"
 SOURCES = ["dm_api.cu", "dm_simt.cu", "dm_finalize.cu", "dm_fused_sm100.cu", "dm_noalloc.cu", "dm_js.cu", "dm_sample.cu", "dm_rows.cu",
-           "dm_score_sm100.cu"]
+           "dm_rows_grad.cu", "dm_score_sm100.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "-cudart", "static"]
 

@@ -819,6 +819,7 @@ int dropmatch_logprobs_grad(dm_ctx* c, const void* logits, int dtype, int64_t ld
     if (!g.ok) return DM_ECUDA;
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
+    rp.err_out = c->err;
     rp.tokens = tokens;
     rp.g_logprob = g_logprob; rp.g_entropy = g_entropy;
     rp.out_grad = out_grad; rp.ld_grad = ld_grad;
@@ -841,6 +842,7 @@ int dropmatch_distill(dm_ctx* c, const void* logits, int dtype, int64_t ld, int 
     if (!g.ok) return DM_ECUDA;
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
+    rp.err_out = c->err;
     rp.t_ids = teacher_ids; rp.t_logprob = teacher_logprob;
     rp.k = k; rp.tail = tail;
     rp.weight = weight;

@@ -15,7 +15,8 @@ enum : uint32_t {
     ERR_WAIT_ACC_FULL = 4,  // epilogue gave up waiting for an accumulator
     ERR_WAIT_ACC_EMPTY = 5, // MMA issuer gave up waiting for a drained accumulator
     ERR_BAD_ROW = 6,        // debug row selection out of range
-    ERR_WAIT_JS = 7         // a block of the one-kernel JS sweep gave up waiting for the other blocks of its position
+    ERR_WAIT_JS = 7,        // a block of the one-kernel JS sweep gave up waiting for the other blocks of its position
+    ERR_WAIT_ROW = 8        // a cluster of a row kernel gave up waiting for the answer to its request for another row
 };
 
 // One path ("row") of a call: which hidden row it masks and its mask key words.

@@ -294,6 +294,28 @@ __device__ __forceinline__ void griddep_launch_dependents() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// ---- cluster launch control -------------------------------------------------------------------
+// A running cluster asks for one that has not been launched yet: if the request succeeds, that cluster
+// never starts and the asker does its work.  A kernel whose clusters walk over work this way balances
+// itself like separate clusters do, but can fetch the next piece ahead.  The answer (16 bytes) lands in
+// shared memory and counts 16 bytes on an mbarrier; after a request that failed no other may be made.
+__device__ __forceinline__ void request_next_cluster(uint32_t answer_smem, uint32_t bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+                 ::"r"(answer_smem), "r"(bar) : "memory");
+}
+// x index of the granted cluster's first CTA, or -1.
+__device__ __forceinline__ int granted_cluster(uint32_t answer_smem) {
+    int x;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+        "ld.shared.b128 r, [%1];\n\t"
+        "mov.s32 %0, -1;\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+        : "=&r"(x) : "r"(answer_smem) : "memory");
+    return x;
+}
+
 // Named barrier among a subset of warps.
 __device__ __forceinline__ void bar_sync(int id, int threads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");

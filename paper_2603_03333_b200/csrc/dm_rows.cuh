@@ -18,6 +18,7 @@ struct RowsParams {
     int stash_vecs;       // 16-byte vectors in shared memory: a CTA's share, or the ring it streams through (set by the launch)
     int slot_batches;     // batches of a thread that share one remembered maximum (set by the launch)
     const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
+    uint32_t* err_out;    // device error word of the call's context (gradient kernels)
     // logprobs
     const int32_t* tokens;
     int n_top;
@@ -39,5 +40,9 @@ struct RowsParams {
 int launch_rows_logprobs(const RowsParams& P, int dtype, cudaStream_t stream);
 int launch_rows_grad(const RowsParams& P, int dtype, cudaStream_t stream);
 int launch_rows_distill(const RowsParams& P, int dtype, cudaStream_t stream);
+
+// The gradient kernels whose rows stay in shared memory.  False: the row is too long for that, nothing
+// was launched; true: *status is the outcome.
+bool launch_rows_resident(const RowsParams& P, int dtype, bool distill, cudaStream_t stream, int* status);
 
 }  // namespace dm

@@ -1,0 +1,385 @@
+// Gradients on rows of logits whose shares fit in shared memory: the gradient of log-probability and
+// entropy, and distillation with its gradient (dm_rows.cu states the mathematics).
+//
+// Bound: memory, one read and one write of the row.  A cluster of CTAs takes row after row (there is one
+// cluster per row in the grid; a running one takes over rows of clusters that have not started, so that
+// fast and slow SMs share the rows out between them); each CTA keeps its share (up to 64 KB as a rule, three CTAs per SM) in shared memory: one pass over it finds the
+// maximum, one sums, one writes the gradient.  As soon as a thread has converted a batch, the copies of
+// the next row's batch into the same slots are on their way, so that loading overlaps the tail of the
+// row, its barriers and the beginning of the next one.  The CTAs of a cluster meet once per row: every
+// warp writes its sums into every CTA's shared memory ahead of one cluster barrier.
+#include <cooperative_groups.h>
+
+#include "dm_ptx.cuh"
+#include "dm_rows_dev.cuh"
+
+namespace dm {
+
+namespace {
+
+namespace cg = cooperative_groups;
+using namespace rows;
+
+constexpr int kBatch = kUnroll * kThreads;
+constexpr int kShareVecs = 4096;        // share up to which a row is cut: 64 KB, three CTAs per SM
+constexpr int kTeacherWarps = kRowsMaxTop / 32;
+constexpr long long kWaitLimitCycles = 2000000000ll;   // about one second
+
+struct WarpSums { float s, t, tail, cnt; };   // relative to the CTA's maximum: below it; entries equal to it
+
+struct ResidentShared {
+    uint4 answer;                  // to the request for another row (rank 0)
+    uint64_t answer_bar;
+    int abort;
+    int next_row[2];               // written by rank 0 into every CTA, twice over
+    float w_max[kWarps];
+    // written by every CTA of the cluster, twice over: a CTA may be one row ahead of another
+    float part_m[2][kRowsMaxCluster];
+    WarpSums part[2][kRowsMaxCluster][kWarps];
+    Merged cta[kRowsMaxCluster];
+    Merged all;
+    float log_total, inv_total;
+    // teacher (distill), twice over: the loss of a row is finished while the next one has begun
+    int t_id[2][kRowsMaxTop];
+    float t_v[2][kRowsMaxTop], t_x[2][kRowsMaxTop], t_q[2][kRowsMaxTop];
+    float t_max[kTeacherWarps];
+    double t_sum[kTeacherWarps];
+    int t_distinct, t_repeated;
+};
+
+template <typename T, int kOp>
+__global__ void __launch_bounds__(kThreads, 3)
+rows_resident_kernel(const RowsParams P) {
+    constexpr int N = RowVec<T>::N;
+    constexpr bool kEntropy = kOp == OP_GRAD, kTail = kOp == OP_DISTILL;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ ResidentShared ss;
+    uint4* stash = reinterpret_cast<uint4*>(smem);                                    // [stash_vecs]
+    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);   // distill: teacher tokens of the share, a byte per vector
+    cg::cluster_group cluster = cg::this_cluster();
+    const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    if (n_cta > 1) cluster_arrive();   // (waited for before anything is written to another CTA's shared memory)
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n_batches = P.stash_vecs / kBatch;   // of the longest share; what a row does not fill is masked
+    const float c = P.c;
+    const bool bucket = kTail && P.tail == DM_TAIL_BUCKET;
+
+    int row = (int)blockIdx.x / n_cta;
+    Share<T> sh = share_of<T>(P, row, n_cta, rank);
+    for (int b = 0; b < n_batches; ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
+    if (kTail) {
+        for (int i = tid; i < P.stash_vecs / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
+    }
+    // the row's small inputs, one row ahead
+    int next_id = -1;              // token, or this thread's teacher token
+    float next_a = 0.0f, next_b = 0.0f;   // gradients of log-probability and entropy, or the teacher's value and the weight
+    const auto load_small = [&](int r) {
+        if (kOp == OP_GRAD) {
+            next_id = P.tokens != nullptr ? P.tokens[r] : -1;
+            next_a = P.g_logprob != nullptr ? P.g_logprob[r] : 0.0f;
+            next_b = P.g_entropy != nullptr ? P.g_entropy[r] : 0.0f;
+        } else {
+            if (tid < P.k) {
+                next_id = P.t_ids[(long long)r * P.k + tid];
+                next_a = P.t_logprob[(long long)r * P.k + tid];
+            }
+            next_b = P.weight != nullptr ? P.weight[r] : 1.0f;
+        }
+    };
+    load_small(row);
+    const uint32_t answer = ptx::smem_u32(&ss.answer), answer_bar = ptx::smem_u32(&ss.answer_bar);
+    if (tid == 0) {
+        ptx::mbar_init(answer_bar, 1);
+        ss.abort = 0;
+        ptx::fence_mbar_init();
+        ptx::fence_proxy_async_smem();
+    }
+    bool started = n_cta == 1;
+
+    for (int par = 0; row >= 0; par ^= 1) {
+        const int n_share = sh.last - sh.first;
+        if (rank == 0 && tid == 0) {   // the answer is waited for when the row's sums are known
+            ptx::mbar_arrive_expect_tx(answer_bar, 16);
+            ptx::request_next_cluster(answer, answer_bar);
+        }
+        T* grad_row = static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad;
+        float w = P.inv_temp, g_lp = 0.0f, g_h = 0.0f;
+        int tok = -1;
+        float tok_x = neg_inf();
+        bool zero_grad;
+        TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
+        if (kOp == OP_GRAD) {
+            if (next_id >= 0 && next_id < P.V) { tok = next_id; tok_x = RowVec<T>::get(sh.row + tok); g_lp = next_a; }
+            g_h = next_b;
+            zero_grad = g_lp == 0.0f && g_h == 0.0f;
+        } else {
+            zero_grad = next_b == 0.0f;
+            w *= next_b;
+            if (tid < P.k && next_id >= 0 && next_id < P.V) {
+                te.id = next_id;
+                te.v = next_a;
+                te.x = RowVec<T>::get(sh.row + te.id);
+            }
+            if (tid < P.k) { ss.t_id[par][tid] = te.id; ss.t_v[par][tid] = te.v; }
+            if (tid == 0) ss.t_distinct = ss.t_repeated = 0;
+            if (warp < kTeacherWarps) {
+                float vm = te.v;
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+                if (lane == 0) ss.t_max[warp] = vm;
+            }
+            __syncthreads();
+        }
+        uint32_t* my_word = nullptr;   // word of the bitmap in which this thread's token is marked
+        float v_shift = 0.0f;          // renorm: the largest teacher value
+        if (kOp == OP_DISTILL) {
+            if (te.id >= 0) {
+                const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
+                if (at >= 0 && at < n_share) {
+                    const uint32_t bit = 1u << (8 * (at & 3) + (te.id + sh.phase) % N);
+                    my_word = reinterpret_cast<uint32_t*>(bitmap) + (at >> 2);
+                    te.first = (atomicOr(my_word, bit) & bit) == 0u;
+                    if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
+                }
+            }
+            if (warp < kTeacherWarps) {
+                float vm = ss.t_max[0];
+#pragma unroll
+                for (int i = 1; i < kTeacherWarps; ++i) vm = fmaxf(vm, ss.t_max[i]);
+                if (P.tail == DM_TAIL_RENORM && vm > neg_inf()) v_shift = vm;
+                if (te.id >= 0) te.q = exp((double)te.v - (double)v_shift);
+                double sum = te.q;
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+                if (lane == 0) ss.t_sum[warp] = sum;
+            }
+        }
+
+        // A row whose gradient is zero whatever it holds is not looked at (unless its loss is wanted).
+        const bool need_stats = !(zero_grad && (kOp == OP_GRAD || P.out_loss == nullptr));
+        // which row comes next, told to every CTA ahead of the row's cluster barrier
+        const auto tell_next = [&]() {
+            if (rank == 0 && warp == 0) {
+                int next = -1;
+                if (lane == 0) {
+                    if (ptx::mbar_wait<32>(answer_bar, (uint32_t)par, &ss.abort, kWaitLimitCycles)) {
+                        next = ptx::granted_cluster(answer);
+                        if (next >= 0) next /= n_cta;
+                        ptx::fence_proxy_async_smem();   // read before the next request writes it
+                    } else {
+                        atomicCAS(P.err_out, 0u, (uint32_t)ERR_WAIT_ROW);
+                    }
+                }
+                next = __shfl_sync(0xFFFFFFFFu, next, 0);
+                if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->next_row[par] = next;
+                __syncwarp();
+            }
+        };
+        const auto meet = [&]() {
+            if (n_cta == 1) {
+                __syncthreads();
+            } else {
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+            }
+        };
+        if (!started) { cluster_wait(); started = true; }
+        if (need_stats) {
+            float thread_max = neg_inf();
+            for (int b = 0; b < n_batches; ++b) {
+                copy_wait(n_batches - 1 - b);
+                uint4 v[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
+                thread_max = max_nan(thread_max, RowVec<T>::vmax(v));
+            }
+            float m = thread_max;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
+            if (lane == 0) ss.w_max[warp] = m;
+            __syncthreads();   // (the teacher's marks are complete behind it, too)
+            m = ss.w_max[0];
+#pragma unroll
+            for (int i = 1; i < kWarps; ++i) m = max_nan(m, ss.w_max[i]);
+            Stats st;
+            st.init();
+            st.set_maximum<T>(m, c);
+            const bool holder = __any_sync(0xFFFFFFFFu, thread_max == m && m != neg_inf());
+            for (int b = 0; b < n_batches && (holder || st.ce != 0.0f); ++b) {
+                uint4 v[kUnroll];
+                uint32_t bits[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    v[u] = stash[b * kBatch + u * kThreads + tid];
+                    bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
+                }
+                if (holder) st.take<T, kTail>(v, bits);
+                if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, bits);
+            }
+            st.finish();
+            WarpSums r{warp_sum(st.s), kEntropy ? warp_sum(st.t) : 0.0f, kTail ? warp_sum(st.tail) : 0.0f, warp_sum((float)st.cnt)};
+            __syncwarp();
+            if (lane < n_cta) {
+                ResidentShared* other = n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane);
+                other->part[par][rank][warp] = r;
+                if (warp == 0) other->part_m[par][rank] = m;
+            }
+            tell_next();
+            meet();
+            if (warp == 0) {
+                // one lane joins the warps of a CTA, then all lanes alike join the CTAs
+                if (lane < n_cta) {
+                    float s = 0.0f, t = 0.0f, tail = 0.0f, cnt = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < kWarps; ++i) {
+                        const WarpSums p = ss.part[par][lane][i];
+                        s += p.s; t += p.t; tail += p.tail; cnt += p.cnt;
+                    }
+                    const float pm = ss.part_m[par][lane];
+                    Merged p{pm, s + fmaxf(cnt - 1.0f, 0.0f), t, tail};
+                    if (!(pm < __uint_as_float(0x7F800000u))) p.rest = p.t = p.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
+                    ss.cta[lane] = p;
+                }
+                __syncwarp();
+                Merged a = ss.cta[0];
+#pragma unroll 1
+                for (int i = 1; i < n_cta; ++i) a = join(a, ss.cta[i], c);
+                if (lane == 0) {
+                    ss.all = a;
+                    ss.log_total = log1pf(a.rest);
+                    ss.inv_total = 1.0f / (1.0f + a.rest);
+                }
+            }
+        } else {
+            copy_wait(0);
+            tell_next();
+            meet();
+            if (tid == 0) {
+                ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
+                ss.log_total = ss.inv_total = 0.0f;
+            }
+        }
+        // (the passes that read the bitmap are over)
+        if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
+        const int next_row = ss.next_row[par];
+        const bool more = next_row >= 0;
+        if (more) load_small(next_row);
+        float mass = 0.0f, rest = 0.0f, q = 0.0f;   // sum of the teacher's q, mass of its bucket, this thread's q
+        double q_sum = 0.0;
+        if (kOp == OP_DISTILL) {
+#pragma unroll
+            for (int i = 0; i < kTeacherWarps; ++i) q_sum += ss.t_sum[i];
+            const double scale = P.tail == DM_TAIL_RENORM ? (q_sum != 0.0 ? 1.0 / q_sum : 0.0) : 1.0;
+            mass = (float)(q_sum * scale);
+            // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
+            if (bucket && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - q_sum > 0.0 || q_sum != q_sum ? (float)(1.0 - q_sum) : 0.0f;
+            q = (float)(te.q * scale);
+            if (tid < P.k) { ss.t_q[par][tid] = q; ss.t_x[par][tid] = te.x; }
+        }
+        const bool repeated = kOp == OP_DISTILL && ss.t_repeated != 0;
+        __syncthreads();
+        const Merged a = ss.all;
+        const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
+        const float log_total = ss.log_total, inv_total = ss.inv_total;
+        const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
+        const bool none = zero_grad || dead;
+        const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
+                                             : distill_factors(w, mass, rest, a.tail, inv_total);
+
+        // the gradient; each batch's slots are handed to the next row at once (a thread reads its slots in
+        // program order before its copies into them are issued, and only ever touches its own)
+        const bool same_phase = phase_of(grad_row, sh.phase);
+        const Share<T> next = more ? share_of<T>(P, next_row, n_cta, rank) : sh;
+        for (int b = 0; b < n_batches; ++b) {
+            uint4 v[kUnroll];
+            uint4* slot = stash + b * kBatch + tid;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) v[u] = slot[u * kThreads];
+            if (more) next.fetch_batch(next.first + b * kBatch, slot);
+            const int j0 = sh.first + b * kBatch;
+            if (same_phase && !none && j0 >= sh.whole_lo && j0 + kBatch <= min(sh.last, sh.whole_hi)) {
+                uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase) + j0 + tid;
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) __stcs(dst + u * kThreads, grad_vector<T, kOp>(v[u], a.m, c, f));
+            } else {
+#pragma unroll 1
+                for (int u = 0; u < kUnroll; ++u) {
+                    const int j = j0 + u * kThreads + tid;
+                    const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
+                    if (j < sh.last) store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(x, a.m, c, f));
+                }
+            }
+        }
+        if (kOp == OP_GRAD) {
+            // the token's entry, by the thread that has just written its vector
+            const int at = tok >= 0 && !none ? (tok + sh.phase) / N - sh.first : -1;
+            if (at >= 0 && at < n_share && at % kThreads == tid)
+                RowVec<T>::put(grad_row + tok, token_grad(tok_x, a, c, w, g_lp, g_h, entropy, log_total, inv_total));
+        } else {
+            __syncthreads();   // the teacher's entries are written over by one thread each
+            if (te.first && !none) {                         // (set only for tokens of this share)
+                if (repeated) {
+                    q = 0.0f;
+                    for (int o = 0; o < P.k; ++o) q += ss.t_id[par][o] == te.id ? ss.t_q[par][o] : 0.0f;
+                }
+                RowVec<T>::put(grad_row + te.id, fmaf(f.top, ex2((te.x - a.m) * c), -w * q));
+            }
+            if (rank == 0 && P.out_loss != nullptr && warp == kWarps - 1) {
+                // L = sum q (log q - log p), log q = v - shift - log(sum): one warp, while the others go on
+                const float log_sum = P.tail == DM_TAIL_RENORM && q_sum > 0.0 ? logf((float)q_sum) : 0.0f;
+                float vm = neg_inf();
+                for (int i = lane; i < P.k; i += 32) vm = fmaxf(vm, ss.t_v[par][i]);
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+                const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + (double)log_sum : 0.0;
+                float loss = 0.0f;
+                for (int i = lane; i < P.k; i += 32) {
+                    const float qi = ss.t_q[par][i], x = ss.t_x[par][i];
+                    if (ss.t_id[par][i] < 0 || qi == 0.0f) continue;
+                    const double logp = dead || x == neg_inf() ? -INFINITY : ((double)x - (double)a.m) * P.inv_temp_d - (double)log_total;
+                    loss += (float)((double)qi * (((double)ss.t_v[par][i] - base) - logp));
+                }
+                loss = warp_sum(loss);
+                if (rest != 0.0f && !(dead && mass == 0.0f)) loss += rest * (logf(rest) - (logf(a.tail) - log_total));
+                if (lane == 0) P.out_loss[row] = loss;
+            }
+        }
+        sh = next;
+        row = next_row;
+    }
+}
+
+template <typename T, int kOp>
+bool launch(RowsParams P, cudaStream_t stream, int* status) {
+    constexpr int N = RowVec<T>::N;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        *status = DM_ECUDA;
+        return true;
+    }
+    const int n_vec = (P.V + 2 * N - 2) / N;          // at most, whatever the row's alignment
+    // CTAs per row: as many as run at once where rows are few, not less than one batch each; and until
+    // three shares fit an SM's shared memory
+    int cluster = 1;
+    while (cluster < kRowsMaxCluster && 2ll * P.rows * cluster <= 3ll * sms && n_vec > cluster * kBatch) cluster *= 2;
+    while (cluster < kRowsMaxCluster && (n_vec + cluster - 1) / cluster > kShareVecs) cluster *= 2;
+    const int per = (n_vec + cluster - 1) / cluster;
+    P.stash_vecs = (per + kBatch - 1) / kBatch * kBatch;
+    const size_t smem = (size_t)P.stash_vecs * 16 + (kOp == OP_DISTILL ? (size_t)P.stash_vecs : 0);
+    if (smem > kRowsSmemLimit) return false;
+    static std::atomic<unsigned long long> prepared{0};
+    *status = launch_clusters(rows_resident_kernel<T, kOp>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
+    return true;
+}
+
+}  // namespace
+
+bool launch_rows_resident(const RowsParams& P, int dtype, bool distill, cudaStream_t stream, int* status) {
+    if (dtype == DM_F32) return distill ? launch<float, OP_DISTILL>(P, stream, status) : launch<float, OP_GRAD>(P, stream, status);
+    return distill ? launch<__nv_bfloat16, OP_DISTILL>(P, stream, status) : launch<__nv_bfloat16, OP_GRAD>(P, stream, status);
+}
+
+}  // namespace dm
