@@ -370,8 +370,8 @@ rows_kernel(const RowsParams P) {
         if (use_bits && te.id >= 0) {
             const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
             if (at >= 0 && at < sh.last - sh.first) {
-                const uint32_t bit = 1u << (8 * (at & 3) + (te.id + sh.phase) % N);
-                te.first = (atomicOr(reinterpret_cast<uint32_t*>(bitmap) + (at >> 2), bit) & bit) == 0u;
+                const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
+                te.first = (atomicOr(mark_word(bitmap, at), bit) & bit) == 0u;
                 if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
             }
         }
@@ -403,13 +403,10 @@ rows_kernel(const RowsParams P) {
             uint4* ring = stash + tid;
             for (int b = 0; b < n_batches; ++b) {   // the same for the whole block; kRing batches in flight
                 uint4 v[kUnroll];
-                uint32_t bits[kUnroll];
                 copy_wait(kRing - 1);
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    v[u] = ring[u * kThreads];
-                    bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
-                }
+                for (int u = 0; u < kUnroll; ++u) v[u] = ring[u * kThreads];
+                const uint32_t marks = bucket ? reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid] : 0u;
                 sh.fetch_batch(sh.first + (b + kRing) * kBatch, ring);
                 ring = ring == stash + tid + (kRing - 1) * kBatch ? stash + tid : ring + kBatch;
                 const float lane_max = RowVec<T>::vmax(v);
@@ -423,7 +420,7 @@ rows_kernel(const RowsParams P) {
                         in_slot = 0;
                     }
                 }
-                st.add<T, kEntropy, kTail>(v, lane_max, c, bits);
+                st.add<T, kEntropy, kTail>(v, lane_max, c, marks);
             }
         }
         copy_wait(0);   // (what is still in flight are empty batches)

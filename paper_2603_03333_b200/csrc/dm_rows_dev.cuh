@@ -233,44 +233,69 @@ struct Stats {
     }
     // Entries equal to the maximum are counted and taken out of the batch.
     template <typename T, bool kTail>
-    __device__ __forceinline__ void take(uint4 (&v)[kUnroll], const uint32_t (&top_bits)[kUnroll]) {
+    __device__ __forceinline__ void take(uint4 (&v)[kUnroll], uint32_t marks) {
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const uint32_t eq = RowVec<T>::take(v[u], m);
             cnt += __popc(eq);
-            if (kTail) tail = fmaf((float)__popc(eq & ~top_bits[u]), of_maximum(), tail);
+            if (kTail) tail = fmaf((float)__popc(eq & ~(marks >> (8 * u))), of_maximum(), tail);
         }
     }
-    // A batch of entries below the maximum.
+    // A batch of entries below the maximum.  marks: the teacher's tokens in it (see mark_word); most warps
+    // see none in a batch.
     template <typename T, bool kEntropy, bool kTail>
-    __device__ __forceinline__ void sum(uint4 (&v)[kUnroll], const uint32_t (&top_bits)[kUnroll]) {
+    __device__ __forceinline__ void sum(uint4 (&v)[kUnroll], uint32_t marks) {
+        if (kTail && __any_sync(0xFFFFFFFFu, marks != 0u)) sum_marked<T>(v, marks);
+        else sum_plain<T, kEntropy, kTail>(v);
+    }
+    template <typename T, bool kEntropy, bool kTail>
+    __device__ __forceinline__ void sum_plain(uint4 (&v)[kUnroll]) {
         constexpr int N = RowVec<T>::N;
         const f32x2 c2 = pair(ce, ce), rc2 = pair(-rc, -rc);
         f32x2 bs = pair(0.0f, 0.0f), bt = bs;
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (kEntropy) RowVec<T>::raise(v[u], floor2);
-            f32x2 x[N / 2], vs = pair(0.0f, 0.0f);
+            f32x2 x[N / 2];
             RowVec<T>::pairs(v[u], x);
 #pragma unroll
             for (int n = 0; n < N / 2; ++n) {
                 f32x2 w = fma2(x[n], c2, rc2);
                 if (kEntropy && !RowVec<T>::kFloorsEntries) { w.x = fmaxf(w.x, kFloorExp); w.y = fmaxf(w.y, kFloorExp); }
                 const f32x2 e = pair(ex2(w.x), ex2(w.y));
-                if (kTail) { vs = add2(vs, e); x[n] = e; } else { bs = add2(bs, e); }
+                bs = add2(bs, e);
                 if (kEntropy) bt = fma2(e, w, bt);   // (a masked entry: 0 * a finite exponent)
             }
-            if (kTail) {
-                bs = add2(bs, vs);
-                tail += top_bits[u] == 0u ? sum2(vs) : outside<N>(x, top_bits[u]);
+        }
+        const float all = sum2(bs);
+        s += all;
+        if (kTail) tail += all;
+        if (kEntropy) t += sum2(bt);
+    }
+    template <typename T>
+    __device__ __forceinline__ void sum_marked(const uint4 (&v)[kUnroll], uint32_t marks) {
+        constexpr int N = RowVec<T>::N;
+        const f32x2 c2 = pair(ce, ce), rc2 = pair(-rc, -rc);
+        f32x2 in = pair(0.0f, 0.0f), out = in;     // the teacher's tokens, the others
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            f32x2 x[N / 2];
+            RowVec<T>::pairs(v[u], x);
+#pragma unroll
+            for (int n = 0; n < N / 2; ++n) {
+                const f32x2 w = fma2(x[n], c2, rc2), e = pair(ex2(w.x), ex2(w.y));
+                const bool lo = (marks >> (8 * u + 2 * n)) & 1u, hi = (marks >> (8 * u + 2 * n + 1)) & 1u;
+                out = add2(out, pair(lo ? 0.0f : e.x, hi ? 0.0f : e.y));
+                in = add2(in, pair(lo ? e.x : 0.0f, hi ? e.y : 0.0f));
             }
         }
-        s += sum2(bs);
-        t += sum2(bt);
+        const float rest = sum2(out);
+        s += rest + sum2(in);
+        tail += rest;
     }
     // A batch of whatever entries, with the maximum so far kept exactly.
     template <typename T, bool kEntropy, bool kTail>
-    __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, const uint32_t (&top_bits)[kUnroll]) {
+    __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, uint32_t marks) {
         float wm = lane_max;
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) wm = max_nan(wm, __shfl_xor_sync(0xFFFFFFFFu, wm, off));
@@ -289,19 +314,10 @@ struct Stats {
                     s = t = tail = 0.0f;
                 }
             }
-            take<T, kTail>(v, top_bits);
+            take<T, kTail>(v, marks);
             if (ce == 0.0f) return;
         }
-        sum<T, kEntropy, kTail>(v, top_bits);
-    }
-    template <int N> __device__ __forceinline__ static float outside(const f32x2 (&e)[N / 2], uint32_t bits) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int n = 0; n < N / 2; ++n) {
-            sum += ((bits >> (2 * n)) & 1u) ? 0.0f : e[n].x;
-            sum += ((bits >> (2 * n + 1)) & 1u) ? 0.0f : e[n].y;
-        }
-        return sum;
+        sum<T, kEntropy, kTail>(v, marks);
     }
     __device__ __forceinline__ void finish() {
         if (ce == 0.0f) return;
@@ -405,13 +421,20 @@ __device__ __forceinline__ Share<T> share_of(const RowsParams& P, int row, int n
     sh.row = static_cast<const T*>(P.logits) + (long long)row * P.ld;
     sh.V = P.V;
     sh.phase = (int)((reinterpret_cast<uintptr_t>(sh.row) & 15u) / sizeof(T));
-    const int n_vec = (sh.phase + P.V + N - 1) / N, per = (n_vec + n_cta - 1) / n_cta;
+    const int n_vec = (sh.phase + P.V + N - 1) / N, per = (n_vec + n_cta - 1) >> (__ffs(n_cta) - 1);   // (a power of two)
     sh.first = min(n_vec, rank * per);
     sh.last = min(n_vec, sh.first + per);
     sh.whole_lo = sh.phase != 0 ? 1 : 0;
     sh.whole_hi = (sh.phase + P.V) / N;
     return sh;
 }
+// Marks of a share's teacher tokens: a byte per vector, the bytes of a thread's batch in one word.
+__device__ __forceinline__ uint32_t* mark_word(unsigned char* marks, int at) {   // at: vector within the share
+    return reinterpret_cast<uint32_t*>(marks) + at / (kUnroll * kThreads) * kThreads + at % kThreads;
+}
+__device__ __forceinline__ uint32_t mark_bit(int at, int entry) { return 1u << (8 * (at / kThreads % kUnroll) + entry); }
+static_assert(kUnroll == 4, "the marks of a batch fill a word");
+
 template <typename T>
 __device__ __forceinline__ bool phase_of(const T* p, int phase) {
     return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)) == phase;

@@ -136,8 +136,8 @@ rows_resident_kernel(const RowsParams P) {
             if (te.id >= 0) {
                 const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
                 if (at >= 0 && at < n_share) {
-                    const uint32_t bit = 1u << (8 * (at & 3) + (te.id + sh.phase) % N);
-                    my_word = reinterpret_cast<uint32_t*>(bitmap) + (at >> 2);
+                    const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
+                    my_word = mark_word(bitmap, at);
                     te.first = (atomicOr(my_word, bit) & bit) == 0u;
                     if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
                 }
@@ -208,14 +208,11 @@ rows_resident_kernel(const RowsParams P) {
             const bool holder = __any_sync(0xFFFFFFFFu, thread_max == m && m != neg_inf());
             for (int b = 0; b < n_batches && (holder || st.ce != 0.0f); ++b) {
                 uint4 v[kUnroll];
-                uint32_t bits[kUnroll];
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    v[u] = stash[b * kBatch + u * kThreads + tid];
-                    bits[u] = bucket ? bitmap[b * kBatch + u * kThreads + tid] : 0u;
-                }
-                if (holder) st.take<T, kTail>(v, bits);
-                if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, bits);
+                for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
+                const uint32_t marks = bucket ? reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid] : 0u;
+                if (holder) st.take<T, kTail>(v, marks);
+                if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, marks);
             }
             st.finish();
             WarpSums r{warp_sum(st.s), kEntropy ? warp_sum(st.t) : 0.0f, kTail ? warp_sum(st.tail) : 0.0f, warp_sum((float)st.cnt)};
@@ -291,24 +288,38 @@ rows_resident_kernel(const RowsParams P) {
         // program order before its copies into them are issued, and only ever touches its own)
         const bool same_phase = phase_of(grad_row, sh.phase);
         const Share<T> next = more ? share_of<T>(P, next_row, n_cta, rank) : sh;
-        for (int b = 0; b < n_batches; ++b) {
-            uint4 v[kUnroll];
-            uint4* slot = stash + b * kBatch + tid;
+        const int whole_end = min(sh.last, sh.whole_hi);
+        if (same_phase && !none) {
+            uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase);
+            for (int b = 0; b < n_batches; ++b) {
+                uint4 v[kUnroll];
+                uint4* slot = stash + b * kBatch + tid;
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) v[u] = slot[u * kThreads];
-            if (more) next.fetch_batch(next.first + b * kBatch, slot);
-            const int j0 = sh.first + b * kBatch;
-            if (same_phase && !none && j0 >= sh.whole_lo && j0 + kBatch <= min(sh.last, sh.whole_hi)) {
-                uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase) + j0 + tid;
+                for (int u = 0; u < kUnroll; ++u) v[u] = slot[u * kThreads];
+                if (more) next.fetch_batch(next.first + b * kBatch, slot);
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) __stcs(dst + u * kThreads, grad_vector<T, kOp>(v[u], a.m, c, f));
-            } else {
+                for (int u = 0; u < kUnroll; ++u) {
+                    const int j = sh.first + b * kBatch + u * kThreads + tid;
+                    v[u] = grad_vector<T, kOp>(v[u], a.m, c, f);
+                    if (j >= sh.whole_lo && j < whole_end) __stcs(dst + j, v[u]);
+                }
+            }
+            // the row's first and last vector, where it shares them with its neighbours: read again
+            const int edge = sh.first + tid < sh.whole_lo ? sh.first + tid
+                             : sh.last > sh.whole_hi && (sh.last - 1 - sh.first) % kThreads == tid ? sh.last - 1 : -1;
+            if (edge >= 0) store_vector(grad_row, sh, edge, true, grad_vector<T, kOp>(sh.load(edge), a.m, c, f));
+            if (edge >= 0 && edge < sh.whole_lo && sh.last > sh.whole_hi && sh.last - 1 != edge && (sh.last - 1 - sh.first) % kThreads == tid)
+                store_vector(grad_row, sh, sh.last - 1, true, grad_vector<T, kOp>(sh.load(sh.last - 1), a.m, c, f));
+        } else {
+            for (int b = 0; b < n_batches; ++b) {
+                uint4* slot = stash + b * kBatch + tid;
 #pragma unroll 1
                 for (int u = 0; u < kUnroll; ++u) {
-                    const int j = j0 + u * kThreads + tid;
-                    const uint4 x = u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3];
-                    if (j < sh.last) store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(x, a.m, c, f));
+                    const int j = sh.first + b * kBatch + u * kThreads + tid;
+                    if (j < sh.last)
+                        store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(slot[u * kThreads], a.m, c, f));
                 }
+                if (more) next.fetch_batch(next.first + b * kBatch, slot);
             }
         }
         if (kOp == OP_GRAD) {
