@@ -44,10 +44,9 @@ struct RowsShared {
     unsigned int scan[kWarps];
     // teacher (distill): warps 0..3 hold its entries, one per thread
     int t_id[kRowsMaxTop];
-    float t_q[kRowsMaxTop];
+    float t_q[kRowsMaxTop], t_v[kRowsMaxTop], t_x[kRowsMaxTop];
     float t_max[kRowsMaxTop / 32];
     double t_sum[kRowsMaxTop / 32];
-    float t_loss[kRowsMaxTop / 32];
     int t_distinct, t_repeated;
 };
 
@@ -501,32 +500,11 @@ rows_kernel(const RowsParams P) {
         mass = (float)(sum * scale);
         // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
         if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
-        if (warp < kRowsMaxTop / 32) {
-            const float q = (float)(te.q * scale);
-            if (tid < P.k) ss.t_q[tid] = q;
-            if (rank == 0 && P.out_loss != nullptr) {
-                // log q = v - shift - log(sum): no logarithm per entry
-                float vm = ss.t_max[0];
-#pragma unroll
-                for (int i = 1; i < kRowsMaxTop / 32; ++i) vm = fmaxf(vm, ss.t_max[i]);
-                const float log_sum = P.tail == DM_TAIL_RENORM && sum > 0.0 ? logf((float)sum) : 0.0f;
-                const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + (double)log_sum : 0.0;
-                float term = 0.0f;
-                if (te.id >= 0 && !(q == 0.0f)) {
-                    const double logp = dead || te.x == neg_inf() ? -INFINITY : ((double)te.x - (double)a.m) * P.inv_temp_d - (double)log_total;
-                    term = (float)((double)q * (((double)te.v - base) - logp));
-                }
-                term = warp_sum(term);
-                if (lane == 0) ss.t_loss[warp] = term;
-            }
-        }
+        if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
         __syncthreads();
-        if (rank == 0 && tid == 0 && P.out_loss != nullptr) {
-            float loss = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kRowsMaxTop / 32; ++i) loss += ss.t_loss[i];
-            if (rest != 0.0f && !(dead && mass == 0.0f)) loss += rest * (logf(rest) - (logf(a.tail) - log_total));
-            P.out_loss[row] = loss;
+        if (rank == 0 && warp == kWarps - 1 && P.out_loss != nullptr) {
+            const float loss = teacher_loss(P, a, ss.t_id, ss.t_v, ss.t_x, ss.t_q, sum, sum * scale, rest != 0.0f ? 1.0 - sum : 0.0);
+            if (lane == 0) P.out_loss[row] = loss;
         }
     }
 

@@ -359,6 +359,31 @@ __device__ __forceinline__ float warp_sum(float x) {
 // precision as a difference) and tells entries that name the same token apart.
 struct TeacherEntry { int id; float v, x; bool first; double q; };
 
+// The loss of a row, by one warp.  fp64: it is a small difference of logarithms that are not small, and
+// there are only k of them.  mass, rest: of the teacher's tokens and of its bucket (0: no bucket).
+__device__ __forceinline__ float teacher_loss(const RowsParams& P, const Merged& a, const int* id, const float* v, const float* x,
+                                              const float* q, double q_sum, double mass, double rest) {
+    const int lane = threadIdx.x & 31;
+    const bool dead = a.m == neg_inf();
+    const double log_total = log1p((double)a.rest);
+    float vm = neg_inf();
+    for (int i = lane; i < P.k; i += 32) vm = fmaxf(vm, id[i] >= 0 ? v[i] : neg_inf());
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+    // log q = v - base: the teacher's normaliser
+    const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + log(q_sum) : 0.0;
+    double loss = 0.0;
+    for (int i = lane; i < P.k; i += 32) {
+        if (id[i] < 0 || q[i] == 0.0f) continue;
+        const double logp = dead || x[i] == neg_inf() ? -INFINITY : ((double)x[i] - (double)a.m) * P.inv_temp_d - log_total;
+        loss += (double)q[i] * (((double)v[i] - base) - logp);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, off);
+    if (rest != 0.0 && !(dead && mass == 0.0)) loss += rest * (log(rest) - (log((double)a.tail) - log_total));
+    return (float)loss;
+}
+
 // Factors of a gradient, from the row's statistics: with w = (x - m) c in powers of two, every entry's
 // gradient is 2^w (A + B w) (logprobs) or 2^w A (distill, where the teacher's tokens differ: top).
 struct GradFactors { float A, B, top; };

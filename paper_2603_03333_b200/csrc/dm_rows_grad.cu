@@ -337,22 +337,10 @@ rows_resident_kernel(const RowsParams P) {
                 RowVec<T>::put(grad_row + te.id, fmaf(f.top, ex2((te.x - a.m) * c), -w * q));
             }
             if (rank == 0 && P.out_loss != nullptr && warp == kWarps - 1) {
-                // L = sum q (log q - log p), log q = v - shift - log(sum): one warp, while the others go on
-                const float log_sum = P.tail == DM_TAIL_RENORM && q_sum > 0.0 ? logf((float)q_sum) : 0.0f;
-                float vm = neg_inf();
-                for (int i = lane; i < P.k; i += 32) vm = fmaxf(vm, ss.t_v[par][i]);
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
-                const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + (double)log_sum : 0.0;
-                float loss = 0.0f;
-                for (int i = lane; i < P.k; i += 32) {
-                    const float qi = ss.t_q[par][i], x = ss.t_x[par][i];
-                    if (ss.t_id[par][i] < 0 || qi == 0.0f) continue;
-                    const double logp = dead || x == neg_inf() ? -INFINITY : ((double)x - (double)a.m) * P.inv_temp_d - (double)log_total;
-                    loss += (float)((double)qi * (((double)ss.t_v[par][i] - base) - logp));
-                }
-                loss = warp_sum(loss);
-                if (rest != 0.0f && !(dead && mass == 0.0f)) loss += rest * (logf(rest) - (logf(a.tail) - log_total));
+                // one warp, while the others go on
+                const double scale = P.tail == DM_TAIL_RENORM ? (q_sum != 0.0 ? 1.0 / q_sum : 0.0) : 1.0;
+                const float loss = teacher_loss(P, a, ss.t_id[par], ss.t_v[par], ss.t_x[par], ss.t_q[par], q_sum, q_sum * scale,
+                                                rest != 0.0f ? 1.0 - q_sum : 0.0);
                 if (lane == 0) P.out_loss[row] = loss;
             }
         }

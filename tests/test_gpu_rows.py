@@ -404,3 +404,108 @@ def test_refusals(ctx):
     with pytest.raises(TypeError):
         ctx.logprobs_grad(x, tok, torch.ones(4, device=DEV), out=torch.empty((4, 100), dtype=torch.bfloat16, device=DEV))
     assert ctx.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 500_003), (torch.bfloat16, 1_000_001), (torch.float32, 2_300_001)],
+                         ids=["f32", "bf16", "f32_long"])
+def test_rows_too_long_for_shared_memory(ctx, dtype, V):
+    """Gradients of rows that are read twice, and the top entries of rows of many batches."""
+    x, g = make(2, V, dtype)
+    tok = tokens_for(2, V, g)
+    check_logprobs(ctx, x, tok, 40, 1.0)
+    g_lp, g_h = torch.randn(2, generator=g, device=DEV), torch.randn(2, generator=g, device=DEV)
+    got = check_grad(ctx, x, tok, g_lp, g_h, 1.0)
+    ids, v = teacher_for(x, 50, g, 1.0)
+    both = check_distill(ctx, x, ids, v, binding.TAIL_BUCKET, 1.0)
+    check_distill(ctx, x, ids, v, binding.TAIL_RENORM, 1.0)
+    assert torch.equal(ctx.logprobs_grad(x.clone(), tok, g_lp, g_h), got)
+    y = x.clone()
+    assert torch.equal(ctx.distill(y, ids, v, tail=binding.TAIL_BUCKET, grad=True, out=y)["grad"], both["grad"])
+
+
+def test_distill_refuses_rows_whose_marks_do_not_fit(ctx):
+    x = torch.zeros((1, 13_000_000), dtype=torch.bfloat16, device=DEV)
+    ids, v = torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.zeros((1, 1), device=DEV)
+    with pytest.raises(pk.DropMatchError) as e:
+        ctx.distill(x, ids, v, tail=binding.TAIL_BUCKET, grad=True)
+    assert e.value.status == binding.EUNSUPPORTED
+    assert abs(float(ctx.distill(x, ids, v)["loss"]) - 16.3805) < 1e-3      # log V: nothing to mark
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(5000, 67), (3001, 2049), (700, 40001)])
+def test_many_rows_shared_out_between_clusters(ctx, dtype, rows, V):
+    """Every row gets its gradient exactly once, whichever cluster takes it, with zero rows in between."""
+    x, g = make(rows, V, dtype, ld=V + 1)
+    tok = tokens_for(rows, V, g)
+    g_lp, g_h = torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV)
+    g_lp[::7] = 0.0
+    g_h[::7] = 0.0
+    check_grad(ctx, x, tok, g_lp, g_h, 1.0)
+    ids, v = teacher_for(x, 9, g, 1.0)
+    w = torch.rand(rows, generator=g, device=DEV)
+    w[::5] = 0.0
+    check_distill(ctx, x, ids, v, binding.TAIL_BUCKET, 1.0, w)
+    check_distill(ctx, x, ids, v, binding.TAIL_RENORM, 1.0, w, loss=False)
+    assert ctx.device_error() == 0
+
+
+def test_two_calls_at_once(ctx):
+    """Calls of one context on two streams share nothing."""
+    x, g = make(300, 32003, torch.bfloat16)
+    y, _ = make(200, 50001, torch.float32, seed=1)
+    ids, v = teacher_for(x, 16, g, 1.0)
+    jds, u = teacher_for(y, 16, g, 1.0)
+    a, b = ctx.distill(x, ids, v, tail=1, grad=True), ctx.distill(y, jds, u, tail=1, grad=True)
+    p, q = ctx.logprobs(x, None, n_top=9), ctx.logprobs(y, None, n_top=9)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    out = []
+    for _ in range(5):
+        with torch.cuda.stream(streams[0]):
+            out.append((ctx.distill(x, ids, v, tail=1, grad=True), a))
+            out.append((ctx.logprobs(x, None, n_top=9), p))
+        with torch.cuda.stream(streams[1]):
+            out.append((ctx.distill(y, jds, u, tail=1, grad=True), b))
+            out.append((ctx.logprobs(y, None, n_top=9), q))
+    torch.cuda.synchronize()
+    for got, want in out:
+        for key in want:
+            assert torch.equal(got[key], want[key]), key
+
+
+def test_teacher_to_student(ctx):
+    """The operators together, as a draft head is trained: the target scores the hidden rows of a text, the
+    draft's logits are pulled towards its top tokens, and the draft's log-probabilities are looked at."""
+    V, d, rows, k = 4000, 128, 96, 32
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    target = (torch.randn((V, d), generator=g, device=DEV) * 0.3).to(torch.bfloat16)
+    H = torch.randn((rows, d), generator=g, device=DEV).to(torch.bfloat16)
+    c = pk.Context(0)
+    try:
+        c.set_head(target, max_rows=rows)
+        c.enable_score(rows, k)
+        T = 1.5
+        teach = c.score(H, None, n_top=k, temperature=T)
+        W = (torch.randn((V, d), generator=g, device=DEV) * 0.02).requires_grad_(True)
+        hidden = H.float()
+        weight = torch.full((rows,), 1.0 / rows, device=DEV)
+        for _ in range(3):
+            logits = hidden @ W.T
+            res = c.distill(logits.detach(), teach["top_ids"], teach["top_logprob"], tail=binding.TAIL_BUCKET,
+                            temperature=T, weight=weight, grad=True)
+            want, want_g = ref.distill(logits.detach(), teach["top_ids"], teach["top_logprob"], True, T, weight)
+            ref.same(res["loss"], want, 1e-4 * want.abs() + 1e-5)
+            W.grad = None
+            logits.backward(res["grad"])
+            # the weight's gradient is the 64-bit one's
+            exact = want_g.T @ hidden.double()
+            assert float((W.grad.double() - exact).norm() / exact.norm()) < 1e-4
+            with torch.no_grad():
+                given = c.logprobs(logits, teach["top_ids"][:, 0].contiguous())
+                check_logprobs(c, logits.detach(), teach["top_ids"][:, 0].contiguous(), 0, 1.0)
+                assert given["logprob"].shape == (rows,)
+                W -= 2.0 * W.grad
+    finally:
+        c.close()

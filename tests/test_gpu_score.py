@@ -167,3 +167,58 @@ def test_score_refusals_and_the_wait_limit():
             assert torch.equal(good[key], again[key])
     finally:
         ctx.close()
+
+
+def test_score_on_the_cuda_cores_and_without_early_start():
+    """The kernel families agree on one head; switching programmatic stream serialization off changes nothing."""
+    W, H = inputs(70, 20011, 192, torch.bfloat16)
+    tok = torch.randint(0, 20011, (70,), device=DEV, dtype=torch.int32)
+    ctx = pk.Context(0)
+    try:
+        ctx.set_head(W, max_rows=70)
+        ctx.enable_score(70, 6)
+        a = ctx.score(H, tok, n_top=6)
+        assert ctx.last_impl() == binding.IMPL_TCGEN05 and ctx.last_launches() == 2
+        ctx.set_pdl(False)
+        b = ctx.score(H, tok, n_top=6)
+        for key in a:
+            assert torch.equal(a[key], b[key]), key
+        ctx.set_impl(binding.IMPL_SIMT)
+        c = ctx.score(H, tok, n_top=6)
+        assert ctx.last_impl() == binding.IMPL_SIMT
+        check(c, W, H, tok, 6, 1.0)
+        ctx.set_impl(binding.IMPL_AUTO)
+        ctx.enable_score(70, 0)                 # no alternatives: no room for the CUDA-core kernel's logits
+        few = ctx.score(H, tok)
+        for key in few:
+            assert torch.equal(a[key], few[key]), key
+        ctx.set_impl(binding.IMPL_SIMT)
+        with pytest.raises(pk.DropMatchError) as e:
+            ctx.score(H, tok)
+        assert e.value.status == binding.EWORKSPACE
+        ctx.enable_score(70, 0)                 # ... unless it is the family in force
+        check(ctx.score(H, tok), W, H, tok, 0, 1.0)
+    finally:
+        ctx.close()
+
+
+def test_score_workspace_is_counted_and_replaced():
+    W, H = inputs(300, 9000, 64, torch.bfloat16)
+    ctx = pk.Context(0)
+    try:
+        ctx.set_head(W, max_rows=300)
+        base = ctx.workspace_bytes()
+        ctx.enable_score(300, 8)
+        one = ctx.workspace_bytes()
+        assert one > base
+        ctx.enable_score(300, 8)
+        assert ctx.workspace_bytes() == one
+        ctx.enable_score(10, 0)
+        assert base < ctx.workspace_bytes() < one
+        check(ctx.score(H[:10], None), W, H[:10], None, 0, 1.0)
+        ctx.set_head(W, max_rows=300)           # drops it
+        with pytest.raises(pk.DropMatchError) as e:
+            ctx.score(H[:1])
+        assert e.value.status == binding.EWORKSPACE
+    finally:
+        ctx.close()
