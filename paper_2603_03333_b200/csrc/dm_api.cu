@@ -776,7 +776,7 @@ int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows,
             st = launch_simt(c->head, Hc, rows, map, mk, &n_slices, c->partials, logits, c->err, s);
             if (st != DM_OK) return st;
             part.logits = logits;
-            part.err = c->err;
+            part.err = part.err_out = c->err;
             st = launch_rows_logprobs(part, DM_F32, s);
         }
         if (st != DM_OK) return st;
@@ -802,6 +802,7 @@ int dropmatch_logprobs(dm_ctx* c, const void* logits, int dtype, int64_t ld, int
     if (!g.ok) return DM_ECUDA;
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
+    rp.err_out = c->err;
     return launch_rows_logprobs(rp, dtype, static_cast<cudaStream_t>(stream));
 }
 

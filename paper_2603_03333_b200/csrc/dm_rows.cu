@@ -19,6 +19,7 @@
 
 #include <atomic>
 
+#include "dm_ptx.cuh"
 #include "dm_rows_dev.cuh"
 
 namespace dm {
@@ -30,10 +31,14 @@ using namespace rows;
 
 constexpr int kRing = 2;               // batches in flight
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
-constexpr int kHitCap = 2048;          // batches that hold them
-constexpr int kMaxSlots = 16;          // maxima a thread keeps of its batches (for finding the top entries again)
+constexpr int kHitCap = 1024;          // batches that hold them
+constexpr int kMaxSlots = 16, kWalkSlots = 8;   // maxima a thread keeps of its batches (for finding the top entries again)
+constexpr long long kWaitLimitCycles = 2000000000ll;   // about one second
 
 struct RowsShared {
+    uint4 answer;                // to the request for another row
+    uint64_t answer_bar;
+    int abort, next_row;
     float w_m[kWarps], w_s[kWarps], w_t[kWarps], w_tail[kWarps];
     int w_cnt[kWarps];
     Merged part[kRowsMaxCluster];   // every CTA's statistics, each written by its CTA
@@ -300,9 +305,13 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
 // ------------------------------------------------------------------------------------ the kernel
 // Gradients are written by a second pass that reads the row again (rows whose shares fit in shared
 // memory take the kernel of dm_rows_grad.cu instead).
-template <typename T, int kOp>
+// kWalk (logprobs, rows of one CTA): there is a CTA per row in the grid; a running one takes over rows of
+// CTAs that have not started, so that the first batches of its next row are on their way while the
+// present one's entries are selected.
+template <typename T, int kOp, bool kWalk>
 __global__ void __launch_bounds__(kThreads, 4)
 rows_kernel(const RowsParams P) {
+    static_assert(!kWalk || kOp == OP_LOGPROBS, "only rows without a gradient are walked over");
     constexpr int N = RowVec<T>::N;
     constexpr bool kEntropy = kOp != OP_DISTILL, kTail = kOp == OP_DISTILL;
     constexpr int kBatch = kUnroll * kThreads;
@@ -314,22 +323,39 @@ rows_kernel(const RowsParams P) {
     uint4* stash = reinterpret_cast<uint4*>(smem);                                      // [stash_vecs], vector first + x
     unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);     // distill: teacher tokens of the share, a byte per vector
     // logprobs: behind the ring what is kept while the row streams, in the ring's place what comes after
+    // (behind it, too, where the ring is busy with the next row by then)
     unsigned long long* merged = reinterpret_cast<unsigned long long*>(stash + kRing * kBatch);   // rank 0: every CTA's sorted list
     uint32_t* slots = reinterpret_cast<uint32_t*>(merged + (n_cta > 1 ? n_cta * P.n_top : 0));    // maxima of the threads' batches
-    unsigned long long* cand = reinterpret_cast<unsigned long long*>(smem);             // candidates
+    unsigned long long* cand = kWalk ? reinterpret_cast<unsigned long long*>(slots + P.n_slots * kThreads)
+                                     : reinterpret_cast<unsigned long long*>(smem);     // candidates
     unsigned long long* sorted = cand + kCandCap;                                       // the largest of the share, sorted
     int* hits = reinterpret_cast<int*>(sorted + kRowsMaxTop);                           // [kHitCap]
 
-    const int row = (int)(blockIdx.x / (unsigned)n_cta), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int row = (int)(blockIdx.x / (unsigned)n_cta);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const float c = P.c;
 
-    const Share<T> sh = share_of<T>(P, row, n_cta, rank);
+    Share<T> sh = share_of<T>(P, row, n_cta, rank);
     T* grad_row = kOp != OP_LOGPROBS && P.out_grad != nullptr ? static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad : nullptr;
 
-    const int n_share = sh.last - sh.first, n_batches = (n_share + kBatch - 1) / kBatch;
+    const int n_share = sh.last - sh.first, n_batches = kWalk ? P.n_batches : (n_share + kBatch - 1) / kBatch;
+    uint4* ring = stash + tid;
+    const uint32_t answer = ptx::smem_u32(&ss.answer), answer_bar = ptx::smem_u32(&ss.answer_bar);
+    if (kWalk && tid == 0) {
+        ptx::mbar_init(answer_bar, 1);
+        ss.abort = 0;
+        ptx::fence_mbar_init();
+        ptx::fence_proxy_async_smem();
+    }
     // on its way before anything else is looked at: the first batches
     for (int b = 0; b < kRing; ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
 
+    for (uint32_t parity = 0;; parity ^= 1u) {
+    if (kWalk && tid == 0) {
+        ptx::mbar_arrive_expect_tx(answer_bar, 16);
+        ptx::request_next_cluster(answer, answer_bar);
+    }
+    int next_row = -1;
     float w = P.inv_temp;   // factor of the gradient
     int tok = -1;
     float tok_x = neg_inf();
@@ -399,14 +425,30 @@ rows_kernel(const RowsParams P) {
             uint32_t* slot = slots + tid;
             uint32_t slot_key = 0u;
             int in_slot = 0;
-            uint4* ring = stash + tid;
+            Share<T> from = sh;                        // what is fetched: this row, at its end the next one
+            int ahead = kRing;
             for (int b = 0; b < n_batches; ++b) {   // the same for the whole block; kRing batches in flight
                 uint4 v[kUnroll];
                 copy_wait(kRing - 1);
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) v[u] = ring[u * kThreads];
                 const uint32_t marks = bucket ? reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid] : 0u;
-                sh.fetch_batch(sh.first + (b + kRing) * kBatch, ring);
+                if (kWalk && b == n_batches - kRing) {
+                    if (tid == 0) {
+                        int next = -1;
+                        if (ptx::mbar_wait<32>(answer_bar, parity, &ss.abort, kWaitLimitCycles)) {
+                            next = ptx::granted_cluster(answer);
+                            ptx::fence_proxy_async_smem();   // read before the next request writes it
+                        } else {
+                            atomicCAS(P.err_out, 0u, (uint32_t)ERR_WAIT_ROW);
+                        }
+                        ss.next_row = next;
+                    }
+                    __syncthreads();
+                    next_row = ss.next_row;
+                    if (next_row >= 0) { from = share_of<T>(P, next_row, 1, 0); ahead = kRing - n_batches; }
+                }
+                from.fetch_batch(from.first + (b + ahead) * kBatch, ring);   // (past the end of a share: masked entries)
                 ring = ring == stash + tid + (kRing - 1) * kBatch ? stash + tid : ring + kBatch;
                 const float lane_max = RowVec<T>::vmax(v);
                 if (kOp == OP_LOGPROBS && P.n_top > 0) {
@@ -422,7 +464,7 @@ rows_kernel(const RowsParams P) {
                 st.add<T, kEntropy, kTail>(v, lane_max, c, marks);
             }
         }
-        copy_wait(0);   // (what is still in flight are empty batches)
+        if (!kWalk) copy_wait(0);   // (what is still in flight are empty batches)
         if (n_cta > 1) cluster_wait();
         block_merge(st, c, ss, cluster, n_cta, rank);
         if (kOp == OP_LOGPROBS && P.n_top > 0) {
@@ -533,6 +575,10 @@ rows_kernel(const RowsParams P) {
             }
         }
     }
+    if (!kWalk || next_row < 0) break;
+    row = next_row;
+    sh = share_of<T>(P, row, n_cta, rank);
+    }
 }
 
 template <typename T, int kOp>
@@ -549,23 +595,31 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
     int cluster = 1;
     while (cluster < kRowsMaxCluster && 2ll * P.rows * cluster <= 4ll * sms && n_vec > cluster * kBatch) cluster *= 2;
     size_t smem = 0;
+    bool walk = false;
     for (;; cluster *= 2) {
         const int per = (n_vec + cluster - 1) / cluster, batches = (per + kBatch - 1) / kBatch;
         P.stash_vecs = kRing * kBatch;
+        P.n_batches = batches;
+        walk = kOp == OP_LOGPROBS && cluster == 1 && batches >= kRing && P.rows > 4 * sms;
         smem = (size_t)P.stash_vecs * 16;
         if (kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || P.out_grad != nullptr)) smem += (size_t)batches * kBatch;
         if (kOp == OP_LOGPROBS && P.n_top > 0) {
-            P.slot_batches = (batches + kMaxSlots - 1) / kMaxSlots;
-            const int n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
-            smem += (size_t)n_slots * kThreads * sizeof(uint32_t);
+            const int most = walk ? kWalkSlots : kMaxSlots;
+            P.slot_batches = (batches + most - 1) / most;
+            P.n_slots = (batches + P.slot_batches - 1) / P.slot_batches;
+            smem += (size_t)P.n_slots * kThreads * sizeof(uint32_t);
             if (cluster > 1) smem += (size_t)cluster * P.n_top * sizeof(unsigned long long);
-            static_assert((kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + kHitCap * sizeof(int) <= (size_t)kRing * kBatch * 16, "the lists fit the ring");
+            constexpr size_t lists = (kCandCap + kRowsMaxTop) * sizeof(unsigned long long) + kHitCap * sizeof(int);
+            static_assert(lists <= (size_t)kRing * kBatch * 16, "the lists fit the ring");
+            if (walk) smem += lists;
         }
         if (smem <= kRowsSmemLimit) break;
         if (cluster >= kRowsMaxCluster) return DM_EUNSUPPORTED;
     }
-    static std::atomic<unsigned long long> prepared{0};
-    return launch_clusters(rows_kernel<T, kOp>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
+    static std::atomic<unsigned long long> prepared{0}, prepared_walk{0};
+    if (walk)
+        return launch_clusters(rows_kernel<T, kOp, kOp == OP_LOGPROBS>, prepared_walk, dev, P, (long long)P.rows, 1, smem, stream);
+    return launch_clusters(rows_kernel<T, kOp, false>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
 }
 
 }  // namespace

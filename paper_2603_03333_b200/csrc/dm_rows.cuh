@@ -16,9 +16,10 @@ struct RowsParams {
     float c;              // log2(e) / T
     double inv_temp_d;
     int stash_vecs;       // 16-byte vectors in shared memory: a CTA's share, or the ring it streams through (set by the launch)
-    int slot_batches;     // batches of a thread that share one remembered maximum (set by the launch)
+    int n_batches;        // batches of the longest share (set by the launch)
+    int slot_batches, n_slots;   // batches of a thread that share one remembered maximum, and how many of those (set by the launch)
     const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
-    uint32_t* err_out;    // device error word of the call's context (gradient kernels)
+    uint32_t* err_out;    // device error word of the call's context
     // logprobs
     const int32_t* tokens;
     int n_top;
