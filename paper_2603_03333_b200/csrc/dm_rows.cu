@@ -362,7 +362,7 @@ rows_kernel(const RowsParams P) {
     if (kOp != OP_DISTILL && P.tokens != nullptr) {
         tok = P.tokens[row];
         if (tok < 0 || tok >= P.V) tok = -1;
-        if (tok >= 0) tok_x = RowVec<T>::get(sh.row + tok);
+        if (tok >= 0) tok_x = RowVec<T>::get_early(sh.row + tok);
     }
     float g_lp = 0.0f, g_h = 0.0f;
     bool zero_grad = false;
@@ -379,7 +379,7 @@ rows_kernel(const RowsParams P) {
             te.id = P.t_ids[(long long)row * P.k + tid];
             te.v = P.t_logprob[(long long)row * P.k + tid];
             if (te.id < 0 || te.id >= P.V) te.id = -1;
-            if (te.id >= 0) te.x = RowVec<T>::get(sh.row + te.id);
+            if (te.id >= 0) te.x = RowVec<T>::get_early(sh.row + te.id);
             ss.t_id[tid] = te.id;
         }
         if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }

@@ -79,6 +79,12 @@ template <> struct RowVec<float> {
         return eq;
     }
     __device__ static float get(const float* p) { return *p; }
+    // ... issued here and now, though the value is needed only at the end of the row
+    __device__ static float get_early(const float* p) {
+        float x;
+        asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p));
+        return x;
+    }
     __device__ static void put(float* p, float x) { *p = x; }
 };
 template <> struct RowVec<__nv_bfloat16> {
@@ -151,6 +157,11 @@ template <> struct RowVec<__nv_bfloat16> {
     }
     __device__ static float get(const __nv_bfloat16* p) {
         return __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16);
+    }
+    __device__ static float get_early(const __nv_bfloat16* p) {
+        unsigned short x;
+        asm volatile("ld.global.u16 %0, [%1];" : "=h"(x) : "l"(p));
+        return __uint_as_float((uint32_t)x << 16);
     }
     __device__ static void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };

@@ -109,7 +109,7 @@ rows_resident_kernel(const RowsParams P) {
         bool zero_grad;
         TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
         if (kOp == OP_GRAD) {
-            if (next_id >= 0 && next_id < P.V) { tok = next_id; tok_x = RowVec<T>::get(sh.row + tok); g_lp = next_a; }
+            if (next_id >= 0 && next_id < P.V) { tok = next_id; tok_x = RowVec<T>::get_early(sh.row + tok); g_lp = next_a; }
             g_h = next_b;
             zero_grad = g_lp == 0.0f && g_h == 0.0f;
         } else {
@@ -118,7 +118,7 @@ rows_resident_kernel(const RowsParams P) {
             if (tid < P.k && next_id >= 0 && next_id < P.V) {
                 te.id = next_id;
                 te.v = next_a;
-                te.x = RowVec<T>::get(sh.row + te.id);
+                te.x = RowVec<T>::get_early(sh.row + te.id);
             }
             if (tid < P.k) { ss.t_id[par][tid] = te.id; ss.t_v[par][tid] = te.v; }
             if (tid == 0) ss.t_distinct = ss.t_repeated = 0;
