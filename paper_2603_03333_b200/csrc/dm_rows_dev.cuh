@@ -312,7 +312,7 @@ struct Stats {
         for (int off = 16; off > 0; off >>= 1) wm = max_nan(wm, __shfl_xor_sync(0xFFFFFFFFu, wm, off));
         if (!(wm < m && ce != 0.0f)) {
             if (wm == neg_inf()) return;   // nothing but masked entries so far
-            if (!(wm <= m)) {              // a new maximum: the old one becomes an entry like the others
+            if (m == m && !(wm <= m)) {    // a new maximum (a NaN stays one): the old one becomes an entry like the others
                 const Stats old = *this;
                 set_maximum<T>(wm, c);
                 if (old.ce != 0.0f && ce != 0.0f) {

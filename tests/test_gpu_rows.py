@@ -509,3 +509,69 @@ def test_teacher_to_student(ctx):
                 W -= 2.0 * W.grad
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [8200, 16391])
+def test_many_rows_of_every_kind(ctx, dtype, V):
+    """A run of rows long enough that CTAs take over rows of others, with rows in between that leave the
+    usual path: masked, of equal entries (more than a list of candidates takes), NaN, one entry only."""
+    rows = 1500
+    x, g = make(rows, V, dtype, ld=V + 3)
+    x[5::11] = NINF
+    x[6::11] = 1.5
+    x[7::11, 1:] = NINF
+    x[8::11, ::2] = torch.finfo(dtype).min
+    x[9::11, 100:] = NINF
+    tok = tokens_for(rows, V, g)
+    check_logprobs(ctx, x, tok, 5, 0.8)
+    check_logprobs(ctx, x, tok, 100, 1.0)
+    x[10::11, V // 2] = float("nan")
+    got = check_logprobs(ctx, x, None, 0, 1.0)
+    assert torch.isnan(got["lse"][10::11]).all() and not torch.isnan(got["lse"][9::11]).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1001, 30011])
+def test_many_rows_in_place(ctx, dtype, V):
+    """The next row is on its way while a row's gradient takes the place of its logits."""
+    rows = 1200
+    x, g = make(rows, V, dtype, ld=V + 2)
+    tok = tokens_for(rows, V, g)
+    g_lp, g_h = torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV)
+    g_lp[::6] = 0.0
+    g_h[::6] = 0.0
+    ids, v = teacher_for(x, 33, g, 1.0)
+    ids[:, 20] = ids[:, 3]                               # a token that is named twice
+    w = torch.rand(rows, generator=g, device=DEV)
+    w[::4] = 0.0
+    x[::12] = float("nan")                               # padded rows: both factors 0, weight 0
+    for call in (lambda at, out: ctx.logprobs_grad(at, tok, g_lp, g_h, out=out),
+                 lambda at, out: ctx.distill(at, ids, v, tail=binding.TAIL_BUCKET, weight=w, grad=True, out=out)["grad"],
+                 lambda at, out: ctx.distill(at, ids, v, weight=w, loss=False, grad=True, out=out)["grad"]):
+        want = call(x, None)
+        assert not torch.isnan(want).any() and (want[::12] == 0).all()
+        whole = torch.as_strided(x, (rows, V + 2), (V + 2, 1), x.storage_offset()).clone()
+        call(whole[:, :V], whole[:, :V])
+        assert torch.equal(whole[:, :V], want) and (whole[:-1, V:] == 77.0).all()
+    assert ctx.device_error() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=["nan", "inf"])
+def test_nan_or_infinity_anywhere_in_a_row(ctx, dtype, value):
+    """Wherever it stands, whatever comes after it: in rows shared by CTAs and in rows of one."""
+    for rows, V in ((6, 40001), (700, 9001)):
+        x, g = make(rows, V, dtype)
+        for r, at in enumerate((0, 1, 1030, V // 2, V - 1)):
+            x[r, at] = value
+        check_logprobs(ctx, x, tokens_for(rows, V, g), 0, 1.0)
+        ids, v = teacher_for(x, 6, g, 1.0, pad=False)
+        clean = x[5:].clone()
+        for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+            loss = ctx.distill(x, ids, v, tail=tail)["loss"]
+            both = ctx.distill(x, ids, v, tail=tail, grad=True)
+            for got in (loss, both["loss"]):
+                assert torch.isnan(got[:5]).all() and torch.isfinite(got[5:]).all()
+            assert torch.isnan(both["grad"][:5]).any(1).all() and torch.isfinite(both["grad"][5:]).all()
+            ref.same(both["loss"][5:], ref.distill(clean, ids[5:], v[5:], tail == binding.TAIL_BUCKET, 1.0, None)[0], 1e-3)
