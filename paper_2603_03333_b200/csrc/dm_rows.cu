@@ -351,77 +351,76 @@ rows_kernel(const RowsParams P) {
     for (int b = 0; b < kRing; ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
 
     for (uint32_t parity = 0;; parity ^= 1u) {
-    if (kWalk && tid == 0) {
-        ptx::mbar_arrive_expect_tx(answer_bar, 16);
-        ptx::request_next_cluster(answer, answer_bar);
-    }
-    int next_row = -1;
-    float w = P.inv_temp;   // factor of the gradient
-    int tok = -1;
-    float tok_x = neg_inf();
-    if (kOp != OP_DISTILL && P.tokens != nullptr) {
-        tok = P.tokens[row];
-        if (tok < 0 || tok >= P.V) tok = -1;
-        if (tok >= 0) tok_x = RowVec<T>::get_early(sh.row + tok);
-    }
-    float g_lp = 0.0f, g_h = 0.0f;
-    bool zero_grad = false;
-    if (kOp == OP_GRAD) {
-        g_lp = P.g_logprob != nullptr && tok >= 0 ? P.g_logprob[row] : 0.0f;
-        g_h = P.g_entropy != nullptr ? P.g_entropy[row] : 0.0f;
-        zero_grad = g_lp == 0.0f && g_h == 0.0f;
-    }
-    const bool use_bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad_row != nullptr);
-    TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
-    if (kOp == OP_DISTILL) {
-        if (P.weight != nullptr) { const float wt = P.weight[row]; zero_grad = wt == 0.0f; w *= wt; }
-        if (tid < P.k) {
-            te.id = P.t_ids[(long long)row * P.k + tid];
-            te.v = P.t_logprob[(long long)row * P.k + tid];
-            if (te.id < 0 || te.id >= P.V) te.id = -1;
-            if (te.id >= 0) te.x = RowVec<T>::get_early(sh.row + te.id);
-            ss.t_id[tid] = te.id;
+        if (kWalk && tid == 0) {
+            ptx::mbar_arrive_expect_tx(answer_bar, 16);
+            ptx::request_next_cluster(answer, answer_bar);
         }
-        if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }
-        if (use_bits)
-            for (int i = tid; i < n_batches * kBatch / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
-        if (warp < kRowsMaxTop / 32) {
-            float vm = te.id >= 0 ? te.v : neg_inf();
+        int next_row = -1;
+        float w = P.inv_temp;   // factor of the gradient
+        int tok = -1;
+        float tok_x = neg_inf();
+        if (kOp != OP_DISTILL && P.tokens != nullptr) {
+            tok = P.tokens[row];
+            if (tok < 0 || tok >= P.V) tok = -1;
+            if (tok >= 0) tok_x = RowVec<T>::get_early(sh.row + tok);
+        }
+        float g_lp = 0.0f, g_h = 0.0f;
+        bool zero_grad = false;
+        if (kOp == OP_GRAD) {
+            g_lp = P.g_logprob != nullptr && tok >= 0 ? P.g_logprob[row] : 0.0f;
+            g_h = P.g_entropy != nullptr ? P.g_entropy[row] : 0.0f;
+            zero_grad = g_lp == 0.0f && g_h == 0.0f;
+        }
+        const bool use_bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad_row != nullptr);
+        TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
+        if (kOp == OP_DISTILL) {
+            if (P.weight != nullptr) { const float wt = P.weight[row]; zero_grad = wt == 0.0f; w *= wt; }
+            if (tid < P.k) {
+                te.id = P.t_ids[(long long)row * P.k + tid];
+                te.v = P.t_logprob[(long long)row * P.k + tid];
+                if (te.id < 0 || te.id >= P.V) te.id = -1;
+                if (te.id >= 0) te.x = RowVec<T>::get_early(sh.row + te.id);
+                ss.t_id[tid] = te.id;
+            }
+            if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }
+            if (use_bits)
+                for (int i = tid; i < n_batches * kBatch / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
+            if (warp < kRowsMaxTop / 32) {
+                float vm = te.id >= 0 ? te.v : neg_inf();
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
-            if (lane == 0) ss.t_max[warp] = vm;
-        }
-        __syncthreads();
-        if (use_bits && te.id >= 0) {
-            const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
-            if (at >= 0 && at < sh.last - sh.first) {
-                const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
-                te.first = (atomicOr(mark_word(bitmap, at), bit) & bit) == 0u;
-                if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
+                for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+                if (lane == 0) ss.t_max[warp] = vm;
+            }
+            __syncthreads();
+            if (use_bits && te.id >= 0) {
+                const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
+                if (at >= 0 && at < sh.last - sh.first) {
+                    const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
+                    te.first = (atomicOr(mark_word(bitmap, at), bit) & bit) == 0u;
+                    if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
+                }
+            }
+            __syncthreads();
+            if (warp < kRowsMaxTop / 32) {
+                float vm = ss.t_max[0];
+#pragma unroll
+                for (int i = 1; i < kRowsMaxTop / 32; ++i) vm = fmaxf(vm, ss.t_max[i]);
+                const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
+                if (te.id >= 0) te.q = exp((double)te.v - shift);
+                double sum = te.q;
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+                if (lane == 0) ss.t_sum[warp] = sum;      // read behind the barriers below
             }
         }
-        __syncthreads();
-        if (warp < kRowsMaxTop / 32) {
-            float vm = ss.t_max[0];
-#pragma unroll
-            for (int i = 1; i < kRowsMaxTop / 32; ++i) vm = fmaxf(vm, ss.t_max[i]);
-            const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
-            if (te.id >= 0) te.q = exp((double)te.v - shift);
-            double sum = te.q;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
-            if (lane == 0) ss.t_sum[warp] = sum;      // read behind the barriers below
-        }
-    }
 
-    // A row whose gradient is zero whatever it holds is not looked at (unless its loss is wanted).
-    const bool need_stats = !(zero_grad && (kOp == OP_GRAD || P.out_loss == nullptr));
-    if (need_stats) {
-        Stats st;
-        st.init();
-        const bool bucket = kTail && P.tail == DM_TAIL_BUCKET;
-        float thread_max = neg_inf();
-        {
+        // A row whose gradient is zero whatever it holds is not looked at (unless its loss is wanted).
+        const bool need_stats = !(zero_grad && (kOp == OP_GRAD || P.out_loss == nullptr));
+        if (need_stats) {
+            Stats st;
+            st.init();
+            const bool bucket = kTail && P.tail == DM_TAIL_BUCKET;
+            float thread_max = neg_inf();
             uint32_t* slot = slots + tid;
             uint32_t slot_key = 0u;
             int in_slot = 0;
@@ -463,121 +462,120 @@ rows_kernel(const RowsParams P) {
                 }
                 st.add<T, kEntropy, kTail>(v, lane_max, c, marks);
             }
-        }
-        if (!kWalk) copy_wait(0);   // (what is still in flight are empty batches)
-        if (n_cta > 1) cluster_wait();
-        block_merge(st, c, ss, cluster, n_cta, rank);
-        if (kOp == OP_LOGPROBS && P.n_top > 0) {
-            top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, hits, cand, sorted);
-            if (n_cta > 1)
-                for (int i = tid; i < P.n_top; i += kThreads) cluster.map_shared_rank(merged, 0)[rank * P.n_top + i] = sorted[i];
-        }
-        if (n_cta > 1) {
-            __syncwarp();
-            cluster_arrive();
-            cluster_wait();
+            if (!kWalk) copy_wait(0);   // (what is still in flight are empty batches)
+            if (n_cta > 1) cluster_wait();
+            block_merge(st, c, ss, cluster, n_cta, rank);
+            if (kOp == OP_LOGPROBS && P.n_top > 0) {
+                top_of_share(sh, thread_max, P.n_top, slots, P.slot_batches, ss, hits, cand, sorted);
+                if (n_cta > 1)
+                    for (int i = tid; i < P.n_top; i += kThreads) cluster.map_shared_rank(merged, 0)[rank * P.n_top + i] = sorted[i];
+            }
+            if (n_cta > 1) {
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+            } else {
+                __syncthreads();
+            }
+            if (warp == 0) cluster_merge(ss, n_cta, c);
         } else {
-            __syncthreads();
-        }
-        if (warp == 0) cluster_merge(ss, n_cta, c);
-    } else {
-        copy_wait(0);
-        if (n_cta > 1) cluster_wait();
-        if (tid == 0) {
-            ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
-            ss.log_total = ss.inv_total = 0.0f;
-        }
-    }
-    __syncthreads();
-    const Merged a = ss.all;
-    const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
-    const float log_total = ss.log_total, inv_total = ss.inv_total;
-    const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
-
-    if (kOp == OP_LOGPROBS) {
-        // fail-safe: a kernel ahead that produced these logits gave up on a wait
-        const bool failed = P.err != nullptr && *P.err != 0u;
-        const float bad = __uint_as_float(0x7FC00000u);
-        if (rank == 0 && tid == 0) {
-            if (P.out_logprob != nullptr)
-                P.out_logprob[row] = failed ? bad : tok < 0 ? 0.0f : tok_x == neg_inf() && a.rest == a.rest ? neg_inf() : fmaf(tok_x - a.m, P.inv_temp, -log_total);
-            if (P.out_lse != nullptr) P.out_lse[row] = failed ? bad : dead ? neg_inf() : fmaf(a.m, P.inv_temp, log_total);
-            if (P.out_entropy != nullptr) P.out_entropy[row] = failed ? bad : entropy;
-        }
-        if (P.n_top > 0 && rank == 0) {
-            // merge of sorted lists: the rank of an entry is its place in its own list plus the number
-            // of larger ones in each other list
-            const int k = P.n_top;
-            const unsigned long long* lists = n_cta > 1 ? merged : sorted;
-            for (int i = tid; i < n_cta * k; i += kThreads) {
-                const unsigned long long mine = lists[i];
-                if (mine == 0ull) continue;
-                int place = i % k;
-                for (int r = 0; r < n_cta && place < k; ++r) {
-                    if (r == i / k) continue;
-                    int lo = 0, hi = k;       // entries of list r that are larger
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (lists[r * k + mid] > mine) lo = mid + 1; else hi = mid;
-                    }
-                    place += lo;
-                }
-                if (place < k) {
-                    const uint32_t key = (uint32_t)(mine >> 32);
-                    const float x = key == 0xFFFFFFFFu ? bad : key_float(key);
-                    P.out_top_ids[(long long)row * k + place] = failed ? -1 : (int32_t)best_index(mine);
-                    P.out_top_logprob[(long long)row * k + place] =
-                        failed ? bad : x == neg_inf() && a.rest == a.rest ? neg_inf() : fmaf(x - a.m, P.inv_temp, -log_total);
-                }
+            copy_wait(0);
+            if (n_cta > 1) cluster_wait();
+            if (tid == 0) {
+                ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
+                ss.log_total = ss.inv_total = 0.0f;
             }
         }
-    }
-
-    float mass = 0.0f, rest = 0.0f;   // sum of the teacher's q, mass of its bucket (0: no bucket)
-    if (kOp == OP_DISTILL) {
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < kRowsMaxTop / 32; ++i) sum += ss.t_sum[i];
-        const double scale = P.tail == DM_TAIL_RENORM ? (sum != 0.0 ? 1.0 / sum : 0.0) : 1.0;
-        mass = (float)(sum * scale);
-        // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
-        if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
-        if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
         __syncthreads();
-        if (rank == 0 && warp == kWarps - 1 && P.out_loss != nullptr) {
-            const float loss = teacher_loss(P, a, ss.t_id, ss.t_v, ss.t_x, ss.t_q, sum, sum * scale, rest != 0.0f ? 1.0 - sum : 0.0);
-            if (lane == 0) P.out_loss[row] = loss;
-        }
-    }
+        const Merged a = ss.all;
+        const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
+        const float log_total = ss.log_total, inv_total = ss.inv_total;
+        const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
 
-    if (kOp != OP_LOGPROBS && grad_row != nullptr) {
-        const bool none = zero_grad || dead;
-        const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
-                                             : distill_factors(w, mass, rest, a.tail, inv_total);
-        const bool same_phase = phase_of(grad_row, sh.phase);
-#pragma unroll 4
-        for (int j = sh.first + tid; j < sh.last; j += kThreads)
-            store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(sh.load(j), a.m, c, f));
-        __syncthreads();   // the entries that differ are written over by one thread each
-        if (!none) {
-            const int lo = sh.entry0(sh.first), hi = sh.entry0(sh.last);   // this share's entries
-            if (kOp == OP_GRAD) {
-                if (tid == 0 && tok >= 0 && tok >= lo && tok < hi)   // (entries below 0 are the padding of the first vector)
-                    RowVec<T>::put(grad_row + tok, token_grad(tok_x, a, c, w, g_lp, g_h, entropy, log_total, inv_total));
-            } else if (te.first) {                       // (set only for tokens of this share)
-                float q = ss.t_q[tid];
-                if (ss.t_repeated) {
-                    q = 0.0f;
-                    for (int o = 0; o < P.k; ++o) q += ss.t_id[o] == te.id ? ss.t_q[o] : 0.0f;
+        if (kOp == OP_LOGPROBS) {
+            // fail-safe: a kernel ahead that produced these logits gave up on a wait
+            const bool failed = P.err != nullptr && *P.err != 0u;
+            const float bad = __uint_as_float(0x7FC00000u);
+            if (rank == 0 && tid == 0) {
+                if (P.out_logprob != nullptr)
+                    P.out_logprob[row] = failed ? bad : tok < 0 ? 0.0f : tok_x == neg_inf() && a.rest == a.rest ? neg_inf() : fmaf(tok_x - a.m, P.inv_temp, -log_total);
+                if (P.out_lse != nullptr) P.out_lse[row] = failed ? bad : dead ? neg_inf() : fmaf(a.m, P.inv_temp, log_total);
+                if (P.out_entropy != nullptr) P.out_entropy[row] = failed ? bad : entropy;
+            }
+            if (P.n_top > 0 && rank == 0) {
+                // merge of sorted lists: the rank of an entry is its place in its own list plus the number
+                // of larger ones in each other list
+                const int k = P.n_top;
+                const unsigned long long* lists = n_cta > 1 ? merged : sorted;
+                for (int i = tid; i < n_cta * k; i += kThreads) {
+                    const unsigned long long mine = lists[i];
+                    if (mine == 0ull) continue;
+                    int place = i % k;
+                    for (int r = 0; r < n_cta && place < k; ++r) {
+                        if (r == i / k) continue;
+                        int lo = 0, hi = k;       // entries of list r that are larger
+                        while (lo < hi) {
+                            const int mid = (lo + hi) >> 1;
+                            if (lists[r * k + mid] > mine) lo = mid + 1; else hi = mid;
+                        }
+                        place += lo;
+                    }
+                    if (place < k) {
+                        const uint32_t key = (uint32_t)(mine >> 32);
+                        const float x = key == 0xFFFFFFFFu ? bad : key_float(key);
+                        P.out_top_ids[(long long)row * k + place] = failed ? -1 : (int32_t)best_index(mine);
+                        P.out_top_logprob[(long long)row * k + place] =
+                            failed ? bad : x == neg_inf() && a.rest == a.rest ? neg_inf() : fmaf(x - a.m, P.inv_temp, -log_total);
+                    }
                 }
-                const float e = ex2((te.x - a.m) * c);
-                RowVec<T>::put(grad_row + te.id, fmaf(f.top, e, -w * q));
             }
         }
-    }
-    if (!kWalk || next_row < 0) break;
-    row = next_row;
-    sh = share_of<T>(P, row, n_cta, rank);
+
+        float mass = 0.0f, rest = 0.0f;   // sum of the teacher's q, mass of its bucket (0: no bucket)
+        if (kOp == OP_DISTILL) {
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < kRowsMaxTop / 32; ++i) sum += ss.t_sum[i];
+            const double scale = P.tail == DM_TAIL_RENORM ? (sum != 0.0 ? 1.0 / sum : 0.0) : 1.0;
+            mass = (float)(sum * scale);
+            // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
+            if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
+            if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
+            __syncthreads();
+            if (rank == 0 && warp == kWarps - 1 && P.out_loss != nullptr) {
+                const float loss = teacher_loss(P, a, ss.t_id, ss.t_v, ss.t_x, ss.t_q, sum, sum * scale, rest != 0.0f ? 1.0 - sum : 0.0);
+                if (lane == 0) P.out_loss[row] = loss;
+            }
+        }
+
+        if (kOp != OP_LOGPROBS && grad_row != nullptr) {
+            const bool none = zero_grad || dead;
+            const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
+                                                 : distill_factors(w, mass, rest, a.tail, inv_total);
+            const bool same_phase = phase_of(grad_row, sh.phase);
+#pragma unroll 4
+            for (int j = sh.first + tid; j < sh.last; j += kThreads)
+                store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(sh.load(j), a.m, c, f));
+            __syncthreads();   // the entries that differ are written over by one thread each
+            if (!none) {
+                const int lo = sh.entry0(sh.first), hi = sh.entry0(sh.last);   // this share's entries
+                if (kOp == OP_GRAD) {
+                    if (tid == 0 && tok >= 0 && tok >= lo && tok < hi)   // (entries below 0 are the padding of the first vector)
+                        RowVec<T>::put(grad_row + tok, token_grad(tok_x, a, c, w, g_lp, g_h, entropy, log_total, inv_total));
+                } else if (te.first) {                       // (set only for tokens of this share)
+                    float q = ss.t_q[tid];
+                    if (ss.t_repeated) {
+                        q = 0.0f;
+                        for (int o = 0; o < P.k; ++o) q += ss.t_id[o] == te.id ? ss.t_q[o] : 0.0f;
+                    }
+                    const float e = ex2((te.x - a.m) * c);
+                    RowVec<T>::put(grad_row + te.id, fmaf(f.top, e, -w * q));
+                }
+            }
+        }
+        if (!kWalk || next_row < 0) break;
+        row = next_row;
+        sh = share_of<T>(P, row, n_cta, rank);
     }
 }
 
