@@ -28,6 +28,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {   // a NaN on eithe
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
+// Maximum over the warp, in every lane: one instruction on sm_100a.  A NaN in any lane stays.
+__device__ __forceinline__ float warp_max_nan(float x) {
+    float y;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
 // Two entries per instruction: sm_100 has packed fp32 arithmetic.
 typedef float2 f32x2;
 __device__ __forceinline__ f32x2 pair(float lo, float hi) { return make_float2(lo, hi); }
@@ -307,9 +313,7 @@ struct Stats {
     // A batch of whatever entries, with the maximum so far kept exactly.
     template <typename T, bool kEntropy, bool kTail>
     __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, uint32_t marks) {
-        float wm = lane_max;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) wm = max_nan(wm, __shfl_xor_sync(0xFFFFFFFFu, wm, off));
+        const float wm = warp_max_nan(lane_max);
         if (!(wm < m && ce != 0.0f)) {
             if (wm == neg_inf()) return;   // nothing but masked entries so far
             if (m == m && !(wm <= m)) {    // a new maximum (a NaN stays one): the old one becomes an entry like the others
