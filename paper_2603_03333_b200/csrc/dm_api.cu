@@ -225,6 +225,7 @@ int rows_common(RowsParams* rp, int dtype, int64_t ld, int n_rows, int V, float 
     rp->inv_temp_d = 1.0 / (double)temperature;
     rp->inv_temp = (float)rp->inv_temp_d;
     rp->c = (float)(1.4426950408889634074 / (double)temperature);   // log2(e) / T
+    rp->gap = 250.0f / rp->c;
     return DM_OK;
 }
 

@@ -460,7 +460,7 @@ rows_kernel(const RowsParams P) {
                         in_slot = 0;
                     }
                 }
-                st.add<T, kEntropy, kTail>(v, lane_max, c, marks);
+                st.add<T, kEntropy, kTail>(v, lane_max, c, P.gap, marks);
             }
             if (!kWalk) copy_wait(0);   // (what is still in flight are empty batches)
             if (n_cta > 1) cluster_wait();
@@ -555,7 +555,7 @@ rows_kernel(const RowsParams P) {
             const bool same_phase = phase_of(grad_row, sh.phase);
 #pragma unroll 4
             for (int j = sh.first + tid; j < sh.last; j += kThreads)
-                store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(sh.load(j), a.m, c, f));
+                store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp, true>(sh.load(j), a.m, c, GradShift{}, f));
             __syncthreads();   // the entries that differ are written over by one thread each
             if (!none) {
                 const int lo = sh.entry0(sh.first), hi = sh.entry0(sh.last);   // this share's entries

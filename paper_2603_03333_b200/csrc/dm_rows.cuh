@@ -15,6 +15,7 @@ struct RowsParams {
     float inv_temp;       // 1 / T
     float c;              // log2(e) / T
     double inv_temp_d;
+    float gap;            // 250 / c: what lies farther below the maximum is nothing
     int stash_vecs;       // 16-byte vectors in shared memory: a CTA's share, or the ring it streams through (set by the launch)
     int n_batches;        // batches of the longest share (set by the launch)
     int slot_batches, n_slots;   // batches of a thread that share one remembered maximum, and how many of those (set by the launch)

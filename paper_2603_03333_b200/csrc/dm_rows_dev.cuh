@@ -34,6 +34,11 @@ __device__ __forceinline__ float warp_max_nan(float x) {
     asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float warp_max(float x) {   // ... of numbers
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+    return y;
+}
 // Two entries per instruction: sm_100 has packed fp32 arithmetic.
 typedef float2 f32x2;
 __device__ __forceinline__ f32x2 pair(float lo, float hi) { return make_float2(lo, hi); }
@@ -192,6 +197,7 @@ template <typename T> struct Share {
     const T* row;
     int V, phase, first, last;
     int whole_lo, whole_hi;   // vectors of the row that hold N of its entries
+    int whole_end;            // ... and of the share: the smaller of last and whole_hi
     __device__ __forceinline__ int entry0(int j) const { return j * RowVec<T>::N - phase; }
     __device__ __forceinline__ bool whole(int j) const { return j >= whole_lo && j < whole_hi; }
     __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(row - phase); }
@@ -206,21 +212,24 @@ template <typename T> struct Share {
         for (int n = 0; n < N; ++n) x[n] = (i0 + n >= 0 && i0 + n < V) ? RowVec<T>::get(row + i0 + n) : neg_inf();
         return RowVec<T>::pack(x);
     }
+    __device__ __forceinline__ bool whole_batch(int b0) const { return b0 >= whole_lo && b0 + kUnroll * kThreads <= whole_end; }
     // Sends one batch (vectors b0 + u * kThreads + thread) on its way to the thread's slots of shared
     // memory; slots past the end of the share are filled with masked entries.
     __device__ __forceinline__ void fetch_batch(int b0, uint4* slot) const {
-        const int j = b0 + (int)threadIdx.x;
-        if (b0 >= whole_lo && b0 + kUnroll * kThreads <= min(last, whole_hi)) {
-            const uint4* p = vectors() + j;
+        const uint4* p = vectors() + b0 + (int)threadIdx.x;
+        if (whole_batch(b0)) {
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) copy_async(slot + u * kThreads, p + u * kThreads);
         } else {
+            const int j = b0 + (int)threadIdx.x, n = whole_end - j, lo = whole_lo - j;
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
-                const int i = j + u * kThreads;
-                if (i < last && whole(i)) copy_async(slot + u * kThreads, vectors() + i);
-                else slot[u * kThreads] = i < last ? load(i) : RowVec<T>::masked();
+                if (u * kThreads < n && u * kThreads >= lo) copy_async(slot + u * kThreads, p + u * kThreads);
+                else slot[u * kThreads] = RowVec<T>::masked();
             }
+            if (j < whole_lo && j < last) *slot = load(j);   // the row's first vector, where it is not whole
+            const int e = last - 1 - j;                      // ... and its last
+            if (last > whole_hi && e >= 0 && e < kUnroll * kThreads && e % kThreads == 0) slot[e] = load(last - 1);
         }
         copy_commit();
     }
@@ -241,11 +250,11 @@ struct Stats {
     __device__ __forceinline__ float of_maximum() const { return ce != 0.0f ? ex2(fmaf(m, ce, -rc)) : 1.0f; }
 
     // Exponents are taken against `top` from here on (the sums are not moved).
-    template <typename T> __device__ __forceinline__ void set_maximum(float top, float c) {
+    template <typename T> __device__ __forceinline__ void set_maximum(float top, float c, float gap) {
         m = top;
         rc = top * c;
         ce = fabsf(rc) <= 1e37f ? c : 0.0f;
-        floor2 = RowVec<T>::floor_word(top - 250.0f / c);
+        floor2 = RowVec<T>::floor_word(top - gap);
         cnt = 0;
     }
     // Entries equal to the maximum are counted and taken out of the batch.
@@ -312,13 +321,13 @@ struct Stats {
     }
     // A batch of whatever entries, with the maximum so far kept exactly.
     template <typename T, bool kEntropy, bool kTail>
-    __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, uint32_t marks) {
+    __device__ __forceinline__ void add(uint4 (&v)[kUnroll], float lane_max, float c, float gap, uint32_t marks) {
         const float wm = warp_max_nan(lane_max);
         if (!(wm < m && ce != 0.0f)) {
             if (wm == neg_inf()) return;   // nothing but masked entries so far
             if (m == m && !(wm <= m)) {    // a new maximum (a NaN stays one): the old one becomes an entry like the others
                 const Stats old = *this;
-                set_maximum<T>(wm, c);
+                set_maximum<T>(wm, c, gap);
                 if (old.ce != 0.0f && ce != 0.0f) {
                     const float d = fmaxf(old.rc - rc, kFloorExp), f = ex2(d);
                     const float w = fmaxf(fmaf(old.m, c, -rc), kFloorExp), e = (float)old.cnt * ex2(w);
@@ -419,25 +428,33 @@ __device__ __forceinline__ float token_grad(float x, const Merged& a, float c, f
     const float by_entropy = -w * g_h * inv_total * e * fmaf(kLn2, z, entropy - log_total);
     return fmaf(w * g_lp, one_less, by_entropy);
 }
-// A vector of the row -> the same vector of its gradient.
-template <typename T, int kOp>
-__device__ __forceinline__ uint4 grad_vector(const uint4& v, float m, float c, const GradFactors& f) {
+// A vector of the row -> the same vector of its gradient.  shift: the rounded product m c, whose rounding
+// error `factors_against` has moved into the factors; where m c is too large for that, exponents are
+// taken of differences (kPlain).
+struct GradShift { float rc; uint32_t floor2; };
+template <typename T, int kOp, bool kPlain = false>
+__device__ __forceinline__ uint4 grad_vector(uint4 v, float m, float c, const GradShift& g, const GradFactors& f) {
     constexpr int N = RowVec<T>::N;
-    const f32x2 m2 = pair(-m, -m), c2 = pair(c, c), A2 = pair(f.A, f.A), B2 = pair(f.B, f.B);
+    const f32x2 m2 = kPlain ? pair(-m, -m) : pair(-g.rc, -g.rc), c2 = pair(c, c), A2 = pair(f.A, f.A), B2 = pair(f.B, f.B);
+    constexpr bool kClamp = kOp == OP_GRAD && (kPlain || !RowVec<T>::kFloorsEntries);   // (a masked entry: 0 * a finite exponent)
+    if (kOp == OP_GRAD && !kClamp) RowVec<T>::raise(v, g.floor2);
     f32x2 x[N / 2];
     RowVec<T>::pairs(v, x);
 #pragma unroll
     for (int n = 0; n < N / 2; ++n) {
-        f32x2 z = mul2(add2(x[n], m2), c2);
-        if (kOp == OP_GRAD) {
+        f32x2 z = kPlain ? mul2(add2(x[n], m2), c2) : fma2(x[n], c2, m2);
+        if (kClamp) {
             z.x = fmaxf(z.x, kFloorExp);
             z.y = fmaxf(z.y, kFloorExp);
-            x[n] = mul2(pair(ex2(z.x), ex2(z.y)), fma2(B2, z, A2));
-        } else {
-            x[n] = mul2(pair(ex2(z.x), ex2(z.y)), A2);
         }
+        x[n] = mul2(pair(ex2(z.x), ex2(z.y)), kOp == OP_GRAD ? fma2(B2, z, A2) : A2);
     }
     return RowVec<T>::pack_pairs(x);
+}
+// With z' = z + d for every entry (d = m c - rc, tiny): 2^z (A + B z) = 2^z' 2^-d (A - B d + B z').
+__device__ __forceinline__ GradFactors factors_against(const GradFactors& f, float d) {
+    const float scale = ex2(-d);
+    return GradFactors{scale * fmaf(-d, f.B, f.A), scale * f.B, f.top};
 }
 // ... and its way to the gradient's row (which may have another alignment).
 template <typename T>
@@ -466,6 +483,7 @@ __device__ __forceinline__ Share<T> share_of(const RowsParams& P, int row, int n
     sh.last = min(n_vec, sh.first + per);
     sh.whole_lo = sh.phase != 0 ? 1 : 0;
     sh.whole_hi = (sh.phase + P.V) / N;
+    sh.whole_end = min(sh.last, sh.whole_hi);
     return sh;
 }
 // Marks of a share's teacher tokens: a byte per vector, the bytes of a thread's batch in one word.

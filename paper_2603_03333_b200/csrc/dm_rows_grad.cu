@@ -44,7 +44,7 @@ struct ResidentShared {
     float t_v[2][kRowsMaxTop], t_x[2][kRowsMaxTop], t_q[2][kRowsMaxTop];
     float t_max[kTeacherWarps];
     double t_sum[kTeacherWarps];
-    int t_distinct, t_repeated;
+    int t_distinct[2], t_repeated[2];
 };
 
 template <typename T, int kOp>
@@ -69,6 +69,8 @@ rows_resident_kernel(const RowsParams P) {
     for (int b = 0; b < n_batches; ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
     if (kTail) {
         for (int i = tid; i < P.stash_vecs / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
+        if (tid < 2) ss.t_distinct[tid] = ss.t_repeated[tid] = 0;
+        __syncthreads();
     }
     // the row's small inputs, one row ahead
     int next_id = -1;              // token, or this thread's teacher token
@@ -108,6 +110,7 @@ rows_resident_kernel(const RowsParams P) {
         float tok_x = neg_inf();
         bool zero_grad;
         TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
+        uint32_t* my_word = nullptr;   // word of the bitmap in which this thread's token is marked
         if (kOp == OP_GRAD) {
             if (next_id >= 0 && next_id < P.V) { tok = next_id; tok_x = RowVec<T>::get_early(sh.row + tok); g_lp = next_a; }
             g_h = next_b;
@@ -120,34 +123,27 @@ rows_resident_kernel(const RowsParams P) {
                 te.v = next_a;
                 te.x = RowVec<T>::get_early(sh.row + te.id);
             }
-            if (tid < P.k) { ss.t_id[par][tid] = te.id; ss.t_v[par][tid] = te.v; }
-            if (tid == 0) ss.t_distinct = ss.t_repeated = 0;
-            if (warp < kTeacherWarps) {
-                float vm = te.v;
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
-                if (lane == 0) ss.t_max[warp] = vm;
-            }
-            __syncthreads();
-        }
-        uint32_t* my_word = nullptr;   // word of the bitmap in which this thread's token is marked
-        float v_shift = 0.0f;          // renorm: the largest teacher value
-        if (kOp == OP_DISTILL) {
             if (te.id >= 0) {
                 const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
                 if (at >= 0 && at < n_share) {
                     const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
                     my_word = mark_word(bitmap, at);
                     te.first = (atomicOr(my_word, bit) & bit) == 0u;
-                    if (te.first) atomicAdd(&ss.t_distinct, 1); else ss.t_repeated = 1;
+                    if (te.first) atomicAdd(&ss.t_distinct[par], 1); else ss.t_repeated[par] = 1;
                 }
             }
+            if (tid < P.k) { ss.t_id[par][tid] = te.id; ss.t_v[par][tid] = te.v; }
             if (warp < kTeacherWarps) {
+                const float vm = warp_max(te.v);
+                if (lane == 0) ss.t_max[warp] = vm;
+            }
+            __syncthreads();
+            if (warp < kTeacherWarps) {   // q in fp64, relative to the largest value (renorm)
                 float vm = ss.t_max[0];
 #pragma unroll
                 for (int i = 1; i < kTeacherWarps; ++i) vm = fmaxf(vm, ss.t_max[i]);
-                if (P.tail == DM_TAIL_RENORM && vm > neg_inf()) v_shift = vm;
-                if (te.id >= 0) te.q = exp((double)te.v - (double)v_shift);
+                const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
+                if (te.id >= 0) te.q = exp((double)te.v - shift);
                 double sum = te.q;
 #pragma unroll
                 for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
@@ -193,26 +189,38 @@ rows_resident_kernel(const RowsParams P) {
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
                 thread_max = max_nan(thread_max, RowVec<T>::vmax(v));
+                if (bucket) {   // the teacher's tokens leave the share: what is left is the tail
+                    for (uint32_t marks = reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid]; marks != 0u; marks &= marks - 1u) {
+                        const int bit = __ffs(marks) - 1;
+                        RowVec<T>::put(reinterpret_cast<T*>(stash + b * kBatch + (bit >> 3) * kThreads + tid) + (bit & 7), neg_inf());
+                    }
+                }
             }
             float m = thread_max;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
             if (lane == 0) ss.w_max[warp] = m;
-            __syncthreads();   // (the teacher's marks are complete behind it, too)
+            __syncthreads();
             m = ss.w_max[0];
 #pragma unroll
             for (int i = 1; i < kWarps; ++i) m = max_nan(m, ss.w_max[i]);
             Stats st;
             st.init();
-            st.set_maximum<T>(m, c);
+            st.set_maximum<T>(m, c, P.gap);
             const bool holder = __any_sync(0xFFFFFFFFu, thread_max == m && m != neg_inf());
             for (int b = 0; b < n_batches && (holder || st.ce != 0.0f); ++b) {
                 uint4 v[kUnroll];
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
-                const uint32_t marks = bucket ? reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid] : 0u;
-                if (holder) st.take<T, kTail>(v, marks);
-                if (st.ce != 0.0f) st.sum<T, kEntropy, kTail>(v, marks);
+                if (holder) st.take<T, false>(v, 0u);
+                if (st.ce != 0.0f) st.sum<T, kEntropy, false>(v, 0u);
+            }
+            if (kTail) {
+                st.tail = fmaf((float)st.cnt, st.of_maximum(), st.s);
+                if (bucket && te.first) {   // the teacher's tokens, by their threads
+                    if (te.x == m) st.cnt += m != neg_inf() ? 1 : 0;
+                    else if (st.ce != 0.0f) st.s += ex2(fmaf(te.x, st.ce, -st.rc));
+                }
             }
             st.finish();
             WarpSums r{warp_sum(st.s), kEntropy ? warp_sum(st.t) : 0.0f, kTail ? warp_sum(st.tail) : 0.0f, warp_sum((float)st.cnt)};
@@ -257,8 +265,9 @@ rows_resident_kernel(const RowsParams P) {
                 ss.log_total = ss.inv_total = 0.0f;
             }
         }
-        // (the passes that read the bitmap are over)
+        // (the pass that reads the bitmap is over; so is the row before's use of its counters)
         if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
+        if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = 0;
         const int next_row = ss.next_row[par];
         const bool more = next_row >= 0;
         if (more) load_small(next_row);
@@ -270,17 +279,19 @@ rows_resident_kernel(const RowsParams P) {
             const double scale = P.tail == DM_TAIL_RENORM ? (q_sum != 0.0 ? 1.0 / q_sum : 0.0) : 1.0;
             mass = (float)(q_sum * scale);
             // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
-            if (bucket && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - q_sum > 0.0 || q_sum != q_sum ? (float)(1.0 - q_sum) : 0.0f;
+            if (bucket && (P.k < P.V || ss.t_distinct[par] < P.V)) rest = 1.0 - q_sum > 0.0 || q_sum != q_sum ? (float)(1.0 - q_sum) : 0.0f;
             q = (float)(te.q * scale);
             if (tid < P.k) { ss.t_q[par][tid] = q; ss.t_x[par][tid] = te.x; }
         }
-        const bool repeated = kOp == OP_DISTILL && ss.t_repeated != 0;
+        const bool repeated = kOp == OP_DISTILL && ss.t_repeated[par] != 0;
         __syncthreads();
         const Merged a = ss.all;
         const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
         const float log_total = ss.log_total, inv_total = ss.inv_total;
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
         const bool none = zero_grad || dead;
+        const float rc = a.m * c;
+        const bool plain = !(fabsf(rc) <= 1e37f);
         const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                              : distill_factors(w, mass, rest, a.tail, inv_total);
 
@@ -288,9 +299,10 @@ rows_resident_kernel(const RowsParams P) {
         // program order before its copies into them are issued, and only ever touches its own)
         const bool same_phase = phase_of(grad_row, sh.phase);
         const Share<T> next = more ? share_of<T>(P, next_row, n_cta, rank) : sh;
-        const int whole_end = min(sh.last, sh.whole_hi);
-        if (same_phase && !none) {
-            uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase);
+        const GradShift shift{rc, RowVec<T>::floor_word(a.m - P.gap)};
+        const GradFactors g = factors_against(f, fmaf(a.m, c, -rc));
+        if (same_phase && !none && !plain) {
+            uint4* dst = reinterpret_cast<uint4*>(grad_row - sh.phase) + sh.first + tid;
             for (int b = 0; b < n_batches; ++b) {
                 uint4 v[kUnroll];
                 uint4* slot = stash + b * kBatch + tid;
@@ -298,18 +310,23 @@ rows_resident_kernel(const RowsParams P) {
                 for (int u = 0; u < kUnroll; ++u) v[u] = slot[u * kThreads];
                 if (more) next.fetch_batch(next.first + b * kBatch, slot);
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    const int j = sh.first + b * kBatch + u * kThreads + tid;
-                    v[u] = grad_vector<T, kOp>(v[u], a.m, c, f);
-                    if (j >= sh.whole_lo && j < whole_end) __stcs(dst + j, v[u]);
+                for (int u = 0; u < kUnroll; ++u) v[u] = grad_vector<T, kOp>(v[u], a.m, c, shift, g);
+                if (sh.whole_batch(sh.first + b * kBatch)) {
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u) __stcs(dst + b * kBatch + u * kThreads, v[u]);
+                } else {
+                    const int j = sh.first + b * kBatch + tid, n = sh.whole_end - j, lo = sh.whole_lo - j;
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u)
+                        if (u * kThreads < n && u * kThreads >= lo) __stcs(dst + b * kBatch + u * kThreads, v[u]);
                 }
             }
             // the row's first and last vector, where it shares them with its neighbours: read again
             const int edge = sh.first + tid < sh.whole_lo ? sh.first + tid
                              : sh.last > sh.whole_hi && (sh.last - 1 - sh.first) % kThreads == tid ? sh.last - 1 : -1;
-            if (edge >= 0) store_vector(grad_row, sh, edge, true, grad_vector<T, kOp>(sh.load(edge), a.m, c, f));
+            if (edge >= 0) store_vector(grad_row, sh, edge, true, grad_vector<T, kOp>(sh.load(edge), a.m, c, shift, g));
             if (edge >= 0 && edge < sh.whole_lo && sh.last > sh.whole_hi && sh.last - 1 != edge && (sh.last - 1 - sh.first) % kThreads == tid)
-                store_vector(grad_row, sh, sh.last - 1, true, grad_vector<T, kOp>(sh.load(sh.last - 1), a.m, c, f));
+                store_vector(grad_row, sh, sh.last - 1, true, grad_vector<T, kOp>(sh.load(sh.last - 1), a.m, c, shift, g));
         } else {
             for (int b = 0; b < n_batches; ++b) {
                 uint4* slot = stash + b * kBatch + tid;
@@ -317,7 +334,10 @@ rows_resident_kernel(const RowsParams P) {
                 for (int u = 0; u < kUnroll; ++u) {
                     const int j = sh.first + b * kBatch + u * kThreads + tid;
                     if (j < sh.last)
-                        store_vector(grad_row, sh, j, same_phase, none ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T, kOp>(slot[u * kThreads], a.m, c, f));
+                        store_vector(grad_row, sh, j, same_phase,
+                                     none    ? make_uint4(0u, 0u, 0u, 0u)
+                                     : plain ? grad_vector<T, kOp, true>(slot[u * kThreads], a.m, c, shift, f)
+                                             : grad_vector<T, kOp>(slot[u * kThreads], a.m, c, shift, g));
                 }
                 if (more) next.fetch_batch(next.first + b * kBatch, slot);
             }
