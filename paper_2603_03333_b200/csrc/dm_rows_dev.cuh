@@ -383,28 +383,38 @@ __device__ __forceinline__ float warp_sum(float x) {
 // precision as a difference) and tells entries that name the same token apart.
 struct TeacherEntry { int id; float v, x; bool first; double q; };
 
+// The largest value of the entries that are present, of those that a lane looks at.
+__device__ __forceinline__ float v_of(const int* id, const float* v, int lane, int k) {
+    float vm = neg_inf();
+    for (int i = lane; i < k; i += 32) vm = fmaxf(vm, id[i] >= 0 ? v[i] : neg_inf());
+    __syncwarp();
+    return vm;
+}
+
 // The loss of a row, by one warp.  fp64: it is a small difference of logarithms that are not small, and
 // there are only k of them.  mass, rest: of the teacher's tokens and of its bucket (0: no bucket).
 __device__ __forceinline__ float teacher_loss(const RowsParams& P, const Merged& a, const int* id, const float* v, const float* x,
                                               const float* q, double q_sum, double mass, double rest) {
     const int lane = threadIdx.x & 31;
     const bool dead = a.m == neg_inf();
-    const double log_total = log1p((double)a.rest);
-    float vm = neg_inf();
-    for (int i = lane; i < P.k; i += 32) vm = fmaxf(vm, id[i] >= 0 ? v[i] : neg_inf());
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) vm = fmaxf(vm, __shfl_xor_sync(0xFFFFFFFFu, vm, off));
+    const float all_v = warp_max(v_of(id, v, lane, P.k));
+    // four logarithms at once, a lane each: of the student's total, the teacher's sum, its bucket, the tail
+    const double of = lane == 0 ? 1.0 + (double)a.rest : lane == 1 ? q_sum : lane == 2 ? rest : (double)a.tail;
+    const double logs = lane < 4 ? log(of) : 0.0;
+    const double log_total = __shfl_sync(0xFFFFFFFFu, logs, 0), log_q = __shfl_sync(0xFFFFFFFFu, logs, 1);
+    const double log_rest = __shfl_sync(0xFFFFFFFFu, logs, 2), log_tail = __shfl_sync(0xFFFFFFFFu, logs, 3);
     // log q = v - base: the teacher's normaliser
-    const double base = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm + log(q_sum) : 0.0;
+    const double base = P.tail == DM_TAIL_RENORM && all_v > neg_inf() ? (double)all_v + log_q : 0.0;
     double loss = 0.0;
     for (int i = lane; i < P.k; i += 32) {
         if (id[i] < 0 || q[i] == 0.0f) continue;
         const double logp = dead || x[i] == neg_inf() ? -INFINITY : ((double)x[i] - (double)a.m) * P.inv_temp_d - log_total;
         loss += (double)q[i] * (((double)v[i] - base) - logp);
     }
+    __syncwarp();
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, off);
-    if (rest != 0.0 && !(dead && mass == 0.0)) loss += rest * (log(rest) - (log((double)a.tail) - log_total));
+    if (rest != 0.0 && !(dead && mass == 0.0)) loss += rest * (log_rest - (log_tail - log_total));
     return (float)loss;
 }
 
