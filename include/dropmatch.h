@@ -212,9 +212,10 @@ int dropmatch_verify_js(dm_ctx* ctx, const void* H, const int32_t* draft, const 
 
 /* ---- log-probabilities, and training the draft model ---------------------------------------------
  * The paper decides on tokens; an engine around it also wants their log-probabilities, and a draft
- * model whose tokens get accepted has to be trained towards the target.  The three calls below cover
+ * model whose tokens get accepted has to be trained towards the target.  The calls below cover
  * that: dropmatch_score reads the target's head (and gives a teacher's top tokens), dropmatch_distill
  * trains the draft's logits towards them, dropmatch_logprobs and its gradient work on any logits.
+ * Results do not depend on the order in which CTAs run: equal calls give equal bits.
  *
  * Definitions, for a row of logits l[0..V) and a temperature T > 0:
  *   z = l / T;  lse = log sum_v exp(z[v]);  log p[v] = z[v] - lse;  entropy = - sum_v p[v] log p[v].
@@ -231,10 +232,12 @@ int dropmatch_verify_js(dm_ctx* ctx, const void* H, const int32_t* draft, const 
  * log-probabilities close to 0 keep their relative precision. */
 
 /* Score hidden rows against the context's head, without dropout: l = H W^T (Eq. 3).
- * dm_enable_score reserves, after dm_set_head, the workspace for calls of up to max_rows rows and
- * max_top alternatives (fp32 logits of at most 512 rows at a time).  Allocates; synchronises the
- * device; a later dm_set_head drops the buffers.
- *   H[n_rows,d]      storage type of the head, 16-byte aligned
+ * dm_enable_score reserves, after dm_set_head, the workspace for calls of up to max_rows rows (at most
+ * dm_set_head's) and max_top alternatives: records of every vocabulary slice and, with alternatives, fp32
+ * logits of at most 512 rows at a time.  Allocates; synchronises the device; a later dm_set_head or
+ * dm_enable_score drops the buffers (graphs captured with them must not be replayed).
+ *   H[n_rows,d]      storage type of the head, 16-byte aligned; finite, as W (what a row reports that a NaN
+ *                    or an infinity in either reaches is unspecified; it is never a fault)
  *   tokens[n_rows]   device, may be NULL (then out_logprob must be NULL)
  * n_rows = 0 is allowed and does nothing.  DM_EWORKSPACE beyond what dm_enable_score reserved.
  * Sharded heads (dm_set_vocab_offset) are not supported: DM_EUNSUPPORTED.  Like every context-based
@@ -248,7 +251,9 @@ int dropmatch_score(dm_ctx* ctx, const void* H, const int32_t* tokens, int n_row
 /* The same on logits in memory.  Needs no head and no workspace: calls of one context may overlap.
  *   logits[n_rows][ld]   dtype DM_F32 or DM_BF16, row stride ld >= V entries, aligned to one entry
  *                        (16-byte aligned rows of the same alignment are the fastest)
- * n_rows = 0 is allowed and does nothing.  V <= 2^30. */
+ * n_rows = 0 is allowed and does nothing.  V <= 2^30.
+ * Error word (dm_device_error) 8, this call and the gradients: a cluster gave up waiting (a second) for the
+ * answer to its request for another row; rows that it would have taken are unwritten. */
 int dropmatch_logprobs(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
                        const int32_t* tokens, int n_top, float temperature, float* out_logprob, float* out_lse,
                        float* out_entropy, int32_t* out_top_ids, float* out_top_logprob, void* stream);
@@ -257,7 +262,8 @@ int dropmatch_logprobs(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, i
  * logits:  dl[v] = (1/T) ( g_logprob (1[v = token] - p[v]) - g_entropy p[v] (log p[v] + entropy) ).
  *   g_logprob, g_entropy [n_rows]   float32; either may be NULL (zero); `tokens` is needed with g_logprob
  *   out_grad[n_rows][ld_grad]       same type as the logits, rounded once; may be the logits themselves
- *                                   (same pointer, ld_grad = ld), else must not overlap them.
+ *                                   (same pointer, ld_grad = ld), else the two ranges, from the first row's
+ *                                   first entry to the last row's last, must not overlap.
  *                                   Entries V..ld_grad of a row are left as they are
  * A row whose two factors are 0 (or that has no token and g_entropy = 0) gets a gradient of 0 whatever
  * its logits hold; so does a row of nothing but -inf.  Recomputes the row's sums: one read of the
@@ -282,7 +288,8 @@ int dropmatch_logprobs_grad(dm_ctx* ctx, const void* logits, int dtype, int64_t 
  *   dl[v] = weight / T * ( M p[v] - q[v] - [v is no teacher token] q_t p[v] / p_t ),  M = sum q + q_t
  * No factor T^2 is applied.  A row without a present entry: loss 0 (and gradient 0).  A teacher token
  * the student gives probability 0: loss +inf.  A row of nothing but -inf: gradient 0.  A row of weight 0
- * gets a gradient of 0 whatever it holds.  DM_EUNSUPPORTED beyond V of about 12 million (bucket). */
+ * gets a gradient of 0 whatever it holds.  DM_EUNSUPPORTED beyond V of about 12 million (bf16) or 6 million
+ * (fp32) with DM_TAIL_BUCKET or a gradient. */
 int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
                       const int32_t* teacher_ids, const float* teacher_logprob, int k, int tail, float temperature,
                       const float* weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream);

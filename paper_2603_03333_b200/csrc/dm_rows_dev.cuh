@@ -383,12 +383,12 @@ __device__ __forceinline__ float warp_sum(float x) {
 // precision as a difference) and tells entries that name the same token apart.
 struct TeacherEntry { int id; float v, x; bool first; double q; };
 
-// The largest value of the entries that are present, of those that a lane looks at.
-__device__ __forceinline__ float v_of(const int* id, const float* v, int lane, int k) {
+// The largest value of a teacher's entries that are present, by one warp.
+__device__ __forceinline__ float largest_value(const int* id, const float* v, int k) {
     float vm = neg_inf();
-    for (int i = lane; i < k; i += 32) vm = fmaxf(vm, id[i] >= 0 ? v[i] : neg_inf());
+    for (int i = (int)(threadIdx.x & 31); i < k; i += 32) vm = fmaxf(vm, id[i] >= 0 ? v[i] : neg_inf());
     __syncwarp();
-    return vm;
+    return warp_max(vm);
 }
 
 // The loss of a row, by one warp.  fp64: it is a small difference of logarithms that are not small, and
@@ -397,7 +397,7 @@ __device__ __forceinline__ float teacher_loss(const RowsParams& P, const Merged&
                                               const float* q, double q_sum, double mass, double rest) {
     const int lane = threadIdx.x & 31;
     const bool dead = a.m == neg_inf();
-    const float all_v = warp_max(v_of(id, v, lane, P.k));
+    const float all_v = largest_value(id, v, P.k);
     // four logarithms at once, a lane each: of the student's total, the teacher's sum, its bucket, the tail
     const double of = lane == 0 ? 1.0 + (double)a.rest : lane == 1 ? q_sum : lane == 2 ? rest : (double)a.tail;
     const double logs = lane < 4 ? log(of) : 0.0;
