@@ -36,27 +36,61 @@ constexpr int kShareVecs = 4096;        // share up to which a row is cut: 64 KB
 constexpr int kTeacherWarps = kRowsMaxTop / 32;
 constexpr long long kWaitLimitCycles = 2000000000ll;   // about one second
 
-struct WarpSums { float s, t, tail, cnt; };   // relative to the CTA's maximum: below it; entries equal to it
+// A warp's part of a row: its CTA's maximum, and relative to it the sum of exponentials over the entries
+// below it, the same weighted with the exponents (gradient of the entropy) or over the tail (distillation,
+// maximum included), and how many entries equal the maximum.
+struct __align__(16) WarpSums { float m, s, x, cnt; };
+struct PendingLoss { Merged a; double q_sum, mass, rest; int row; };   // row -1: none
 
 struct ResidentShared {
+    // written by every CTA of the cluster, twice over: a CTA may be one row ahead of another
+    WarpSums part[2][kRowsMaxCluster * kWarps];
     uint4 answer;                  // to the request for another row (rank 0)
     uint64_t answer_bar;
     int abort;
     int next_row[2];               // written by rank 0 into every CTA, twice over
     float w_max[kWarps];
-    // written by every CTA of the cluster, twice over: a CTA may be one row ahead of another
-    float part_m[2][kRowsMaxCluster];
-    WarpSums part[2][kRowsMaxCluster][kWarps];
-    Merged cta[kRowsMaxCluster];
-    Merged all;
-    float log_total, inv_total;
-    // teacher (distill), twice over: the loss of a row is finished while the next one has begun
+    // teacher (distill), twice over: the loss of a row is finished while the next one is under way
     int t_id[2][kRowsMaxTop];
     float t_v[2][kRowsMaxTop], t_x[2][kRowsMaxTop], t_q[2][kRowsMaxTop];
+    int t_distinct[2], t_repeated[2];
     float t_max[kTeacherWarps];
     double t_sum[kTeacherWarps];
-    int t_distinct[2], t_repeated[2];
+    PendingLoss loss;              // of the row before, until its warp finds the time (rank 0)
 };
+
+// The row's statistics from its warps' parts: every warp does the same for itself (some 100 instructions)
+// instead of one that keeps the others waiting behind another barrier (2000 cycles of a row's 16 to 27 thousand).
+template <bool kEntropy, bool kTail>
+__device__ __forceinline__ Merged merge_parts(const WarpSums* part, int n, float c) {
+    const int lane = threadIdx.x & 31;
+    const WarpSums none{neg_inf(), 0.0f, 0.0f, 0.0f};
+    const WarpSums r0 = lane < n ? part[lane] : none;
+    const WarpSums r1 = lane + 32 < n ? part[lane + 32] : none;
+    Merged a{warp_max_nan(max_nan(r0.m, r1.m)), 0.0f, 0.0f, 0.0f};
+    float cnt = 0.0f;
+    const auto take = [&](const WarpSums& r) {
+        if (r.m == a.m) {
+            a.rest += r.s; cnt += r.cnt;
+            if (kEntropy) a.t += r.x;
+            if (kTail) a.tail += r.x;
+        } else if (r.m != neg_inf()) {
+            const float d = fmaxf((r.m - a.m) * c, kFloorExp), f = ex2(d), all = r.s + r.cnt;
+            a.rest = fmaf(f, all, a.rest);
+            if (kEntropy) a.t = fmaf(f, fmaf(d, all, r.x), a.t);
+            if (kTail) a.tail = fmaf(f, r.x, a.tail);
+        }
+    };
+    take(r0);
+    if (n > 32) take(r1);
+    __syncwarp();
+    a.rest = warp_sum(a.rest);
+    if (kEntropy) a.t = warp_sum(a.t);
+    if (kTail) a.tail = warp_sum(a.tail);
+    a.rest += fmaxf(warp_sum(cnt) - 1.0f, 0.0f);
+    if (!(a.m < __uint_as_float(0x7F800000u))) a.rest = a.t = a.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
+    return a;
+}
 
 template <typename T, int kOp>
 __global__ void __launch_bounds__(kThreads, 3)
@@ -109,7 +143,23 @@ rows_resident_kernel(const RowsParams P) {
     }
     bool started = n_cta == 1;
 
+    // The loss of a distillation row is left to one warp, which finishes it where the cluster meets over
+    // the row after it: its logarithms take some 3000 cycles that the others would wait for.
+    const auto finish_loss = [&](int p) {
+        if (kOp != OP_DISTILL || rank != 0 || warp != kWarps - 1) return;
+        __syncwarp();
+        const PendingLoss of = ss.loss;
+        if (of.row >= 0) {
+            const float loss = teacher_loss(P, of.a, ss.t_id[p], ss.t_v[p], ss.t_x[p], ss.t_q[p], of.q_sum, of.mass, of.rest);
+            if (lane == 0) P.out_loss[of.row] = loss;
+        }
+        __syncwarp();
+    };
+    if (tid == kThreads - 32) ss.loss.row = -1;
+
+    int last_par = 0;
     for (int par = 0; row >= 0; par ^= 1) {
+        last_par = par;
         const int n_share = sh.last - sh.first;
         if (rank == 0 && tid == 0) {   // the answer is waited for when the row's sums are known
             ptx::mbar_arrive_expect_tx(answer_bar, 16);
@@ -185,9 +235,11 @@ rows_resident_kernel(const RowsParams P) {
         const auto meet = [&]() {
             if (n_cta == 1) {
                 __syncthreads();
+                finish_loss(par ^ 1);
             } else {
                 __syncwarp();
                 cluster_arrive();
+                finish_loss(par ^ 1);
                 cluster_wait();
             }
         };
@@ -207,18 +259,16 @@ rows_resident_kernel(const RowsParams P) {
                     }
                 }
             }
-            float m = thread_max;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, off));
-            if (lane == 0) ss.w_max[warp] = m;
+            const float warp_top = warp_max_nan(thread_max);
+            if (lane == 0) ss.w_max[warp] = warp_top;
             __syncthreads();
-            m = ss.w_max[0];
+            float m = ss.w_max[0];
 #pragma unroll
             for (int i = 1; i < kWarps; ++i) m = max_nan(m, ss.w_max[i]);
             Stats st;
             st.init();
             st.set_maximum<T>(m, c, P.gap);
-            const bool holder = __any_sync(0xFFFFFFFFu, thread_max == m && m != neg_inf());
+            const bool holder = warp_top == m && m != neg_inf();
             for (int b = 0; b < n_batches && (holder || st.ce != 0.0f); ++b) {
                 uint4 v[kUnroll];
 #pragma unroll
@@ -234,54 +284,21 @@ rows_resident_kernel(const RowsParams P) {
                 }
             }
             st.finish();
-            WarpSums r{warp_sum(st.s), kEntropy ? warp_sum(st.t) : 0.0f, kTail ? warp_sum(st.tail) : 0.0f, warp_sum((float)st.cnt)};
-            __syncwarp();
-            if (lane < n_cta) {
-                ResidentShared* other = n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane);
-                other->part[par][rank][warp] = r;
-                if (warp == 0) other->part_m[par][rank] = m;
-            }
-            tell_next();
-            meet();
-            if (warp == 0) {
-                // one lane joins the warps of a CTA, then all lanes alike join the CTAs
-                if (lane < n_cta) {
-                    float s = 0.0f, t = 0.0f, tail = 0.0f, cnt = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < kWarps; ++i) {
-                        const WarpSums p = ss.part[par][lane][i];
-                        s += p.s; t += p.t; tail += p.tail; cnt += p.cnt;
-                    }
-                    const float pm = ss.part_m[par][lane];
-                    Merged p{pm, s + fmaxf(cnt - 1.0f, 0.0f), t, tail};
-                    if (!(pm < __uint_as_float(0x7F800000u))) p.rest = p.t = p.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
-                    ss.cta[lane] = p;
-                }
-                __syncwarp();
-                Merged a = ss.cta[0];
-#pragma unroll 1
-                for (int i = 1; i < n_cta; ++i) a = join(a, ss.cta[i], c);
-                if (lane == 0) {
-                    ss.all = a;
-                    ss.log_total = log1pf(a.rest);
-                    ss.inv_total = 1.0f / (1.0f + a.rest);
-                }
-            }
+            const WarpSums r{m, warp_sum(st.s), warp_sum(kTail ? st.tail : st.t), (float)__reduce_add_sync(0xFFFFFFFFu, st.cnt)};
+            if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->part[par][rank * kWarps + warp] = r;
         } else {
             copy_wait(0);
-            tell_next();
-            meet();
-            if (tid == 0) {
-                ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
-                ss.log_total = ss.inv_total = 0.0f;
-            }
         }
-        // (the pass that reads the bitmap is over; so is the row before's use of its counters)
-        if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
-        if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = 0;
+        tell_next();
+        meet();
         const int next_row = ss.next_row[par];
         const bool more = next_row >= 0;
         if (more) load_small(next_row);
+        const Merged a = need_stats ? merge_parts<kEntropy, kTail>(ss.part[par], n_cta * kWarps, c) : Merged{0.0f, 0.0f, 0.0f, 0.0f};
+        const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
+        // (the pass that reads the bitmap is over; so is the row before's use of its counters)
+        if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
+        if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = 0;
         float mass = 0.0f, rest = 0.0f, q = 0.0f;   // sum of the teacher's q, mass of its bucket, this thread's q
         double q_sum = 0.0;
         if (kOp == OP_DISTILL) {
@@ -295,10 +312,7 @@ rows_resident_kernel(const RowsParams P) {
             if (tid < P.k) { ss.t_q[par][tid] = q; ss.t_x[par][tid] = te.x; }
         }
         const bool repeated = kOp == OP_DISTILL && ss.t_repeated[par] != 0;
-        __syncthreads();
-        const Merged a = ss.all;
         const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
-        const float log_total = ss.log_total, inv_total = ss.inv_total;
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
         const bool none = zero_grad || dead;
         const float rc = a.m * c;
@@ -328,16 +342,12 @@ rows_resident_kernel(const RowsParams P) {
                 } else {
                     const int j = sh.first + b * kBatch + tid, n = sh.whole_end - j, lo = sh.whole_lo - j;
 #pragma unroll
-                    for (int u = 0; u < kUnroll; ++u)
+                    for (int u = 0; u < kUnroll; ++u) {
                         if (u * kThreads < n && u * kThreads >= lo) __stcs(dst + b * kBatch + u * kThreads, v[u]);
+                        else if (j + u * kThreads < sh.last) store_vector(grad_row, sh, j + u * kThreads, true, v[u]);   // the row's first and last
+                    }
                 }
             }
-            // the row's first and last vector, where it shares them with its neighbours: read again
-            const int edge = sh.first + tid < sh.whole_lo ? sh.first + tid
-                             : sh.last > sh.whole_hi && (sh.last - 1 - sh.first) % kThreads == tid ? sh.last - 1 : -1;
-            if (edge >= 0) store_vector(grad_row, sh, edge, true, grad_vector<T, kOp>(sh.load(edge), a.m, c, shift, g));
-            if (edge >= 0 && edge < sh.whole_lo && sh.last > sh.whole_hi && sh.last - 1 != edge && (sh.last - 1 - sh.first) % kThreads == tid)
-                store_vector(grad_row, sh, sh.last - 1, true, grad_vector<T, kOp>(sh.load(sh.last - 1), a.m, c, shift, g));
         } else {
             for (int b = 0; b < n_batches; ++b) {
                 uint4* slot = stash + b * kBatch + tid;
@@ -367,17 +377,15 @@ rows_resident_kernel(const RowsParams P) {
                 }
                 RowVec<T>::put(grad_row + te.id, fmaf(f.top, ex2((te.x - a.m) * c), -w * q));
             }
-            if (rank == 0 && P.out_loss != nullptr && warp == kWarps - 1) {
-                // one warp, while the others go on
+            if (rank == 0 && tid == kThreads - 32) {
                 const double scale = P.tail == DM_TAIL_RENORM ? (q_sum != 0.0 ? 1.0 / q_sum : 0.0) : 1.0;
-                const float loss = teacher_loss(P, a, ss.t_id[par], ss.t_v[par], ss.t_x[par], ss.t_q[par], q_sum, q_sum * scale,
-                                                rest != 0.0f ? 1.0 - q_sum : 0.0);
-                if (lane == 0) P.out_loss[row] = loss;
+                ss.loss = PendingLoss{a, q_sum, q_sum * scale, rest != 0.0f ? 1.0 - q_sum : 0.0, P.out_loss != nullptr ? row : -1};
             }
         }
         sh = next;
         row = next_row;
     }
+    finish_loss(last_par);
 }
 
 template <typename T, int kOp>
