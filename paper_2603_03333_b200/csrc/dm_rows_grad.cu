@@ -198,18 +198,6 @@ rows_resident_kernel(const RowsParams P) {
                 const float vm = warp_max(te.v);
                 if (lane == 0) ss.t_max[warp] = vm;
             }
-            __syncthreads();
-            if (warp < kTeacherWarps) {   // q in fp64, relative to the largest value (renorm)
-                float vm = ss.t_max[0];
-#pragma unroll
-                for (int i = 1; i < kTeacherWarps; ++i) vm = fmaxf(vm, ss.t_max[i]);
-                const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
-                if (te.id >= 0) te.q = exp((double)te.v - shift);
-                double sum = te.q;
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
-                if (lane == 0) ss.t_sum[warp] = sum;
-            }
         }
 
         // A row whose gradient is zero whatever it holds is not looked at (unless its loss is wanted).
@@ -252,12 +240,6 @@ rows_resident_kernel(const RowsParams P) {
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + tid];
                 thread_max = max_nan(thread_max, RowVec<T>::vmax(v));
-                if (bucket) {   // the teacher's tokens leave the share: what is left is the tail
-                    for (uint32_t marks = reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid]; marks != 0u; marks &= marks - 1u) {
-                        const int bit = __ffs(marks) - 1;
-                        RowVec<T>::put(reinterpret_cast<T*>(stash + b * kBatch + (bit >> 3) * kThreads + tid) + (bit & 7), neg_inf());
-                    }
-                }
             }
             const float warp_top = warp_max_nan(thread_max);
             if (lane == 0) ss.w_max[warp] = warp_top;
@@ -265,6 +247,24 @@ rows_resident_kernel(const RowsParams P) {
             float m = ss.w_max[0];
 #pragma unroll
             for (int i = 1; i < kWarps; ++i) m = max_nan(m, ss.w_max[i]);
+            if (kTail) {
+                // the teacher's tokens leave the share by their threads' hands: what is left is the tail
+                if (bucket) {
+                    if (te.first) RowVec<T>::put(reinterpret_cast<T*>(stash) + (te.id + sh.phase - sh.first * N), neg_inf());
+                    __syncthreads();
+                }
+                if (warp < kTeacherWarps) {   // q in fp64, relative to the largest value (renorm)
+                    float vm = ss.t_max[0];
+#pragma unroll
+                    for (int i = 1; i < kTeacherWarps; ++i) vm = fmaxf(vm, ss.t_max[i]);
+                    const double shift = P.tail == DM_TAIL_RENORM && vm > neg_inf() ? (double)vm : 0.0;
+                    if (te.id >= 0) te.q = exp((double)te.v - shift);
+                    double sum = te.q;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, off);
+                    if (lane == 0) ss.t_sum[warp] = sum;
+                }
+            }
             Stats st;
             st.init();
             st.set_maximum<T>(m, c, P.gap);
@@ -296,7 +296,7 @@ rows_resident_kernel(const RowsParams P) {
         if (more) load_small(next_row);
         const Merged a = need_stats ? merge_parts<kEntropy, kTail>(ss.part[par], n_cta * kWarps, c) : Merged{0.0f, 0.0f, 0.0f, 0.0f};
         const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
-        // (the pass that reads the bitmap is over; so is the row before's use of its counters)
+        // (the marks have served; so have the counters of the row before)
         if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
         if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = 0;
         float mass = 0.0f, rest = 0.0f, q = 0.0f;   // sum of the teacher's q, mass of its bucket, this thread's q
