@@ -89,6 +89,9 @@ template <> struct RowVec<float> {
         if (__uint_as_float(v.w) == m) { eq |= 8u; v.w = 0xFF800000u; }
         return eq;
     }
+    // ... counted only
+    __device__ static void take_count(uint4& v, float m, uint32_t& n) { n += __popc(take(v, m)); }
+    __device__ static int counted(uint32_t n) { return (int)n; }
     __device__ static float get(const float* p) { return *p; }
     // ... issued here and now, though the value is needed only at the end of the row
     __device__ static float get_early(const float* p) {
@@ -166,6 +169,18 @@ template <> struct RowVec<__nv_bfloat16> {
         const uint32_t mm = (__float_as_uint(m) >> 16) * 0x10001u;
         return take_pair(v.x, mm) | (take_pair(v.y, mm) << 2) | (take_pair(v.z, mm) << 4) | (take_pair(v.w, mm) << 6);
     }
+    // ... counted only, in the two halves of a word
+    __device__ static void take_count_pair(uint32_t& v, uint32_t mm, uint32_t& n) {
+        uint32_t eq;
+        asm("set.eq.u32.bf16x2 %0, %1, %2;" : "=r"(eq) : "r"(v), "r"(mm));
+        v = (v & ~eq) | (0xFF80FF80u & eq);
+        n += eq & 0x00010001u;
+    }
+    __device__ static void take_count(uint4& v, float m, uint32_t& n) {
+        const uint32_t mm = (__float_as_uint(m) >> 16) * 0x10001u;
+        take_count_pair(v.x, mm, n); take_count_pair(v.y, mm, n); take_count_pair(v.z, mm, n); take_count_pair(v.w, mm, n);
+    }
+    __device__ static int counted(uint32_t n) { return (int)((n & 0xFFFFu) + (n >> 16)); }
     __device__ static float get(const __nv_bfloat16* p) {
         return __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(p) << 16);
     }
@@ -260,11 +275,18 @@ struct Stats {
     // Entries equal to the maximum are counted and taken out of the batch.
     template <typename T, bool kTail>
     __device__ __forceinline__ void take(uint4 (&v)[kUnroll], uint32_t marks) {
+        if constexpr (kTail) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const uint32_t eq = RowVec<T>::take(v[u], m);
-            cnt += __popc(eq);
-            if (kTail) tail = fmaf((float)__popc(eq & ~(marks >> (8 * u))), of_maximum(), tail);
+            for (int u = 0; u < kUnroll; ++u) {
+                const uint32_t eq = RowVec<T>::take(v[u], m);
+                cnt += __popc(eq);
+                tail = fmaf((float)__popc(eq & ~(marks >> (8 * u))), of_maximum(), tail);
+            }
+        } else {
+            uint32_t n = 0u;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) RowVec<T>::take_count(v[u], m, n);
+            cnt += RowVec<T>::counted(n);
         }
     }
     // A batch of entries below the maximum.  marks: the teacher's tokens in it (see mark_word); most warps
