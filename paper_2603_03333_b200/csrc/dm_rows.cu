@@ -14,9 +14,11 @@
 // block, CTAs through distributed shared memory.  Sums never contain the row's largest entry, so that
 // log(1 + rest) keeps its precision next to a near-certain token.
 //
-// Bound: memory, one read of x.  Measured on 622 MB of bf16 logits (2047 rows of 151936): 109 us for the
-// sums (5.7 TB/s, 0.87 of a measured copy's rate), 119 us with the 5 largest entries, 141 us with 20, 183 us
-// with 100; two thirds of the issue slots are taken by then.  Few rows are bound by latency: some 12 us for
+// Bound: memory, one read of x.  Measured on 622 MB of bf16 logits (2047 rows of 151936): 106 us for the
+// sums (5.9 TB/s, 0.90 of a measured copy's rate), 117 us with the 5 largest entries, 139 us with 20, 181 us
+// with 100 (under sustained load, at the clock the power cap leaves, 121, 133 and 149); two thirds of the
+// issue slots are taken.  Batches of six vectors per thread with three CTAs per SM were slower (146 against
+// 136 us).  Few rows are bound by latency: some 12 us for
 // one row of 128256.
 #include <cooperative_groups.h>
 

@@ -11,14 +11,15 @@
 // memory ahead of one cluster barrier.
 //
 // Bound: memory, one read and one write of the row.  Measured: distillation with its gradient, 1024
-// rows of 128256 bf16 (525 MB in all), 133 us = 4.0 TB/s; gradient of log-probability and entropy, 513
-// rows of 128256 fp32 (526 MB), 106 us = 5.0 TB/s; 1021 rows of 32003 bf16 (131 MB), 41 us = 3.2 TB/s.
-// What keeps it there is the chain of a row: of some 26 thousand cycles that a CTA spends on 64 KB,
-// its barriers, sums, merge and teacher take a third, the two exponentials per entry (16 per cycle and
-// SM) the rest; three CTAs per SM hide half of it.  Tried: shares of 32 KB with five CTAs per SM (step
-// 173-195 us: the fixed part doubles), shares held in registers with the next row always in flight (two
-// CTAs per SM: 181 us), every warp merging for itself with two barriers less (142 us), CTAs of 128 and
-// 512 threads.
+// rows of 128256 bf16 (525 MB in all), 118 us = 4.5 TB/s; gradient of log-probability and entropy, 513
+// rows of 128256 fp32 (526 MB), 100 us = 5.3 TB/s; 1021 rows of 32003 bf16 (131 MB), 38 us = 3.5 TB/s.
+// What keeps it there is the chain of a row: of some 21 thousand cycles that a CTA spends on 64 KB, the
+// two passes with exponentials (16 per cycle and SM) take 8, waiting for the cluster 3 to 4, barriers,
+// sums, merge and the teacher the rest; three CTAs per SM hide half of it.  Tried, on the step: shares of
+// 32 KB with five CTAs per SM (the fixed part doubles), shares held in registers with the next row always
+// in flight (two CTAs per SM: 181 against 134 us at the time), a maximum per warp in place of the block's
+// (142 against 138), sums sent with asynchronous stores that count on a barrier instead of the cluster
+// barrier (136 against 127), CTAs of 128 and 512 threads.
 #include <cooperative_groups.h>
 
 #include "dm_ptx.cuh"
@@ -100,7 +101,7 @@ rows_resident_kernel(const RowsParams P) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ ResidentShared ss;
     uint4* stash = reinterpret_cast<uint4*>(smem);                                    // [stash_vecs]
-    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);   // distill: teacher tokens of the share, a byte per vector
+    unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);   // distill: teacher tokens of the share, a byte per vector: tells repeated ones apart
     cg::cluster_group cluster = cg::this_cluster();
     const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     if (n_cta > 1) cluster_arrive();   // (waited for before anything is written to another CTA's shared memory)
