@@ -251,6 +251,10 @@ rows_resident_kernel(const RowsParams P) {
             if (kTail) {
                 // the teacher's tokens leave the share by their threads' hands: what is left is the tail
                 if (bucket) {
+                    if (ss.t_repeated[par] != 0 && te.id >= 0) {   // of those that name one token the first counts, whichever was faster
+                        te.first = my_word != nullptr;
+                        for (int o = 0; o < tid; ++o) te.first = te.first && ss.t_id[par][o] != te.id;
+                    }
                     if (te.first) RowVec<T>::put(reinterpret_cast<T*>(stash) + (te.id + sh.phase - sh.first * N), neg_inf());
                     __syncthreads();
                 }

@@ -532,10 +532,9 @@ def test_many_rows_of_every_kind(ctx, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("V", [1001, 30011])
-def test_many_rows_in_place(ctx, dtype, V):
+@pytest.mark.parametrize("rows,V", [(1200, 1001), (1200, 30011), (170, 128256)])
+def test_many_rows_in_place(ctx, dtype, rows, V):
     """The next row is on its way while a row's gradient takes the place of its logits."""
-    rows = 1200
     x, g = make(rows, V, dtype, ld=V + 2)
     tok = tokens_for(rows, V, g)
     g_lp, g_h = torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV)
@@ -555,6 +554,17 @@ def test_many_rows_in_place(ctx, dtype, V):
         call(whole[:, :V], whole[:, :V])
         assert torch.equal(whole[:, :V], want) and (whole[:-1, V:] == 77.0).all()
     assert ctx.device_error() == 0
+
+
+@pytest.mark.parametrize("tail", [0, 1], ids=["renorm", "bucket"])
+def test_repeated_tokens_give_the_same_bits_every_time(ctx, tail):
+    x, g = make(600, 5001, torch.bfloat16)
+    ids = torch.randint(-1, 60, (600, 100), generator=g, device=DEV, dtype=torch.int32)
+    v = torch.log_softmax(torch.randn((600, 100), generator=g, device=DEV), 1) - 0.3
+    first = check_distill(ctx, x, ids, v, tail, 1.0)
+    for _ in range(20):
+        again = ctx.distill(x, ids, v, tail=tail, grad=True)
+        assert torch.equal(again["grad"], first["grad"]) and torch.equal(again["loss"], first["loss"])
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
