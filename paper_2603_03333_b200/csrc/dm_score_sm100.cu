@@ -301,8 +301,9 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         for (int b = 0; b < 2; ++b) {
             if (b >= P.n_blk || row[b] - lane >= P.rows) continue;     // (the same for the whole warp)
             const int n_here = min(tile == n_tiles - 1 ? P.last_n : P.tile_n, v_end - (v_slice + tile * P.tile_n));
+            int n0 = 32 * set;
 #pragma unroll 1
-            for (int n0 = 32 * set; n0 < n_here; n0 += 64) {
+            for (; n0 < n_here; n0 += 64) {
                 uint32_t acc[32];
                 ptx::tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((slot * P.n_blk + b) * kTileN + n0), acc);
                 ptx::tmem_ld_wait();
@@ -350,6 +351,11 @@ score_head_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 rec[b] = merge(rec[b], group_record(x, gm, P.c), P.c);
                 __syncwarp();
             }
+            // groups that hold nothing (a last tile shorter than the others, the end of the vocabulary) say so
+            if (P.group_max != nullptr && row[b] < P.rows) {
+                for (; n0 < 32 * P.groups_per_tile; n0 += 64)
+                    P.group_max[(size_t)row[b] * P.n_groups + (size_t)slice * P.groups_per_slice + tile * P.groups_per_tile + (n0 >> 5)] = neg_inf();
+            }
         }
         ptx::tc_fence_before();
         __syncwarp();
@@ -395,7 +401,7 @@ constexpr int kFinOwn = 20;     // maxima of groups a thread keeps in registers 
 
 struct FinishParams {
     int rows, V, n_records, groups_per_tile, n_tiles, slice, tile_n;
-    int n_groups, n_written;   // groups per row (stride), and how many of them lie within the vocabulary (the first ones)
+    int n_groups;              // per row; a maximum of -inf: nothing in it, its logits are not written
     float c, inv_temp;
     const float4* records;
     const float *tok_logit, *group_max, *logits;
@@ -433,12 +439,12 @@ score_finish_kernel(const FinishParams P) {
     float thread_max = neg_inf();
     if (P.n_top > 0) {
 #pragma unroll
-        for (int i = 0; i < kFinOwn; ++i) own[i] = i * kFinThreads + tid < P.n_written ? gm[i * kFinThreads + tid] : neg_inf();
+        for (int i = 0; i < kFinOwn; ++i) own[i] = i * kFinThreads + tid < P.n_groups ? gm[i * kFinThreads + tid] : neg_inf();
 #pragma unroll
         for (int i = 0; i < kFinOwn; ++i) thread_max = fmaxf(thread_max, own[i]);
 #pragma unroll 4
-        for (int g = kFinOwn * kFinThreads + tid; g < P.n_written; g += kFinThreads) thread_max = fmaxf(thread_max, gm[g]);
-        s_key[tid] = tid < P.n_written ? float_key(thread_max) : 0u;
+        for (int g = kFinOwn * kFinThreads + tid; g < P.n_groups; g += kFinThreads) thread_max = fmaxf(thread_max, gm[g]);
+        s_key[tid] = tid < P.n_groups ? float_key(thread_max) : 0u;
     }
     Record r{neg_inf(), 0.0f, 0.0f};
     for (int i = tid; i < P.n_records; i += kFinThreads) {
@@ -490,9 +496,9 @@ score_finish_kernel(const FinishParams P) {
         };
 #pragma unroll
         for (int i = 0; i < kFinOwn; ++i)
-            if (i * kFinThreads + tid < P.n_written && float_key(own[i]) >= thr) take(i * kFinThreads + tid);
-        for (int g = kFinOwn * kFinThreads + tid; g < P.n_written; g += kFinThreads)
-            if (float_key(gm[g]) >= thr) take(g);
+            if (own[i] > neg_inf() && float_key(own[i]) >= thr) take(i * kFinThreads + tid);
+        for (int g = kFinOwn * kFinThreads + tid; g < P.n_groups; g += kFinThreads)
+            if (gm[g] > neg_inf() && float_key(gm[g]) >= thr) take(g);
     }
     __syncthreads();
     const float* logits = P.logits + (size_t)row * P.n_groups * 32 + lane;
@@ -517,8 +523,8 @@ score_finish_kernel(const FinishParams P) {
             __syncthreads();
             if (tid == 0) s_n = 0;
             __syncthreads();
-            for (int g = warp; g < P.n_written; g += kFinWarps) {
-                if (float_key(gm[g]) < (uint32_t)(c >> 32)) continue;
+            for (int g = warp; g < P.n_groups; g += kFinWarps) {
+                if (!(gm[g] > neg_inf()) || float_key(gm[g]) < (uint32_t)(c >> 32)) continue;
                 const float x = logits[(size_t)g * 32];
                 const unsigned long long word = pack_best(float_key(x), (uint32_t)(group_first(P, g) + lane));
                 if (x != neg_inf() && word >= c) {
@@ -686,9 +692,6 @@ int launch_score(const ScoreState* st, const HeadDesc& head, const void* H, cons
     }
     FinishParams F{};
     F.rows = rp.rows; F.V = head.V; F.n_records = 2 * cut.n_slices; F.n_groups = P.n_groups;
-    // groups up to the end of the vocabulary: full tiles, then the groups that the last tile reaches into
-    const int in_last = head.V - (cut.n_slices - 1) * cut.slice;
-    F.n_written = (cut.n_slices - 1) * P.groups_per_slice + in_last / cut.tile_n * cut.groups_per_tile + (in_last % cut.tile_n + 31) / 32;
     F.groups_per_tile = cut.groups_per_tile; F.n_tiles = cut.n_tiles; F.slice = cut.slice; F.tile_n = cut.tile_n;
     F.c = rp.c; F.inv_temp = rp.inv_temp;
     F.records = P.records; F.tok_logit = P.tok_logit; F.group_max = P.group_max; F.logits = P.logits;

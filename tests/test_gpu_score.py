@@ -222,3 +222,21 @@ def test_score_workspace_is_counted_and_replaced():
         assert e.value.status == binding.EWORKSPACE
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("V", [47253, 77745, 103093, 128256])
+def test_alternatives_after_calls_of_other_sizes(V):
+    """Whatever earlier calls have left in the workspace: both cuts of the vocabulary, last tiles shorter than
+    the others, fewer rows than before."""
+    W, H = inputs(300, V, 64, torch.bfloat16)
+    big = H * 16
+    ctx = pk.Context(0)
+    try:
+        ctx.set_head(W, max_rows=300)
+        ctx.enable_score(300, 40)
+        for rows in (300, 27, 130, 128, 1, 257):
+            ctx.score(big, None, n_top=40)
+            ctx.score(big[:128], None, n_top=40)
+            check(ctx.score(H[:rows], None, n_top=9), W, H[:rows], None, 9, 1.0)
+    finally:
+        ctx.close()
