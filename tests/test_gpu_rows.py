@@ -584,3 +584,16 @@ def test_nan_or_infinity_anywhere_in_a_row(ctx, dtype, value):
                 assert torch.isnan(got[:5]).all() and torch.isfinite(got[5:]).all()
             assert torch.isnan(both["grad"][:5]).any(1).all() and torch.isfinite(both["grad"][5:]).all()
             check_distill(ctx, x[5:], ids[5:], v[5:], tail, 1.0)
+
+
+def test_a_tail_below_the_range_of_fp32(ctx):
+    """Less than 1e-38 of the row's mass outside the teacher's tokens: an infinite loss, a finite gradient."""
+    x = torch.full((3, 500), -400.0, device=DEV)
+    x[:, :2] = 0.0
+    x[2] = 0.0
+    ids = torch.tensor([[0, 1]] * 3, dtype=torch.int32, device=DEV)
+    v = torch.log(torch.full((3, 2), 0.25, device=DEV))
+    res = ctx.distill(x, ids, v, tail=binding.TAIL_BUCKET, grad=True)
+    assert torch.isinf(res["loss"][:2]).all() and (res["loss"][:2] > 0).all() and torch.isfinite(res["loss"][2])
+    assert torch.isfinite(res["grad"]).all()
+    assert torch.equal(ctx.distill(x, ids, v, tail=binding.TAIL_BUCKET)["loss"][:2], res["loss"][:2])
