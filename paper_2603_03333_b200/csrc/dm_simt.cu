@@ -129,7 +129,11 @@ static int launch_simt_rc(const HeadDesc& head, const void* H, int rows, const R
     if (v_per_block < 8) v_per_block = 8;
     const int n_slices = (head.V + v_per_block - 1) / v_per_block;
     auto kern = simt_head_kernel<T, RC>;
-    if (smem > 48 * 1024 &&   // (a microsecond of host time that smaller launches need not spend)
+    // A launch may ask for 48 KB without a raised limit, the kernel's own arrays included (544 bytes for
+    // eight rows).  Below that the call, a microsecond of host time, is left out.
+    constexpr size_t own = 8 * RC * sizeof(unsigned long long) + RC * sizeof(int), margin = 1024;
+    static_assert(own <= margin, "the kernel's own shared arrays");
+    if (smem > 48 * 1024 - margin &&
         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
         return DM_ECUDA;
     kern<<<n_slices, 256, smem, stream>>>(static_cast<const T*>(head.W), static_cast<const T*>(H),
