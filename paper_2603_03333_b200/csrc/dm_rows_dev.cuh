@@ -13,6 +13,10 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;             // vectors of a batch: 16-byte loads in flight per thread
 constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 0 in fp32, and 0 * clamp stays 0
+// Exponents are taken against the rounded product m c while that is below this: its rounding error is then
+// at most 64, half a step of fp32.  From here on the next number below m lies 2^-24 |m| or more away, 128
+// powers of two: nothing next to m.
+constexpr float kExactShift = 2147483648.0f;   // 2^31
 constexpr size_t kRowsSmemLimit = 216 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -252,8 +256,8 @@ template <typename T> struct Share {
 
 // Running statistics of a warp's entries.  Exponents are taken against rc, the rounded product m * c:
 // w(x) = fma(x, ce, -rc) is then off by one rounding only; finish() moves the sums to m itself.  Where
-// |m| c is beyond 1e37 (a row of nothing but the type's lowest value, say) every other entry is
-// thousands of powers of two below m and adds nothing: ce = 0 says so.
+// |m| c reaches kExactShift (rows filled with -1e10 or the type's lowest value, temperatures near 0) every
+// other entry is nothing next to m: ce = 0 says so.
 struct Stats {
     float m, rc, ce;          // the warp's maximum (all lanes alike), and how exponents are taken
     uint32_t floor2;          // bf16: entries below this are raised to it (250 powers of two below m)
@@ -268,7 +272,7 @@ struct Stats {
     template <typename T> __device__ __forceinline__ void set_maximum(float top, float c, float gap) {
         m = top;
         rc = top * c;
-        ce = fabsf(rc) <= 1e37f ? c : 0.0f;
+        ce = fabsf(rc) < kExactShift ? c : 0.0f;
         floor2 = RowVec<T>::floor_word(top - gap);
         cnt = 0;
     }
@@ -367,7 +371,7 @@ struct Stats {
     }
     __device__ __forceinline__ void finish() {
         if (ce == 0.0f) return;
-        const float d = fminf(fmaxf(fmaf(m, ce, -rc), -100.0f), 100.0f), f = ex2(-d);   // rounding of rc: tiny, either sign
+        const float d = fmaf(m, ce, -rc), f = ex2(-d);   // rounding of rc, either sign: at most 64
         t = f * fmaf(-d, s, t);
         s *= f;
         tail *= f;

@@ -1,0 +1,70 @@
+"""The operators on rows of logits at the ends of their range: large magnitudes, small temperatures, tails that are
+nearly nothing, rows without a teacher.  Statements and error bounds are those of rows_ref.py."""
+import pytest
+import torch
+
+import paper_2603_03333_b200 as pk
+from paper_2603_03333_b200 import binding
+from test_gpu_rows import check_distill, check_logprobs, make, teacher_for
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NINF = float("-inf")
+DTYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+# rows of one CTA, rows shared by a cluster, rows that are read twice
+LENGTHS = pytest.mark.parametrize("V", [1000, 40001, 500_003])
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = pk.Context(0)
+    yield c
+    c.close()
+
+
+FILLS = [-1e9, -1.4e9, -1.6e9, -1e10, -1e12, -1e20, -1e30, 1e10, 1e30]
+
+
+def large_rows(V, dtype):
+    """One row of each fill, then each as the one entry among ordinary ones, then each among its double."""
+    x, g = make(3 * len(FILLS), V, dtype)
+    n = len(FILLS)
+    for r, value in enumerate(FILLS):
+        x[r] = value
+        x[n + r, V // 3] = value
+        x[2 * n + r] = 2 * value
+        x[2 * n + r, V // 5::7] = value
+    return x, g
+
+
+@DTYPES
+@LENGTHS
+@pytest.mark.parametrize("T", [1.0, 0.37])
+def test_statistics_of_large_logits(ctx, dtype, V, T):
+    x, g = large_rows(V, dtype)
+    tok = torch.full((x.shape[0],), V // 3, dtype=torch.int32, device=DEV)
+    check_logprobs(ctx, x, tok, 5, T)
+    check_logprobs(ctx, x, tok + 1, 0, T)
+    for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+        ids = torch.randint(0, V, (x.shape[0], 6), generator=g, device=DEV, dtype=torch.int32)
+        ids[::2, 1] = V // 3
+        v = torch.log_softmax(torch.randn(ids.shape, generator=g, device=DEV), 1) - 0.5
+        check_distill(ctx, x, ids, v, tail, T, None, grad=False)
+
+
+SMALL = pytest.mark.parametrize("exponent", [-26, -28, -30, -40, -66, -96])   # powers of two: 1 / T is exact
+
+
+@DTYPES
+@LENGTHS
+@SMALL
+def test_statistics_at_small_temperatures(ctx, dtype, V, exponent):
+    """Ordinary logits are then a certain token, or equal ones."""
+    T = 2.0 ** exponent
+    x, g = make(4, V, dtype)
+    tok = torch.tensor([0, V - 1, -1, 0], dtype=torch.int32, device=DEV)
+    tok[3] = x[3].argmax()
+    check_logprobs(ctx, x, tok, 5, T)
+    ids, v = teacher_for(x, 8, g, T, pad=False)
+    for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+        check_distill(ctx, x, ids, v, tail, T, None, grad=False)
