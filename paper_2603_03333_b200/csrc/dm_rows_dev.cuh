@@ -17,6 +17,7 @@ constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 
 // at most 64, half a step of fp32.  From here on the next number below m lies 2^-24 |m| or more away, 128
 // powers of two: nothing next to m.
 constexpr float kExactShift = 2147483648.0f;   // 2^31
+constexpr float kSmallShift = 16777216.0f;     // 2^24: the error is at most half a power of two, and may scale any factor
 constexpr size_t kRowsSmemLimit = 216 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -465,8 +466,8 @@ __device__ __forceinline__ float token_grad(float x, const Merged& a, float c, f
     return fmaf(w * g_lp, one_less, by_entropy);
 }
 // A vector of the row -> the same vector of its gradient.  shift: the rounded product m c, whose rounding
-// error `factors_against` has moved into the factors; where m c is too large for that, exponents are
-// taken of differences (kPlain).
+// error `factors_against` has moved into the factors; where m c reaches kSmallShift exponents are taken of
+// differences (kPlain).
 struct GradShift { float rc; uint32_t floor2; };
 template <typename T, int kOp, bool kPlain = false>
 __device__ __forceinline__ uint4 grad_vector(uint4 v, float m, float c, const GradShift& g, const GradFactors& f) {
@@ -487,7 +488,7 @@ __device__ __forceinline__ uint4 grad_vector(uint4 v, float m, float c, const Gr
     }
     return RowVec<T>::pack_pairs(x);
 }
-// With z' = z + d for every entry (d = m c - rc, tiny): 2^z (A + B z) = 2^z' 2^-d (A - B d + B z').
+// With z' = z + d for every entry (d = m c - rc, at most 1/2 either way): 2^z (A + B z) = 2^z' 2^-d (A - B d + B z').
 __device__ __forceinline__ GradFactors factors_against(const GradFactors& f, float d) {
     const float scale = ex2(-d);
     return GradFactors{scale * fmaf(-d, f.B, f.A), scale * f.B, f.top};

@@ -321,7 +321,7 @@ rows_resident_kernel(const RowsParams P) {
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
         const bool none = zero_grad || dead;
         const float rc = a.m * c;
-        const bool plain = !(fabsf(rc) <= 1e37f);
+        const bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
         const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                              : distill_factors(w, mass, rest, a.tail, inv_total);
 

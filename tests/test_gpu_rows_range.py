@@ -5,7 +5,7 @@ import torch
 
 import paper_2603_03333_b200 as pk
 from paper_2603_03333_b200 import binding
-from test_gpu_rows import check_distill, check_logprobs, make, teacher_for
+from test_gpu_rows import check_distill, check_grad, check_logprobs, make, teacher_for
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -20,6 +20,10 @@ def ctx():
     c = pk.Context(0)
     yield c
     c.close()
+
+
+def factors(rows, g):
+    return torch.randn(rows, generator=g, device=DEV), torch.randn(rows, generator=g, device=DEV)
 
 
 FILLS = [-1e9, -1.4e9, -1.6e9, -1e10, -1e12, -1e20, -1e30, 1e10, 1e30]
@@ -52,6 +56,25 @@ def test_statistics_of_large_logits(ctx, dtype, V, T):
         check_distill(ctx, x, ids, v, tail, T, None, grad=False)
 
 
+@DTYPES
+@LENGTHS
+@pytest.mark.parametrize("T", [1.0, 0.37])
+def test_gradients_at_large_logits(ctx, dtype, V, T):
+    x, g = large_rows(V, dtype)
+    rows = x.shape[0]
+    tok = torch.full((rows,), V // 3, dtype=torch.int32, device=DEV)
+    g_lp, g_h = factors(rows, g)
+    for at in (tok, tok + 1):
+        check_grad(ctx, x, at, g_lp, g_h, T)
+        check_grad(ctx, x, at, g_lp, None, T)
+    ids = torch.randint(0, V, (rows, 6), generator=g, device=DEV, dtype=torch.int32)
+    ids[::2, 1] = V // 3
+    v = torch.log_softmax(torch.randn(ids.shape, generator=g, device=DEV), 1) - 0.5
+    w = torch.rand(rows, generator=g, device=DEV) + 0.1
+    for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+        check_distill(ctx, x, ids, v, tail, T, w)
+
+
 SMALL = pytest.mark.parametrize("exponent", [-26, -28, -30, -40, -66, -96])   # powers of two: 1 / T is exact
 
 
@@ -68,3 +91,18 @@ def test_statistics_at_small_temperatures(ctx, dtype, V, exponent):
     ids, v = teacher_for(x, 8, g, T, pad=False)
     for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
         check_distill(ctx, x, ids, v, tail, T, None, grad=False)
+
+
+@DTYPES
+@LENGTHS
+@SMALL
+def test_gradients_at_small_temperatures(ctx, dtype, V, exponent):
+    T = 2.0 ** exponent
+    x, g = make(4, V, dtype)
+    tok = torch.tensor([0, V - 1, -1, 0], dtype=torch.int32, device=DEV)
+    tok[3] = x[3].argmax()
+    g_lp, g_h = factors(4, g)
+    check_grad(ctx, x, tok, g_lp, g_h, T)
+    ids, v = teacher_for(x, 8, g, T, pad=False)
+    for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+        check_distill(ctx, x, ids, v, tail, T)
