@@ -58,6 +58,7 @@ struct RowsShared {
     float t_max[kRowsMaxTop / 32];
     double t_sum[kRowsMaxTop / 32];
     int t_distinct, t_repeated;
+    float raised[kRowsMaxCluster * kWarps];   // parts of a tail that is summed anew, from every CTA
 };
 
 // The block's statistics from its warps', written to every CTA of the cluster (complete behind the
@@ -494,7 +495,7 @@ rows_kernel(const RowsParams P) {
             }
         }
         __syncthreads();
-        const Merged a = ss.all;
+        Merged a = ss.all;
         const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
         const float log_total = ss.log_total, inv_total = ss.inv_total;
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
@@ -539,6 +540,7 @@ rows_kernel(const RowsParams P) {
         }
 
         float mass = 0.0f, rest = 0.0f;   // sum of the teacher's q, mass of its bucket (0: no bucket)
+        float raised = -1.0f;             // the tail where it was summed anew
         if (kOp == OP_DISTILL) {
             double sum = 0.0;
 #pragma unroll
@@ -549,6 +551,30 @@ rows_kernel(const RowsParams P) {
             if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
             if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
             __syncthreads();
+            if (P.tail == DM_TAIL_BUCKET && need_stats && small_tail(a)) {   // the row is read again
+                raised = 0.0f;
+                for (int b = 0; b < n_batches; ++b) {
+                    uint4 v[kUnroll];
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u) {
+                        const int j = sh.first + b * kBatch + u * kThreads + tid;
+                        v[u] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
+                    }
+                    raised += raised_sum<T>(v, reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid], a.m, c);
+                }
+                raised = warp_sum(raised);
+                if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->raised[rank * kWarps + warp] = raised;
+                if (n_cta == 1) {
+                    __syncthreads();
+                } else {
+                    __syncwarp();
+                    cluster_arrive();
+                    cluster_wait();
+                }
+                raised = (lane < n_cta * kWarps ? ss.raised[lane] : 0.0f) + (lane + 32 < n_cta * kWarps ? ss.raised[lane + 32] : 0.0f);
+                raised = counted_tail(warp_sum(raised), inv_total);
+                a.tail = raised * kTailInv;
+            }
             if (rank == 0 && warp == kWarps - 1 && P.out_loss != nullptr) {
                 const float loss = teacher_loss(P, a, ss.t_id, ss.t_v, ss.t_x, ss.t_q, sum, sum * scale, rest != 0.0f ? 1.0 - sum : 0.0);
                 if (lane == 0) P.out_loss[row] = loss;
@@ -558,7 +584,8 @@ rows_kernel(const RowsParams P) {
         if (kOp != OP_LOGPROBS && grad_row != nullptr) {
             const bool none = zero_grad || dead;
             const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
-                                                 : distill_factors(w, mass, rest, a.tail, inv_total);
+                                  : raised < 0.0f ? distill_factors(w, mass, rest, a.tail, inv_total)
+                                                  : raised_factors(w, mass, rest, raised, inv_total);
             const bool same_phase = phase_of(grad_row, sh.phase);
 #pragma unroll 4
             for (int j = sh.first + tid; j < sh.last; j += kThreads)

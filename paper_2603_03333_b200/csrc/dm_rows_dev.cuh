@@ -18,6 +18,10 @@ constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 
 // powers of two: nothing next to m.
 constexpr float kExactShift = 2147483648.0f;   // 2^31
 constexpr float kSmallShift = 16777216.0f;     // 2^24: the error is at most half a power of two, and may scale any factor
+// A tail of less than 2^-60 is summed anew, 2^64 times as large: 2^-126 of the row's mass may consist of
+// entries far below fp32's range.
+constexpr float kTailSmall = 8.673617379884035e-19f;   // 2^-60
+constexpr float kTailUp = 64.0f, kTailInv = 5.421010862427522e-20f;   // 2^-64
 constexpr size_t kRowsSmemLimit = 216 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -399,6 +403,28 @@ __device__ __forceinline__ float warp_sum(float x) {
     return x;
 }
 
+// A batch's part of a small tail (entries that the teacher's tokens, marked, leave), 2^64 times as large.
+template <typename T>
+__device__ __forceinline__ float raised_sum(const uint4 (&v)[kUnroll], uint32_t marks, float m, float c) {
+    constexpr int N = RowVec<T>::N;
+    float sum = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        float x[N];
+        RowVec<T>::unpack(v[u], x);
+#pragma unroll
+        for (int n = 0; n < N; ++n) sum += (marks >> (8 * u + n)) & 1u ? 0.0f : ex2(fmaf(x[n] - m, c, kTailUp));
+    }
+    return sum;
+}
+// Is the row's tail to be summed anew?  (The same in all CTAs of the cluster.)
+__device__ __forceinline__ bool small_tail(const Merged& a) { return a.tail < kTailSmall && a.m != neg_inf(); }
+
+// Less than 2^-126 of the row's mass counts as nothing.
+__device__ __forceinline__ float counted_tail(float raised, float inv_total) {
+    return raised * inv_total < 2.168404344971009e-19f ? 0.0f : raised;   // 2^(64 - 126)
+}
+
 // ---------------------------------------------------------------------------------- the teacher
 // The teacher of a row is known by k tokens and values v (an id outside [0,V) is an absent entry):
 //   renorm  q = Softmax(v) over the present entries:  L = sum q (log q - log p)
@@ -446,16 +472,25 @@ __device__ __forceinline__ float teacher_loss(const RowsParams& P, const Merged&
 }
 
 // Factors of a gradient, from the row's statistics: with w = (x - m) c in powers of two, every entry's
-// gradient is 2^w (A + B w) (logprobs) or 2^w A (distill, where the teacher's tokens differ: top).
-struct GradFactors { float A, B, top; };
+// gradient is 2^w (A + B w) (logprobs) or 2^(w + up) A (distill, where the teacher's tokens differ: top).
+struct GradFactors { float A, B, top, up; };
 __device__ __forceinline__ GradFactors logprob_factors(float w, float g_lp, float g_h, float entropy, float log_total, float inv_total) {
-    return GradFactors{-w * inv_total * fmaf(g_h, entropy - log_total, g_lp), -w * inv_total * g_h * kLn2, 0.0f};
+    return GradFactors{-w * inv_total * fmaf(g_h, entropy - log_total, g_lp), -w * inv_total * g_h * kLn2, 0.0f, 0.0f};
 }
 // mass: sum of the teacher's q; rest: mass of its bucket (0: no bucket), taken off every entry's share by
 // q_t / (sum of the tail's exponentials)
 __device__ __forceinline__ GradFactors distill_factors(float w, float mass, float rest, float tail, float inv_total) {
     const float share = rest > 0.0f && tail > 0.0f ? rest / tail : 0.0f;
-    return GradFactors{w * fmaf(mass + rest, inv_total, -share), 0.0f, w * (mass + rest) * inv_total};
+    return GradFactors{w * fmaf(mass + rest, inv_total, -share), 0.0f, w * (mass + rest) * inv_total, 0.0f};
+}
+// The same for a tail that was summed anew: `raised`, 2^64 times as large; 0 if it counts as nothing.  The
+// factor is 2^64 times too small and the exponents are raised, so that neither leaves fp32's range (all
+// entries but the teacher's tokens, which are written apart, are small).
+__device__ __forceinline__ GradFactors raised_factors(float w, float mass, float rest, float raised, float inv_total) {
+    if (raised == 0.0f) return distill_factors(w, mass, rest, 0.0f, inv_total);
+    float A = w * fmaf((mass + rest) * kTailInv, inv_total, -rest / raised);
+    if (A == neg_inf()) A = -3.4028234e38f;   // (0 for a masked entry all the same)
+    return GradFactors{A, 0.0f, w * (mass + rest) * inv_total, kTailUp};
 }
 // Gradient at the given token.  1 - p of the largest entry is rest / total, without cancellation.
 __device__ __forceinline__ float token_grad(float x, const Merged& a, float c, float w, float g_lp, float g_h, float entropy,
@@ -466,20 +501,21 @@ __device__ __forceinline__ float token_grad(float x, const Merged& a, float c, f
     return fmaf(w * g_lp, one_less, by_entropy);
 }
 // A vector of the row -> the same vector of its gradient.  shift: the rounded product m c, whose rounding
-// error `factors_against` has moved into the factors; where m c reaches kSmallShift exponents are taken of
-// differences (kPlain).
+// error `factors_against` has moved into the factors; where m c reaches kSmallShift, and for raised exponents,
+// they are taken of differences (kPlain).
 struct GradShift { float rc; uint32_t floor2; };
 template <typename T, int kOp, bool kPlain = false>
 __device__ __forceinline__ uint4 grad_vector(uint4 v, float m, float c, const GradShift& g, const GradFactors& f) {
     constexpr int N = RowVec<T>::N;
-    const f32x2 m2 = kPlain ? pair(-m, -m) : pair(-g.rc, -g.rc), c2 = pair(c, c), A2 = pair(f.A, f.A), B2 = pair(f.B, f.B);
+    const f32x2 m2 = kPlain ? pair(-m, -m) : pair(-g.rc, -g.rc), c2 = pair(c, c), A2 = pair(f.A, f.A), B2 = pair(f.B, f.B),
+                up2 = pair(f.up, f.up);
     constexpr bool kClamp = kOp == OP_GRAD && (kPlain || !RowVec<T>::kFloorsEntries);   // (a masked entry: 0 * a finite exponent)
     if (kOp == OP_GRAD && !kClamp) RowVec<T>::raise(v, g.floor2);
     f32x2 x[N / 2];
     RowVec<T>::pairs(v, x);
 #pragma unroll
     for (int n = 0; n < N / 2; ++n) {
-        f32x2 z = kPlain ? mul2(add2(x[n], m2), c2) : fma2(x[n], c2, m2);
+        f32x2 z = kPlain ? kOp == OP_GRAD ? mul2(add2(x[n], m2), c2) : fma2(add2(x[n], m2), c2, up2) : fma2(x[n], c2, m2);
         if (kClamp) {
             z.x = fmaxf(z.x, kFloorExp);
             z.y = fmaxf(z.y, kFloorExp);
@@ -491,7 +527,7 @@ __device__ __forceinline__ uint4 grad_vector(uint4 v, float m, float c, const Gr
 // With z' = z + d for every entry (d = m c - rc, at most 1/2 either way): 2^z (A + B z) = 2^z' 2^-d (A - B d + B z').
 __device__ __forceinline__ GradFactors factors_against(const GradFactors& f, float d) {
     const float scale = ex2(-d);
-    return GradFactors{scale * fmaf(-d, f.B, f.A), scale * f.B, f.top};
+    return GradFactors{scale * fmaf(-d, f.B, f.A), scale * f.B, f.top, 0.0f};
 }
 // ... and its way to the gradient's row (which may have another alignment).
 template <typename T>

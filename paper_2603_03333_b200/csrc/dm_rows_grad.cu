@@ -57,6 +57,7 @@ struct ResidentShared {
     int t_distinct[2], t_repeated[2];
     float t_max[kTeacherWarps];
     double t_sum[kTeacherWarps];
+    float raised[kRowsMaxCluster * kWarps];   // parts of a tail that is summed anew, from every CTA
     PendingLoss loss;              // of the row before, until its warp finds the time (rank 0)
 };
 
@@ -91,6 +92,34 @@ __device__ __forceinline__ Merged merge_parts(const WarpSums* part, int n, float
     a.rest += fmaxf(warp_sum(cnt) - 1.0f, 0.0f);
     if (!(a.m < __uint_as_float(0x7F800000u))) a.rest = a.t = a.tail = __uint_as_float(0x7FC00000u);   // NaN or +inf: no distribution
     return a;
+}
+
+// The tail of a row that is summed anew, 2^64 times as large, or 0 if it counts as nothing.  By all threads of
+// the cluster, while the shares without the teacher's tokens still lie in shared memory.
+template <typename T>
+__device__ __noinline__ float resident_tail(const uint4* stash, int n_batches, float m, float c, float inv_total, ResidentShared& ss) {
+    cg::cluster_group cluster = cg::this_cluster();
+    const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float raised = 0.0f;
+#pragma unroll 1
+    for (int b = 0; b < n_batches; ++b) {
+        uint4 v[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + threadIdx.x];
+        raised += raised_sum<T>(v, 0u, m, c);
+    }
+    raised = warp_sum(raised);
+    if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->raised[rank * kWarps + warp] = raised;
+    if (n_cta == 1) {
+        __syncthreads();
+    } else {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
+    raised = (lane < n_cta * kWarps ? ss.raised[lane] : 0.0f) + (lane + 32 < n_cta * kWarps ? ss.raised[lane + 32] : 0.0f);
+    return counted_tail(warp_sum(raised), inv_total);
 }
 
 template <typename T, int kOp>
@@ -299,7 +328,7 @@ rows_resident_kernel(const RowsParams P) {
         const int next_row = ss.next_row[par];
         const bool more = next_row >= 0;
         if (more) load_small(next_row);
-        const Merged a = need_stats ? merge_parts<kEntropy, kTail>(ss.part[par], n_cta * kWarps, c) : Merged{0.0f, 0.0f, 0.0f, 0.0f};
+        Merged a = need_stats ? merge_parts<kEntropy, kTail>(ss.part[par], n_cta * kWarps, c) : Merged{0.0f, 0.0f, 0.0f, 0.0f};
         const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
         // (the marks have served; so have the counters of the row before)
         if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
@@ -321,9 +350,15 @@ rows_resident_kernel(const RowsParams P) {
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
         const bool none = zero_grad || dead;
         const float rc = a.m * c;
-        const bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
-        const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
-                                             : distill_factors(w, mass, rest, a.tail, inv_total);
+        bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
+        GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
+                                       : distill_factors(w, mass, rest, a.tail, inv_total);
+        if (kOp == OP_DISTILL && bucket && need_stats && small_tail(a)) {   // (the teacher's tokens have left the share)
+            const float raised = resident_tail<T>(stash, n_batches, a.m, c, inv_total, ss);
+            a.tail = raised * kTailInv;
+            f = raised_factors(w, mass, rest, raised, inv_total);
+            plain = plain || f.up != 0.0f;
+        }
 
         // the gradient; each batch's slots are handed to the next row at once (a thread reads its slots in
         // program order before its copies into them are issued, and only ever touches its own)

@@ -1,10 +1,13 @@
 """The operators on rows of logits at the ends of their range: large magnitudes, small temperatures, tails that are
 nearly nothing, rows without a teacher.  Statements and error bounds are those of rows_ref.py."""
+import math
+
 import pytest
 import torch
 
 import paper_2603_03333_b200 as pk
 from paper_2603_03333_b200 import binding
+import rows_ref as ref
 from test_gpu_rows import check_distill, check_grad, check_logprobs, make, teacher_for
 
 pytestmark = pytest.mark.gpu
@@ -106,3 +109,50 @@ def test_gradients_at_small_temperatures(ctx, dtype, V, exponent):
     ids, v = teacher_for(x, 8, g, T, pad=False)
     for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
         check_distill(ctx, x, ids, v, tail, T)
+
+
+def confident_rows(V, dtype, gap, at, T, masked):
+    """The teacher's two tokens certain, everything else `gap` nats below them."""
+    x = torch.full((3, V), -gap * T, device=DEV)
+    if masked:
+        x[:, 1::3] = NINF
+    x[:, at] = 0.0
+    x[:, at + 1] = -0.5 * T
+    x = x.to(dtype)
+    ids = torch.tensor([[at, at + 1]] * 3, dtype=torch.int32, device=DEV)
+    v = torch.log(torch.full((3, 2), 0.25, device=DEV))
+    return x, ids, v
+
+
+@DTYPES
+@LENGTHS
+@pytest.mark.parametrize("T", [1.0, 0.1])
+@pytest.mark.parametrize("masked", [False, True], ids=["all", "masked"])
+def test_bucket_against_a_tail_that_is_nearly_nothing(ctx, dtype, V, T, masked):
+    """A tail of 2^-126 of the row's mass and more is matched, however small its entries are; a smaller one counts
+    as nothing: an infinite loss, and no share of the gradient.  No masked entry gets a NaN."""
+    w = torch.tensor([1.0, 100.0, 1e-3], device=DEV)
+    seen = set()
+    for gap in (30.0, 45.0, 70.0, 80.0, 85.0, 86.5, 88.0, 90.0, 92.0, 95.0, 97.5, 99.0, 103.0, 110.0):
+        for at in (3, V - 40):
+            x, ids, v = confident_rows(V, dtype, gap, at, T, masked)
+            _, _, _, p, _ = ref.stats(x.double(), T)
+            pt = float(p[0, :at].sum() + p[0, at + 2:].sum())
+            assert not 0.98 < pt * 2.0 ** 126 < 1.02
+            there = pt > 2.0 ** -126
+            seen.add(there)
+            if there:
+                check_distill(ctx, x, ids, v, binding.TAIL_BUCKET, T, w)
+                check_distill(ctx, x, ids, v, binding.TAIL_BUCKET, T, w, grad=False)
+                continue
+            both = ctx.distill(x, ids, v, tail=binding.TAIL_BUCKET, temperature=T, weight=w, grad=True)
+            only = ctx.distill(x, ids, v, tail=binding.TAIL_BUCKET, temperature=T, weight=w)
+            assert (both["loss"] == math.inf).all() and (only["loss"] == math.inf).all()
+            assert torch.isfinite(both["grad"]).all()
+            want = p.clone()                                   # M = 1: the pull of the whole mass, less the teacher's q
+            want[:, at:at + 2] -= 0.25
+            want = want * w.double()[:, None] / T
+            tol = 4 * ref.delta(V) * w.double()[:, None] / T + want.abs() * (2.0 ** -8 if dtype == torch.bfloat16 else 0.0) + 1e-38
+            ref.same(both["grad"], want, tol)
+            assert (both["grad"][:, torch.arange(V, device=DEV) % 97 == 60].abs() <= 1e-30).all()
+    assert seen == {False, True}
