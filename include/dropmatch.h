@@ -286,7 +286,7 @@ int dropmatch_logprobs_grad(dm_ctx* ctx, const void* logits, int dtype, int64_t 
  *   weight[n_rows]   float32 or NULL (1): a mask, 1/n, or the upstream gradient of loss[r]
  *   out_loss[n_rows] float32 (without the weight) or NULL;  out_grad as above, or NULL; not both NULL
  *   dl[v] = weight / T * ( M p[v] - q[v] - [v is no teacher token] q_t p[v] / p_t ),  M = sum q + q_t
- * No factor T^2 is applied.  A row without a present entry: loss 0 (and gradient 0).  A teacher token
+ * No factor T^2 is applied.  A row without a present entry: loss 0 and gradient 0, whatever it holds.  A teacher token
  * the student gives probability 0: loss +inf; so does a tail of less than 2^-126 (1.2e-38) of the row's mass,
  * whose gradient is left out.  A row of nothing but -inf: gradient 0.  A row of weight 0
  * gets a gradient of 0 whatever it holds.  DM_EUNSUPPORTED beyond V of about 12 million (bf16) or 6 million

@@ -57,7 +57,7 @@ struct RowsShared {
     float t_q[kRowsMaxTop], t_v[kRowsMaxTop], t_x[kRowsMaxTop];
     float t_max[kRowsMaxTop / 32];
     double t_sum[kRowsMaxTop / 32];
-    int t_distinct, t_repeated;
+    int t_distinct, t_repeated, t_any;
     float raised[kRowsMaxCluster * kWarps];   // parts of a tail that is summed anew, from every CTA
 };
 
@@ -390,7 +390,7 @@ rows_kernel(const RowsParams P) {
                 if (te.id >= 0) te.x = RowVec<T>::get_early(sh.row + te.id);
                 ss.t_id[tid] = te.id;
             }
-            if (tid == 0) { ss.t_distinct = 0; ss.t_repeated = 0; }
+            if (tid == 0) ss.t_distinct = ss.t_repeated = ss.t_any = 0;
             if (use_bits)
                 for (int i = tid; i < n_batches * kBatch / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
             if (warp < kRowsMaxTop / 32) {
@@ -400,6 +400,7 @@ rows_kernel(const RowsParams P) {
                 if (lane == 0) ss.t_max[warp] = vm;
             }
             __syncthreads();
+            if (te.id >= 0) ss.t_any = 1;     // read behind the barriers below
             if (use_bits && te.id >= 0) {
                 const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
                 if (at >= 0 && at < sh.last - sh.first) {
@@ -548,7 +549,7 @@ rows_kernel(const RowsParams P) {
             const double scale = P.tail == DM_TAIL_RENORM ? (sum != 0.0 ? 1.0 / sum : 0.0) : 1.0;
             mass = (float)(sum * scale);
             // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
-            if (P.tail == DM_TAIL_BUCKET && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
+            if (P.tail == DM_TAIL_BUCKET && ss.t_any != 0 && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
             if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
             __syncthreads();
             if (P.tail == DM_TAIL_BUCKET && need_stats && small_tail(a)) {   // the row is read again
@@ -582,7 +583,7 @@ rows_kernel(const RowsParams P) {
         }
 
         if (kOp != OP_LOGPROBS && grad_row != nullptr) {
-            const bool none = zero_grad || dead;
+            const bool none = zero_grad || dead || (kOp == OP_DISTILL && ss.t_any == 0);   // (a row without a teacher counts for nothing)
             const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                   : raised < 0.0f ? distill_factors(w, mass, rest, a.tail, inv_total)
                                                   : raised_factors(w, mass, rest, raised, inv_total);

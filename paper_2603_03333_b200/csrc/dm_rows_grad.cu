@@ -54,7 +54,7 @@ struct ResidentShared {
     // teacher (distill), twice over: the loss of a row is finished while the next one is under way
     int t_id[2][kRowsMaxTop];
     float t_v[2][kRowsMaxTop], t_x[2][kRowsMaxTop], t_q[2][kRowsMaxTop];
-    int t_distinct[2], t_repeated[2];
+    int t_distinct[2], t_repeated[2], t_any[2];   // tokens of the share, named twice; whether the row has a token at all
     float t_max[kTeacherWarps];
     double t_sum[kTeacherWarps];
     float raised[kRowsMaxCluster * kWarps];   // parts of a tail that is summed anew, from every CTA
@@ -144,7 +144,7 @@ rows_resident_kernel(const RowsParams P) {
     for (int b = 0; b < n_batches; ++b) sh.fetch_batch(sh.first + b * kBatch, stash + b * kBatch + tid);
     if (kTail) {
         for (int i = tid; i < P.stash_vecs / 4; i += kThreads) reinterpret_cast<uint32_t*>(bitmap)[i] = 0u;
-        if (tid < 2) ss.t_distinct[tid] = ss.t_repeated[tid] = 0;
+        if (tid < 2) ss.t_distinct[tid] = ss.t_repeated[tid] = ss.t_any[tid] = 0;
         __syncthreads();
     }
     // the row's small inputs, one row ahead
@@ -215,6 +215,7 @@ rows_resident_kernel(const RowsParams P) {
                 te.x = RowVec<T>::get_early(sh.row + te.id);
             }
             if (te.id >= 0) {
+                ss.t_any[par] = 1;
                 const int at = (te.id + sh.phase) / N - sh.first;   // vector within the share
                 if (at >= 0 && at < n_share) {
                     const uint32_t bit = mark_bit(at, (te.id + sh.phase) % N);
@@ -332,7 +333,7 @@ rows_resident_kernel(const RowsParams P) {
         const float log_total = log1pf(a.rest), inv_total = 1.0f / (1.0f + a.rest);
         // (the marks have served; so have the counters of the row before)
         if (kOp == OP_DISTILL && my_word != nullptr) *my_word = 0u;
-        if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = 0;
+        if (kOp == OP_DISTILL && tid == 0) ss.t_distinct[par ^ 1] = ss.t_repeated[par ^ 1] = ss.t_any[par ^ 1] = 0;
         float mass = 0.0f, rest = 0.0f, q = 0.0f;   // sum of the teacher's q, mass of its bucket, this thread's q
         double q_sum = 0.0;
         if (kOp == OP_DISTILL) {
@@ -341,14 +342,15 @@ rows_resident_kernel(const RowsParams P) {
             const double scale = P.tail == DM_TAIL_RENORM ? (q_sum != 0.0 ? 1.0 / q_sum : 0.0) : 1.0;
             mass = (float)(q_sum * scale);
             // tokens outside the teacher's exist unless k reaches V (such a row is one CTA's)
-            if (bucket && (P.k < P.V || ss.t_distinct[par] < P.V)) rest = 1.0 - q_sum > 0.0 || q_sum != q_sum ? (float)(1.0 - q_sum) : 0.0f;
+            if (bucket && ss.t_any[par] != 0 && (P.k < P.V || ss.t_distinct[par] < P.V)) rest = 1.0 - q_sum > 0.0 || q_sum != q_sum ? (float)(1.0 - q_sum) : 0.0f;
             q = (float)(te.q * scale);
             if (tid < P.k) { ss.t_q[par][tid] = q; ss.t_x[par][tid] = te.x; }
         }
         const bool repeated = kOp == OP_DISTILL && ss.t_repeated[par] != 0;
         const bool dead = a.m == neg_inf();                 // every entry masked: no distribution
         const float entropy = dead ? 0.0f : fmaf(-kLn2 * inv_total, a.t, log_total);
-        const bool none = zero_grad || dead;
+        const bool taught = kOp != OP_DISTILL || ss.t_any[par] != 0;   // (a row without a teacher counts for nothing)
+        const bool none = zero_grad || dead || !taught;
         const float rc = a.m * c;
         bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
         GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)

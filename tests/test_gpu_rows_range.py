@@ -1,6 +1,7 @@
 """The operators on rows of logits at the ends of their range: large magnitudes, small temperatures, tails that are
 nearly nothing, rows without a teacher.  Statements and error bounds are those of rows_ref.py."""
 import math
+import types
 
 import pytest
 import torch
@@ -156,3 +157,50 @@ def test_bucket_against_a_tail_that_is_nearly_nothing(ctx, dtype, V, T, masked):
             ref.same(both["grad"], want, tol)
             assert (both["grad"][:, torch.arange(V, device=DEV) % 97 == 60].abs() <= 1e-30).all()
     assert seen == {False, True}
+
+
+@DTYPES
+@LENGTHS
+@pytest.mark.parametrize("tail", [0, 1], ids=["renorm", "bucket"])
+def test_rows_without_a_teacher_count_for_nothing(ctx, dtype, V, tail):
+    """Whatever they hold: a padded row's logits may be anything."""
+    x, g = make(6, V, dtype)
+    x[1] = float("nan")
+    x[2, 7] = float("inf")
+    x[3] = NINF
+    ids, v = teacher_for(x, 5, g, 1.0, pad=False)
+    ids[:4] = -1
+    ids[2] = V
+    v[1] = float("nan")
+    w = torch.rand(6, generator=g, device=DEV) + 0.5
+    for weight in (None, w):
+        both = ctx.distill(x, ids, v, tail=tail, weight=weight, grad=True)
+        assert (both["loss"][:4] == 0).all() and (both["grad"][:4] == 0).all()
+        assert (ctx.distill(x, ids, v, tail=tail, weight=weight)["loss"][:4] == 0).all()
+        check_distill(ctx, x[4:], ids[4:], v[4:], tail, 1.0, None if weight is None else weight[4:])
+    y = x.clone()
+    assert torch.equal(ctx.distill(y, ids, v, tail=tail, weight=w, grad=True, out=y)["grad"], both["grad"])
+
+
+@DTYPES
+def test_many_rows_with_and_without_a_teacher(ctx, dtype):
+    """Rows of every kind one after the other in a cluster's walk: nothing of one reaches the next."""
+    rows, V = 1500, 9001
+    x, g = make(rows, V, dtype)
+    ids, v = teacher_for(x, 7, g, 1.0)
+    ids[::3] = -1
+    x[::6] = float("nan")
+    x[4::9] = -1e10
+    x[7::9] = -90.0
+    for r in range(7, rows, 9):
+        ids[r] = torch.arange(7, device=DEV)
+    x[7::9, :7] = 0.0
+    v[7::9] = math.log(0.1)
+    have = torch.ones(rows, dtype=torch.bool, device=DEV)
+    have[::3] = False
+    for tail in (binding.TAIL_RENORM, binding.TAIL_BUCKET):
+        got = ctx.distill(x, ids, v, tail=tail, grad=True)
+        assert (got["loss"][::3] == 0).all() and (got["grad"][::3] == 0).all()
+        of_have = types.SimpleNamespace(distill=lambda *_, **__: {key: t[have] for key, t in got.items()})
+        check_distill(of_have, x[have], ids[have], v[have], tail, 1.0)
+    assert ctx.device_error() == 0
