@@ -252,8 +252,9 @@ int dropmatch_score(dm_ctx* ctx, const void* H, const int32_t* tokens, int n_row
  *   logits[n_rows][ld]   dtype DM_F32 or DM_BF16, row stride ld >= V entries, aligned to one entry
  *                        (16-byte aligned rows of the same alignment are the fastest)
  * n_rows = 0 is allowed and does nothing.  V <= 2^30.
- * Error word (dm_device_error) 8, this call and the gradients: a cluster gave up waiting (a second) for the
- * answer to its request for another row; rows that it would have taken are unwritten. */
+ * Error word (dm_device_error) 8, this call and the gradients: a cluster's wait for the answer to its request
+ * for another row ran out (dm_debug_set_wait_limit).  It waits once more, for a second, and goes on with the
+ * answer: the outputs are complete.  Only where that wait runs out too are rows that it would have taken unwritten. */
 int dropmatch_logprobs(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
                        const int32_t* tokens, int n_top, float temperature, float* out_logprob, float* out_lse,
                        float* out_entropy, int32_t* out_top_ids, float* out_top_logprob, void* stream);
@@ -410,7 +411,8 @@ int dm_device_error(dm_ctx* ctx, void* stream, uint32_t* out_code);
  * before it gives up, sets the device error word and winds down (0 restores the default, about
  * one second; the time a call spends queued behind the kernel ahead of it counts).  A limit of
  * a few cycles makes the first wait that is not satisfied at once run out: the tests use that
- * to exercise the wind-down and the fail-safe outputs without hanging or faulting anything. */
+ * to exercise the wind-down and the fail-safe outputs without hanging or faulting anything.  The wait of the calls
+ * on logits in memory for their next row, long satisfied as a rule, counts as run out at a limit of 1. */
 int dm_debug_set_wait_limit(dm_ctx* ctx, uint64_t cycles);
 
 /* Timing of the head kernel alone (the dominant kernel).  While enabled, every verify call

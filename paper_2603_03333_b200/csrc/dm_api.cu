@@ -778,6 +778,7 @@ int dropmatch_score(dm_ctx* c, const void* H, const int32_t* tokens, int n_rows,
             if (st != DM_OK) return st;
             part.logits = logits;
             part.err = part.err_out = c->err;
+            part.wait_limit = c->wait_limit;
             st = launch_rows_logprobs(part, DM_F32, s);
         }
         if (st != DM_OK) return st;
@@ -804,6 +805,7 @@ int dropmatch_logprobs(dm_ctx* c, const void* logits, int dtype, int64_t ld, int
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
     rp.err_out = c->err;
+    rp.wait_limit = c->wait_limit;
     return launch_rows_logprobs(rp, dtype, static_cast<cudaStream_t>(stream));
 }
 
@@ -822,6 +824,7 @@ int dropmatch_logprobs_grad(dm_ctx* c, const void* logits, int dtype, int64_t ld
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
     rp.err_out = c->err;
+    rp.wait_limit = c->wait_limit;
     rp.tokens = tokens;
     rp.g_logprob = g_logprob; rp.g_entropy = g_entropy;
     rp.out_grad = out_grad; rp.ld_grad = ld_grad;
@@ -845,6 +848,7 @@ int dropmatch_distill(dm_ctx* c, const void* logits, int dtype, int64_t ld, int 
     if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
     rp.logits = logits;
     rp.err_out = c->err;
+    rp.wait_limit = c->wait_limit;
     rp.t_ids = teacher_ids; rp.t_logprob = teacher_logprob;
     rp.k = k; rp.tail = tail;
     rp.weight = weight;

@@ -24,7 +24,6 @@
 
 #include <atomic>
 
-#include "dm_ptx.cuh"
 #include "dm_rows_dev.cuh"
 
 namespace dm {
@@ -38,12 +37,11 @@ constexpr int kRing = 2;               // batches in flight per CTA, eight per S
 constexpr int kCandCap = 1024;         // candidates for the top entries of a CTA's share
 constexpr int kHitCap = 1024;          // batches that hold them
 constexpr int kMaxSlots = 16, kWalkSlots = 8;   // maxima a thread keeps of its batches (for finding the top entries again)
-constexpr long long kWaitLimitCycles = 2000000000ll;   // about one second
 
 struct RowsShared {
     uint4 answer;                // to the request for another row
     uint64_t answer_bar;
-    int abort, next_row;
+    int next_row;
     float w_m[kWarps], w_s[kWarps], w_t[kWarps], w_tail[kWarps];
     int w_cnt[kWarps];
     Merged part[kRowsMaxCluster];   // every CTA's statistics, each written by its CTA
@@ -351,7 +349,6 @@ rows_kernel(const RowsParams P) {
     const uint32_t answer = ptx::smem_u32(&ss.answer), answer_bar = ptx::smem_u32(&ss.answer_bar);
     if (kWalk && tid == 0) {
         ptx::mbar_init(answer_bar, 1);
-        ss.abort = 0;
         ptx::fence_mbar_init();
         ptx::fence_proxy_async_smem();
     }
@@ -442,16 +439,7 @@ rows_kernel(const RowsParams P) {
                 for (int u = 0; u < kUnroll; ++u) v[u] = ring[u * kThreads];
                 const uint32_t marks = bucket ? reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid] : 0u;
                 if (kWalk && b == n_batches - kRing) {
-                    if (tid == 0) {
-                        int next = -1;
-                        if (ptx::mbar_wait<32>(answer_bar, parity, &ss.abort, kWaitLimitCycles)) {
-                            next = ptx::granted_cluster(answer);
-                            ptx::fence_proxy_async_smem();   // read before the next request writes it
-                        } else {
-                            atomicCAS(P.err_out, 0u, (uint32_t)ERR_WAIT_ROW);
-                        }
-                        ss.next_row = next;
-                    }
+                    if (tid == 0) ss.next_row = granted_row(P, answer, answer_bar, parity);
                     __syncthreads();
                     next_row = ss.next_row;
                     if (next_row >= 0) { from = share_of<T>(P, next_row, 1, 0); ahead = kRing - n_batches; }
@@ -649,6 +637,7 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
         if (smem <= kRowsSmemLimit) break;
         if (cluster >= kRowsMaxCluster) return DM_EUNSUPPORTED;
     }
+    if (P.wait_limit <= 0) P.wait_limit = kRowsWaitCycles;
     static std::atomic<unsigned long long> prepared{0}, prepared_walk{0};
     if (walk)
         return launch_clusters(rows_kernel<T, kOp, kOp == OP_LOGPROBS>, prepared_walk, dev, P, (long long)P.rows, 1, smem, stream);

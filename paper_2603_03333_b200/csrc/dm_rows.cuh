@@ -21,6 +21,7 @@ struct RowsParams {
     int slot_batches, n_slots;   // batches of a thread that share one remembered maximum, and how many of those (set by the launch)
     const uint32_t* err;  // device error word of the kernel that wrote the logits, or null
     uint32_t* err_out;    // device error word of the call's context
+    long long wait_limit; // clock cycles that a wait for the next row may take
     // logprobs
     const int32_t* tokens;
     int n_top;

@@ -4,6 +4,7 @@
 #include <atomic>
 
 #include "dm_internal.h"
+#include "dm_ptx.cuh"
 #include "dm_rows.cuh"
 
 namespace dm {
@@ -22,6 +23,7 @@ constexpr float kSmallShift = 16777216.0f;     // 2^24: the error is at most hal
 // entries far below fp32's range.
 constexpr float kTailSmall = 8.673617379884035e-19f;   // 2^-60
 constexpr float kTailUp = 64.0f, kTailInv = 5.421010862427522e-20f;   // 2^-64
+constexpr long long kRowsWaitCycles = 2000000000ll;   // about one second
 constexpr size_t kRowsSmemLimit = 216 * 1024;
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -569,6 +571,26 @@ static_assert(kUnroll == 4, "the marks of a batch fill a word");
 template <typename T>
 __device__ __forceinline__ bool phase_of(const T* p, int phase) {
     return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)) == phase;
+}
+
+// The answer to a request for another row, by the thread that made it: the granted cluster's first CTA, or -1.
+// An answer that comes after the limit is reported and used all the same: it lands in this CTA's shared memory,
+// and the row that it grants is nobody else's.  (A limit of one cycle, which only dm_debug_set_wait_limit
+// gives, has run out before the first look.)
+__device__ __forceinline__ int granted_row(const RowsParams& P, uint32_t answer, uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    bool late = P.wait_limit <= 1, came = true;
+    while (came && !ptx::mbar_try_wait(bar, parity)) {
+        __nanosleep(32);
+        const long long waited = clock64() - t0;
+        late = late || waited > P.wait_limit;
+        came = waited <= P.wait_limit + kRowsWaitCycles;
+    }
+    if (late) atomicCAS(P.err_out, 0u, (uint32_t)ERR_WAIT_ROW);
+    if (!came) return -1;
+    const int next = ptx::granted_cluster(answer);
+    ptx::fence_proxy_async_smem();   // read before the next request writes it
+    return next;
 }
 
 // `prepared`: devices on which the kernel's shared-memory limit has been raised, one bit each.

@@ -22,7 +22,6 @@
 // barrier (136 against 127), CTAs of 128 and 512 threads.
 #include <cooperative_groups.h>
 
-#include "dm_ptx.cuh"
 #include "dm_rows_dev.cuh"
 
 namespace dm {
@@ -35,7 +34,6 @@ using namespace rows;
 constexpr int kBatch = kUnroll * kThreads;
 constexpr int kShareVecs = 4096;        // share up to which a row is cut: 64 KB, three CTAs per SM
 constexpr int kTeacherWarps = kRowsMaxTop / 32;
-constexpr long long kWaitLimitCycles = 2000000000ll;   // about one second
 
 // A warp's part of a row: its CTA's maximum, and relative to it the sum of exponentials over the entries
 // below it, the same weighted with the exponents (gradient of the entropy) or over the tail (distillation,
@@ -48,7 +46,6 @@ struct ResidentShared {
     WarpSums part[2][kRowsMaxCluster * kWarps];
     uint4 answer;                  // to the request for another row (rank 0)
     uint64_t answer_bar;
-    int abort;
     int next_row[2];               // written by rank 0 into every CTA, twice over
     float w_max[kWarps];
     // teacher (distill), twice over: the loss of a row is finished while the next one is under way
@@ -167,7 +164,6 @@ rows_resident_kernel(const RowsParams P) {
     const uint32_t answer = ptx::smem_u32(&ss.answer), answer_bar = ptx::smem_u32(&ss.answer_bar);
     if (tid == 0) {
         ptx::mbar_init(answer_bar, 1);
-        ss.abort = 0;
         ptx::fence_mbar_init();
         ptx::fence_proxy_async_smem();
     }
@@ -238,13 +234,8 @@ rows_resident_kernel(const RowsParams P) {
             if (rank == 0 && warp == 0) {
                 int next = -1;
                 if (lane == 0) {
-                    if (ptx::mbar_wait<32>(answer_bar, (uint32_t)par, &ss.abort, kWaitLimitCycles)) {
-                        next = ptx::granted_cluster(answer);
-                        if (next >= 0) next /= n_cta;
-                        ptx::fence_proxy_async_smem();   // read before the next request writes it
-                    } else {
-                        atomicCAS(P.err_out, 0u, (uint32_t)ERR_WAIT_ROW);
-                    }
+                    next = granted_row(P, answer, answer_bar, (uint32_t)par);
+                    if (next >= 0) next /= n_cta;
                 }
                 next = __shfl_sync(0xFFFFFFFFu, next, 0);
                 if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->next_row[par] = next;
@@ -450,6 +441,7 @@ bool launch(RowsParams P, cudaStream_t stream, int* status) {
     P.stash_vecs = (per + kBatch - 1) / kBatch * kBatch;
     const size_t smem = (size_t)P.stash_vecs * 16 + (kOp == OP_DISTILL ? (size_t)P.stash_vecs : 0);
     if (smem > kRowsSmemLimit) return false;
+    if (P.wait_limit <= 0) P.wait_limit = kRowsWaitCycles;
     static std::atomic<unsigned long long> prepared{0};
     *status = launch_clusters(rows_resident_kernel<T, kOp>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
     return true;
