@@ -321,7 +321,8 @@ rows_kernel(const RowsParams P) {
     constexpr int N = RowVec<T>::N;
     constexpr bool kEntropy = kOp != OP_DISTILL, kTail = kOp == OP_DISTILL;
     constexpr int kBatch = kUnroll * kThreads;
-    extern __shared__ __align__(16) unsigned char smem[];
+    // (16-byte copies of a warp land in whole 128-byte lines: off that boundary they took up to a tenth longer)
+    extern __shared__ __align__(128) unsigned char smem[];
     __shared__ RowsShared ss;
     cg::cluster_group cluster = cg::this_cluster();
     const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();

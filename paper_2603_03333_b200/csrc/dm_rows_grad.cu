@@ -124,7 +124,8 @@ __global__ void __launch_bounds__(kThreads, 3)
 rows_resident_kernel(const RowsParams P) {
     constexpr int N = RowVec<T>::N;
     constexpr bool kEntropy = kOp == OP_GRAD, kTail = kOp == OP_DISTILL;
-    extern __shared__ __align__(16) unsigned char smem[];
+    // (16-byte copies of a warp land in whole 128-byte lines: off that boundary they took up to a tenth longer)
+    extern __shared__ __align__(128) unsigned char smem[];
     __shared__ ResidentShared ss;
     uint4* stash = reinterpret_cast<uint4*>(smem);                                    // [stash_vecs]
     unsigned char* bitmap = reinterpret_cast<unsigned char*>(stash + P.stash_vecs);   // distill: teacher tokens of the share, a byte per vector: tells repeated ones apart
