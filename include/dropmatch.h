@@ -267,8 +267,8 @@ int dropmatch_logprobs(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, i
  *                                   first entry to the last row's last, must not overlap.
  *                                   Entries V..ld_grad of a row are left as they are
  * A row whose two factors are 0 (or that has no token and g_entropy = 0) gets a gradient of 0 whatever
- * its logits hold; so does a row of nothing but -inf.  Recomputes the row's sums: one read of the
- * logits, one write. */
+ * its logits hold; so does a row of nothing but -inf.  An entry of less than 2^-126 (1.2e-38) of the row's
+ * largest probability counts as 0.  Recomputes the row's sums: one read of the logits, one write. */
 int dropmatch_logprobs_grad(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, int n_rows, int V,
                             const int32_t* tokens, float temperature, const float* g_logprob,
                             const float* g_entropy, void* out_grad, int64_t ld_grad, void* stream);

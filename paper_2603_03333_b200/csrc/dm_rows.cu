@@ -314,7 +314,8 @@ __device__ void top_of_share(const Share<T>& sh, float thread_max, int k, const 
 // present one's entries are selected (2047 rows of 151936, 5 alternatives: 147 -> 138 us when it was
 // introduced).  Only where more rows than CTAs fit: with fewer there is nothing to take over.
 // Four CTAs of 256 threads per SM; five, or CTAs of 128 or 512 threads, were no faster.
-template <typename T, int kOp, bool kWalk>
+// kGrad: with a gradient (distillation has a kernel without, which needs fewer registers).
+template <typename T, int kOp, bool kWalk, bool kGrad>
 __global__ void __launch_bounds__(kThreads, 4)
 rows_kernel(const RowsParams P) {
     static_assert(!kWalk || kOp == OP_LOGPROBS, "only rows without a gradient are walked over");
@@ -343,7 +344,7 @@ rows_kernel(const RowsParams P) {
     const float c = P.c;
 
     Share<T> sh = share_of<T>(P, row, n_cta, rank);
-    T* grad_row = kOp != OP_LOGPROBS && P.out_grad != nullptr ? static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad : nullptr;
+    T* grad_row = kGrad ? static_cast<T*>(P.out_grad) + (long long)row * P.ld_grad : nullptr;
 
     const int n_share = sh.last - sh.first, n_batches = kWalk ? P.n_batches : (n_share + kBatch - 1) / kBatch;
     uint4* ring = stash + tid;
@@ -377,7 +378,7 @@ rows_kernel(const RowsParams P) {
             g_h = P.g_entropy != nullptr ? P.g_entropy[row] : 0.0f;
             zero_grad = g_lp == 0.0f && g_h == 0.0f;
         }
-        const bool use_bits = kOp == OP_DISTILL && (P.tail == DM_TAIL_BUCKET || grad_row != nullptr);
+        const bool use_bits = kOp == OP_DISTILL && (kGrad || P.tail == DM_TAIL_BUCKET);
         TeacherEntry te{-1, neg_inf(), neg_inf(), false, 0.0};
         if (kOp == OP_DISTILL) {
             if (P.weight != nullptr) { const float wt = P.weight[row]; zero_grad = wt == 0.0f; w *= wt; }
@@ -541,17 +542,12 @@ rows_kernel(const RowsParams P) {
             if (P.tail == DM_TAIL_BUCKET && ss.t_any != 0 && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
             if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
             __syncthreads();
-            if (P.tail == DM_TAIL_BUCKET && need_stats && small_tail(a)) {   // the row is read again
+            if (P.tail == DM_TAIL_BUCKET && need_stats &&
+                (small_tail(a, P.V) || (kGrad && distill_factors(w, mass, rest, a.tail, inv_total).A == neg_inf()))) {   // the row is read again
                 raised = 0.0f;
-                for (int b = 0; b < n_batches; ++b) {
-                    uint4 v[kUnroll];
-#pragma unroll
-                    for (int u = 0; u < kUnroll; ++u) {
-                        const int j = sh.first + b * kBatch + u * kThreads + tid;
-                        v[u] = j < sh.last ? sh.load(j) : RowVec<T>::masked();
-                    }
-                    raised += raised_sum<T>(v, reinterpret_cast<const uint32_t*>(bitmap)[b * kThreads + tid], a.m, c);
-                }
+#pragma unroll 1
+                for (int at = tid; at < n_share; at += kThreads)
+                    raised += raised_sum<T>(sh.load(sh.first + at), *mark_word(bitmap, at) >> (at / kThreads % kUnroll * 8), a.m, c);
                 raised = warp_sum(raised);
                 if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->raised[rank * kWarps + warp] = raised;
                 if (n_cta == 1) {
@@ -571,7 +567,7 @@ rows_kernel(const RowsParams P) {
             }
         }
 
-        if (kOp != OP_LOGPROBS && grad_row != nullptr) {
+        if (kGrad) {
             const bool none = zero_grad || dead || (kOp == OP_DISTILL && ss.t_any == 0);   // (a row without a teacher counts for nothing)
             const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                   : raised < 0.0f ? distill_factors(w, mass, rest, a.tail, inv_total)
@@ -639,10 +635,12 @@ int launch_rows(RowsParams P, cudaStream_t stream) {
         if (cluster >= kRowsMaxCluster) return DM_EUNSUPPORTED;
     }
     if (P.wait_limit <= 0) P.wait_limit = kRowsWaitCycles;
-    static std::atomic<unsigned long long> prepared{0}, prepared_walk{0};
+    static std::atomic<unsigned long long> prepared{0}, prepared_walk{0}, prepared_loss{0};
     if (walk)
-        return launch_clusters(rows_kernel<T, kOp, kOp == OP_LOGPROBS>, prepared_walk, dev, P, (long long)P.rows, 1, smem, stream);
-    return launch_clusters(rows_kernel<T, kOp, false>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
+        return launch_clusters(rows_kernel<T, kOp, kOp == OP_LOGPROBS, kOp != OP_LOGPROBS>, prepared_walk, dev, P, (long long)P.rows, 1, smem, stream);
+    if (kOp == OP_DISTILL && P.out_grad == nullptr)
+        return launch_clusters(rows_kernel<T, kOp, false, kOp == OP_GRAD>, prepared_loss, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
+    return launch_clusters(rows_kernel<T, kOp, false, kOp != OP_LOGPROBS>, prepared, dev, P, (long long)P.rows * cluster, cluster, smem, stream);
 }
 
 }  // namespace

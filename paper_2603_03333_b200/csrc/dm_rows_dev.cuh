@@ -19,9 +19,10 @@ constexpr float kFloorExp = -200.0f;   // exponents are clamped here: 2^-200 is 
 // powers of two: nothing next to m.
 constexpr float kExactShift = 2147483648.0f;   // 2^31
 constexpr float kSmallShift = 16777216.0f;     // 2^24: the error is at most half a power of two, and may scale any factor
-// A tail of less than 2^-60 is summed anew, 2^64 times as large: 2^-126 of the row's mass may consist of
-// entries far below fp32's range.
-constexpr float kTailSmall = 8.673617379884035e-19f;   // 2^-60
+// A tail of less than this, times the entries of the row, is summed anew, 2^64 times as large: 2^-126 of the
+// row's mass may consist of entries far below fp32's range.  (Entries below 2^-126 are dropped by the first sum:
+// at most 2^-32 of a larger tail.)
+constexpr float kTailSmall = 5.0487097934144756e-29f;   // 2^-94
 constexpr float kTailUp = 64.0f, kTailInv = 5.421010862427522e-20f;   // 2^-64
 constexpr long long kRowsWaitCycles = 2000000000ll;   // about one second
 constexpr size_t kRowsSmemLimit = 216 * 1024;
@@ -405,22 +406,18 @@ __device__ __forceinline__ float warp_sum(float x) {
     return x;
 }
 
-// A batch's part of a small tail (entries that the teacher's tokens, marked, leave), 2^64 times as large.
+// A vector's part of a small tail (entries that the teacher's tokens, marked, leave), 2^64 times as large.
 template <typename T>
-__device__ __forceinline__ float raised_sum(const uint4 (&v)[kUnroll], uint32_t marks, float m, float c) {
+__device__ __forceinline__ float raised_sum(const uint4& v, uint32_t marks, float m, float c) {
     constexpr int N = RowVec<T>::N;
-    float sum = 0.0f;
+    float x[N], sum = 0.0f;
+    RowVec<T>::unpack(v, x);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        float x[N];
-        RowVec<T>::unpack(v[u], x);
-#pragma unroll
-        for (int n = 0; n < N; ++n) sum += (marks >> (8 * u + n)) & 1u ? 0.0f : ex2(fmaf(x[n] - m, c, kTailUp));
-    }
+    for (int n = 0; n < N; ++n) sum += (marks >> n) & 1u ? 0.0f : ex2(fmaf(x[n] - m, c, kTailUp));
     return sum;
 }
 // Is the row's tail to be summed anew?  (The same in all CTAs of the cluster.)
-__device__ __forceinline__ bool small_tail(const Merged& a) { return a.tail < kTailSmall && a.m != neg_inf(); }
+__device__ __forceinline__ bool small_tail(const Merged& a, int V) { return a.tail < kTailSmall * (float)V && a.m != neg_inf(); }
 
 // Less than 2^-126 of the row's mass counts as nothing.
 __device__ __forceinline__ float counted_tail(float raised, float inv_total) {

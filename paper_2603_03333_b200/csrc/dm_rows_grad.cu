@@ -99,13 +99,8 @@ __device__ __noinline__ float resident_tail(const uint4* stash, int n_batches, f
     const int n_cta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float raised = 0.0f;
-#pragma unroll 1
-    for (int b = 0; b < n_batches; ++b) {
-        uint4 v[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) v[u] = stash[b * kBatch + u * kThreads + threadIdx.x];
-        raised += raised_sum<T>(v, 0u, m, c);
-    }
+#pragma unroll 4
+    for (int i = 0; i < n_batches * kUnroll; ++i) raised += raised_sum<T>(stash[i * kThreads + threadIdx.x], 0u, m, c);
     raised = warp_sum(raised);
     if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->raised[rank * kWarps + warp] = raised;
     if (n_cta == 1) {
@@ -347,7 +342,7 @@ rows_resident_kernel(const RowsParams P) {
         bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
         GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                        : distill_factors(w, mass, rest, a.tail, inv_total);
-        if (kOp == OP_DISTILL && bucket && need_stats && small_tail(a)) {   // (the teacher's tokens have left the share)
+        if (kOp == OP_DISTILL && bucket && need_stats && (small_tail(a, P.V) || f.A == neg_inf())) {   // (the teacher's tokens have left the share)
             const float raised = resident_tail<T>(stash, n_batches, a.m, c, inv_total, ss);
             a.tail = raised * kTailInv;
             f = raised_factors(w, mass, rest, raised, inv_total);
