@@ -457,15 +457,21 @@ __device__ __forceinline__ float teacher_loss(const RowsParams& P, const Merged&
     const double log_rest = __shfl_sync(0xFFFFFFFFu, logs, 2), log_tail = __shfl_sync(0xFFFFFFFFu, logs, 3);
     // log q = v - base: the teacher's normaliser
     const double base = P.tail == DM_TAIL_RENORM && all_v > neg_inf() ? (double)all_v + log_q : 0.0;
-    double loss = 0.0;
+    double loss = 0.0, taken = 0.0;
     for (int i = lane; i < P.k; i += 32) {
         if (id[i] < 0 || q[i] == 0.0f) continue;
         const double logp = dead || x[i] == neg_inf() ? -INFINITY : ((double)x[i] - (double)a.m) * P.inv_temp_d - log_total;
         loss += (double)q[i] * (((double)v[i] - base) - logp);
+        taken += (double)q[i];
     }
     __syncwarp();
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) loss += __shfl_xor_sync(0xFFFFFFFFu, loss, off);
+    for (int off = 16; off > 0; off >>= 1) {
+        loss += __shfl_xor_sync(0xFFFFFFFFu, loss, off);
+        taken += __shfl_xor_sync(0xFFFFFFFFu, taken, off);
+    }
+    // the q's rounded to fp32 do not add up to the mass: log p of -3.4e38 (a mask) would become -inf
+    if (taken > 0.0) loss *= mass / taken;
     if (rest != 0.0 && !(dead && mass == 0.0)) loss += rest * (log_rest - (log_tail - log_total));
     return (float)loss;
 }

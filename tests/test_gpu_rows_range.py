@@ -182,6 +182,22 @@ def test_rows_without_a_teacher_count_for_nothing(ctx, dtype, V, tail):
     assert torch.equal(ctx.distill(y, ids, v, tail=tail, weight=w, grad=True, out=y)["grad"], both["grad"])
 
 
+@LENGTHS
+def test_loss_of_a_teacher_whose_tokens_are_masked_by_the_lowest_value(ctx, V):
+    """Finite where the definition is: the weights of log p = -3.4e38 add up to the teacher's mass, not to a rounding
+    error above it."""
+    rows, k = 40, 33
+    x, g = make(rows, V, torch.float32)
+    ids = torch.stack([torch.randperm(V, generator=g, device=DEV)[:k] for _ in range(rows)]).to(torch.int32)
+    x.scatter_(1, ids.long(), torch.finfo(torch.float32).min)
+    v = torch.log_softmax(torch.randn((rows, k), generator=g, device=DEV) * 3, 1)
+    want = ref.distill(x, ids, v, False, 1.0)[0].float().double()
+    assert torch.isfinite(want).all()
+    for grad in (False, True):
+        got = ctx.distill(x, ids, v, tail=binding.TAIL_RENORM, grad=grad)["loss"]
+        ref.same(got, want, 4 * ref.U * want.abs())
+
+
 @DTYPES
 def test_many_rows_with_and_without_a_teacher(ctx, dtype):
     """Rows of every kind one after the other in a cluster's walk: nothing of one reaches the next."""
