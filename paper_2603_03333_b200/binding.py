@@ -342,7 +342,8 @@ class Context:
     # -- dropmatch_logprobs / dropmatch_logprobs_grad / dropmatch_distill
     def logprobs(self, logits, tokens=None, n_top=0, temperature=1.0):
         """The outputs of `score` for logits[...,V] in memory (float32 or bfloat16; the last dimension
-        dense, one stride between rows)."""
+        dense, one stride between rows).  Autograd does not see this call, nor the two below: what they
+        return carries no graph, and a gradient written into `out` does not count as a change of it."""
         rows, ld = self._rows(logits, "logits")
         out = self._row_outputs(logits.shape[:-1], tokens, n_top)
         _check(lib().dropmatch_logprobs(self._h, _ptr(logits), _DTYPES[logits.dtype], ld, rows, logits.shape[-1],

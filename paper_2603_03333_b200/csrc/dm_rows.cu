@@ -7,18 +7,19 @@
 //                  (the teacher's rules stand in dm_rows_dev.cuh)
 //
 // A row belongs to one thread-block cluster; its CTAs take contiguous shares of the row, cut at
-// 16-byte boundaries.  One pass over the share keeps, per warp, the exact maximum m so far (five
-// shuffles per 1024 entries) and, per lane, the sum of e = 2^((x - m) log2(e) / T) and of e times its
-// exponent (entropy) over the entries below m; entries equal to m are counted.  A batch whose maximum
-// stays below m takes the short path: seven or eight instructions per entry.  Warps meet in the
+// 16-byte boundaries.  One pass over the share keeps, per warp, the exact maximum m so far (one
+// reduction of the warp per 512 fp32 or 1024 bf16 entries) and, per lane, the sum of
+// e = 2^((x - m) log2(e) / T) and of e times its exponent (entropy) over the entries below m; entries equal
+// to m are counted.  A batch whose maximum stays below m takes the short path.  Warps meet in the
 // block, CTAs through distributed shared memory.  Sums never contain the row's largest entry, so that
 // log(1 + rest) keeps its precision next to a near-certain token.
 //
 // Bound: memory, one read of x.  Measured on 622 MB of bf16 logits (2047 rows of 151936): 106 us for the
-// sums (5.9 TB/s, 0.90 of a measured copy's rate), 117 us with the 5 largest entries, 139 us with 20, 181 us
-// with 100 (under sustained load, at the clock the power cap leaves, 121, 133 and 149); two thirds of the
-// issue slots are taken.  Batches of six vectors per thread with three CTAs per SM were slower (146 against
-// 136 us).  Few rows are bound by latency: some 12 us for
+// sums (5.9 TB/s, 0.90 of a measured copy's rate), 117-119 us with the 5 largest entries, 139 us with 20, 181 us
+// with 100 (under sustained load, at the clock the power cap leaves, 121, 132 and 149); two thirds of the
+// issue slots are taken.  Loss of a distillation alone, bucket, 64 tokens: 60 us for 1024 rows of 128256 bf16,
+// 62 us for 512 rows of fp32 (133 and 160 if the tail of every row is summed anew).  Batches of six vectors per
+// thread with three CTAs per SM were slower (146 against 136 us).  Few rows are bound by latency: some 12 us for
 // one row of 128256.
 #include <cooperative_groups.h>
 

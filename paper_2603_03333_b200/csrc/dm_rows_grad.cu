@@ -11,8 +11,9 @@
 // memory ahead of one cluster barrier.
 //
 // Bound: memory, one read and one write of the row.  Measured: distillation with its gradient, 1024
-// rows of 128256 bf16 (525 MB in all), 118 us = 4.5 TB/s; gradient of log-probability and entropy, 513
-// rows of 128256 fp32 (526 MB), 100 us = 5.3 TB/s; 1021 rows of 32003 bf16 (131 MB), 38 us = 3.5 TB/s.
+// rows of 128256 bf16 (525 MB in all), 119-120 us = 4.4 TB/s (167 us if the tail of every row is summed anew);
+// gradient of log-probability and entropy, 513 rows of 128256 fp32 (526 MB), 100-103 us = 5.1 to 5.3 TB/s;
+// 1021 rows of 32003 bf16 (131 MB), 37-38 us = 3.5 TB/s.
 // What keeps it there is the chain of a row: of some 21 thousand cycles that a CTA spends on 64 KB, the
 // two passes with exponentials (16 per cycle and SM) take 8, waiting for the cluster 3 to 4, barriers,
 // sums, merge and the teacher the rest; three CTAs per SM hide half of it.  Tried, on the step: shares of

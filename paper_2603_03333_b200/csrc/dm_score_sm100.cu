@@ -13,9 +13,9 @@
 // two blocks of hidden rows against one W tile, which fill TMEM), W crosses the HBM interface once per
 // 512 hidden rows.  Hidden rows come straight from the caller's array through a tensor map made for the
 // call; rows past its end load as zeros.  Bounds: W from HBM up to some 200 rows, the tensor pipe above.
-// Measured: one row against 128256 x 4096 with 5 alternatives 161-169 us (1.05 GB: 6.2-6.5 TB/s), 61 rows
-// against 151936 x 4096 191-207 us (1.24 GB: 6.0-6.5 TB/s), 509 rows against 128256 x 8192 with 32
-// alternatives 835-889 us (1.07 PFLOP: 1.2-1.28 PFLOP/s, 0.9 of what a GEMM sustains under the power cap;
+// Measured: one row against 128256 x 4096 with 5 alternatives 161-171 us (1.05 GB: 6.1-6.5 TB/s), 61 rows
+// against 151936 x 4096 191-208 us (1.24 GB: 6.0-6.5 TB/s), 509 rows against 128256 x 8192 with 32
+// alternatives 835-895 us (1.07 PFLOP: 1.19-1.28 PFLOP/s, 0.9 of what a GEMM sustains under the power cap;
 // the tensor pipe is busy 85 % of the cycles).
 //
 // Epilogue.  32 columns at a time: their maximum, the sum of 2^((l - max) c) over the others
