@@ -480,7 +480,16 @@ rows_kernel(const RowsParams P) {
             if (warp == 0) cluster_merge(ss, n_cta, c);
         } else {
             copy_wait(0);
-            if (n_cta > 1) cluster_wait();
+            if (n_cta > 1) {
+                // the same meeting as over a row that is summed: another kernel may change a weight meanwhile, and no
+                // CTA may leave while another writes to it or waits for it
+                cluster_wait();
+                const float nan = __uint_as_float(0x7FC00000u);
+                if (tid < n_cta) cluster.map_shared_rank(&ss, tid)->part[rank] = Merged{nan, nan, nan, nan};
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+            }
             if (tid == 0) {
                 ss.all = Merged{0.0f, 0.0f, 0.0f, 0.0f};
                 ss.log_total = ss.inv_total = 0.0f;
@@ -543,8 +552,7 @@ rows_kernel(const RowsParams P) {
             if (P.tail == DM_TAIL_BUCKET && ss.t_any != 0 && (P.k < P.V || ss.t_distinct < P.V)) rest = 1.0 - sum > 0.0 || sum != sum ? (float)(1.0 - sum) : 0.0f;
             if (tid < P.k) { ss.t_q[tid] = (float)(te.q * scale); ss.t_v[tid] = te.v; ss.t_x[tid] = te.x; }
             __syncthreads();
-            if (P.tail == DM_TAIL_BUCKET && need_stats &&
-                (small_tail(a, P.V) || (kGrad && distill_factors(w, mass, rest, a.tail, inv_total).A == neg_inf()))) {   // the row is read again
+            if (P.tail == DM_TAIL_BUCKET && need_stats && small_tail(a, P.V)) {   // the row is read again
                 raised = 0.0f;
 #pragma unroll 1
                 for (int at = tid; at < n_share; at += kThreads)
@@ -570,9 +578,10 @@ rows_kernel(const RowsParams P) {
 
         if (kGrad) {
             const bool none = zero_grad || dead || (kOp == OP_DISTILL && ss.t_any == 0);   // (a row without a teacher counts for nothing)
-            const GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
-                                  : raised < 0.0f ? distill_factors(w, mass, rest, a.tail, inv_total)
-                                                  : raised_factors(w, mass, rest, raised, inv_total);
+            GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
+                                           : distill_factors(w, mass, rest, a.tail, inv_total);
+            if (kOp == OP_DISTILL && (raised >= 0.0f || f.A == neg_inf()))
+                f = raised_factors(w, mass, rest, raised >= 0.0f ? raised : a.tail / kTailInv, inv_total);
             const bool same_phase = phase_of(grad_row, sh.phase);
 #pragma unroll 4
             for (int j = sh.first + tid; j < sh.last; j += kThreads)

@@ -488,9 +488,8 @@ __device__ __forceinline__ GradFactors distill_factors(float w, float mass, floa
     const float share = rest > 0.0f && tail > 0.0f ? rest / tail : 0.0f;
     return GradFactors{w * fmaf(mass + rest, inv_total, -share), 0.0f, w * (mass + rest) * inv_total, 0.0f};
 }
-// The same for a tail that was summed anew: `raised`, 2^64 times as large; 0 if it counts as nothing.  The
-// factor is 2^64 times too small and the exponents are raised, so that neither leaves fp32's range (all
-// entries but the teacher's tokens, which are written apart, are small).
+// The same for a tail that was summed anew, or where the factor overflows (a weight over a temperature of 1e20):
+// `raised`, the tail 2^64 times as large; 0 if it counts as nothing.  The factor is 2^64 times too small and the exponents are raised, so that neither leaves fp32's range.
 __device__ __forceinline__ GradFactors raised_factors(float w, float mass, float rest, float raised, float inv_total) {
     if (raised == 0.0f) return distill_factors(w, mass, rest, 0.0f, inv_total);
     float A = w * fmaf((mass + rest) * kTailInv, inv_total, -rest / raised);

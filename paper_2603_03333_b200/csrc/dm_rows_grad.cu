@@ -311,6 +311,11 @@ rows_resident_kernel(const RowsParams P) {
             if (lane < n_cta) (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->part[par][rank * kWarps + warp] = r;
         } else {
             copy_wait(0);
+            // whether the cluster meets again over this row hangs on what is exchanged here, in every CTA alike,
+            // even where another kernel changes a weight meanwhile
+            if (kTail && lane < n_cta)
+                (n_cta == 1 ? &ss : cluster.map_shared_rank(&ss, lane))->part[par][rank * kWarps + warp] =
+                    WarpSums{__uint_as_float(0x7FC00000u), 0.0f, 0.0f, 0.0f};
         }
         tell_next();
         meet();
@@ -343,9 +348,12 @@ rows_resident_kernel(const RowsParams P) {
         bool plain = !(fabsf(rc) < kSmallShift);   // exponents of differences
         GradFactors f = kOp == OP_GRAD ? logprob_factors(w, g_lp, g_h, entropy, log_total, inv_total)
                                        : distill_factors(w, mass, rest, a.tail, inv_total);
-        if (kOp == OP_DISTILL && bucket && need_stats && (small_tail(a, P.V) || f.A == neg_inf())) {   // (the teacher's tokens have left the share)
-            const float raised = resident_tail<T>(stash, n_batches, a.m, c, inv_total, ss);
-            a.tail = raised * kTailInv;
+        if (kOp == OP_DISTILL && bucket && need_stats && (small_tail(a, P.V) || f.A == neg_inf())) {
+            float raised = a.tail / kTailInv;
+            if (small_tail(a, P.V)) {   // (the teacher's tokens have left the share)
+                raised = resident_tail<T>(stash, n_batches, a.m, c, inv_total, ss);
+                a.tail = raised * kTailInv;
+            }
             f = raised_factors(w, mass, rest, raised, inv_total);
             plain = plain || f.up != 0.0f;
         }

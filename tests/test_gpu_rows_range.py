@@ -161,6 +161,14 @@ def test_bucket_against_a_tail_that_is_nearly_nothing(ctx, dtype, V, T, masked):
 
 @DTYPES
 @LENGTHS
+def test_bucket_at_a_weight_that_overflows_the_share(ctx, dtype, V):
+    """weight / T q_t / p_t beyond fp32, every gradient within it; masked entries get 0."""
+    x, ids, v = confident_rows(V, dtype, 40.0, 3, 1.0, True)
+    check_distill(ctx, x, ids, v, binding.TAIL_BUCKET, 1.0, torch.tensor([1e24, 1e28, 1.0], device=DEV))
+
+
+@DTYPES
+@LENGTHS
 @pytest.mark.parametrize("tail", [0, 1], ids=["renorm", "bucket"])
 def test_rows_without_a_teacher_count_for_nothing(ctx, dtype, V, tail):
     """Whatever they hold: a padded row's logits may be anything."""
