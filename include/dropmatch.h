@@ -296,6 +296,53 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
                       const int32_t* teacher_ids, const float* teacher_logprob, int k, int tail, float temperature,
                       const float* weight, float* out_loss, void* out_grad, int64_t ld_grad, void* stream);
 
+/* ---- verification against the target's own distribution --------------------------------------------
+ * The lossless rule of speculative decoding (Sec. 2), from random numbers that the caller draws: what DropMatch's
+ * criteria are measured against, and what an engine falls back to.  For sequence b and drafted position t, with
+ *   p = Softmax(target[b,t] / temperature),   q = Softmax(draft_logits[b,t] / draft_temperature),
+ * the drafted token x is accepted iff u_accept[b,t] * q(x) < p(x); n is the length of the accepted prefix.  The
+ * next token is drawn from r = max(p - q, 0) of row n (p, if r is 0 everywhere) where a token was rejected, and
+ * from p of row n where all were accepted: the smallest v with  r(0) + ... + r(v) > u_next[b] * sum r.
+ * Decisions and draws are those of 64-bit arithmetic on the given logits; out_accept_prob is fp32.
+ *   target[B][T + bonus_row][ld_target]   dtype DM_F32 or DM_BF16; row stride ld_target >= V entries, aligned to one
+ *                                entry (16-byte aligned rows are the fastest).  bonus_row = 1: one more row per
+ *                                sequence, behind the last drafted token
+ *   draft_logits[B][T][ld_draft] draft_dtype, as above; NULL: a drafter without a distribution (q is 1 on x, draft_dtype,
+ *                                ld_draft and draft_temperature are not looked at)
+ *   draft[B,T]                   ids outside [0,V) have p = 0
+ *   draft_len[B]                 drafted tokens of each sequence, in [0,T] (clamped), or NULL: T.  Rows and tokens behind
+ *                                them are not read, but for row draft_len[b] of the target, which the next token is drawn from
+ *   u_accept[B,T], u_next[B]     float32 in [0,1)
+ *   out_accept_len[B], out_next_token[B]   -1 if every one of T tokens was accepted and there is no bonus row
+ *   out_accept_prob[B,T]         float32, min(1, p(x) / q(x)); 0 behind draft_len.  Read by the call's second kernel
+ * Masked entries: -inf has probability 0; a row of nothing but -inf has probability 0 everywhere.  A row that holds a
+ * NaN or +inf: accept_prob NaN, the token is not accepted, next token -1; next token -1 too where there is nothing to draw from.
+ * T = 0 with a bonus row draws one token per sequence (draft, u_accept and out_accept_prob may be NULL).  B = 0 is
+ * allowed and does nothing.  V <= 2^30.  Needs no head and no workspace: calls of one context may overlap. */
+int dropmatch_verify_lossless(dm_ctx* ctx, const void* target, int dtype, int64_t ld_target, const void* draft_logits,
+                              int draft_dtype, int64_t ld_draft, const int32_t* draft, const int32_t* draft_len, int B,
+                              int T, int bonus_row, int V, float temperature, float draft_temperature,
+                              const float* u_accept, const float* u_next, int32_t* out_accept_len,
+                              int32_t* out_next_token, float* out_accept_prob, void* stream);
+
+/* ---- dropout as an operator ------------------------------------------------------------------------
+ * Eq. 1 and Eq. 2 on rows in memory, with the masks of the verify calls (same key, same counters, dm_set_mask_mode
+ * included): a head or a draft model is trained under the dropout that it is verified with.  No mask is stored; the
+ * gradient generates it again from the same arguments.
+ *   dropmatch_dropout       x[B*T][ld] -> out[B*T*K][ld_out]:  out[(b*T+t)*K+i, j] = keep ? x[b*T+t, j] * s : 0
+ *   dropmatch_dropout_grad  grad[B*T*K][ld] -> out_grad[B*T][ld_out]:  s * sum_i (keep ? grad[(b*T+t)*K+i, j] : 0)
+ * with s = 1 / (1 - p) in fp32; fp32 arithmetic, rounded once to dtype (DM_F32 or DM_BF16).  Dropped entries are +0
+ * and add nothing whatever they hold.  Plain dropout of n rows: B = 1, T = n, K = 1.
+ *   1 <= K <= 1024, B*T*K < 2^30, 1 <= d <= 2^30, strides >= d entries, pointers aligned to one entry (16-byte aligned
+ *   rows are the fastest); entries d..ld_out of a row are left as they are.  The output must not overlap the input,
+ *   but for K = 1 may be the input itself (same pointer and stride).  B*T = 0 is allowed and does nothing.
+ * A row's results do not depend on the other rows of the call.  Needs no head and no workspace: calls of one context
+ * may overlap.  dm_set_mask_mode's value is taken at the call (and fixed in a captured graph). */
+int dropmatch_dropout(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int B, int T, int K, int d, float p,
+                      uint64_t seed, uint64_t seq_base, void* out, int64_t ld_out, void* stream);
+int dropmatch_dropout_grad(dm_ctx* ctx, const void* grad, int dtype, int64_t ld, int B, int T, int K, int d, float p,
+                           uint64_t seed, uint64_t seq_base, void* out_grad, int64_t ld_out, void* stream);
+
 /* Vocabulary-sharded heads (the deployment of Sec. 4.1 is tensor-parallel: every GPU holds a
  * slice of the LM head).  A context whose head is rows [offset, offset+V) of the full head reports
  * global token ids after dm_set_vocab_offset(ctx, offset) (call it after dm_set_head; default 0).

@@ -52,6 +52,10 @@ SIGNATURES = {
     "dropmatch_logprobs": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _ci, _cf, _vp, _vp, _vp, _vp, _vp, _vp]),
     "dropmatch_logprobs_grad": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _cf, _vp, _vp, _vp, _i64, _vp]),
     "dropmatch_distill": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _vp, _ci, _ci, _cf, _vp, _vp, _vp, _i64, _vp]),
+    "dropmatch_verify_lossless": (_ci, [_vp, _vp, _ci, _i64, _vp, _ci, _i64, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _cf, _vp, _vp,
+                                        _vp, _vp, _vp, _vp]),
+    "dropmatch_dropout": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _vp, _i64, _vp]),
+    "dropmatch_dropout_grad": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _vp, _i64, _vp]),
     "dropmatch_verify_tree": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
                                     _vp, _vp, _vp, _vp, _vp, _vp]),
     "dropmatch_verify_tree_next": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
@@ -390,6 +394,74 @@ class Context:
                                        _ptr(res.get("loss")), _ptr(res.get("grad")), ld_out, _stream(self.device)),
                "dropmatch_distill")
         return res
+
+    # -- dropmatch_verify_lossless
+    def verify_lossless(self, target, draft, u_accept, u_next, draft_logits=None, draft_len=None, temperature=1.0,
+                        draft_temperature=1.0):
+        """Drafted tokens against the target's distribution.  target[B,T,V] or, with a row behind the last drafted
+        token, [B,T+1,V] and draft_logits[B,T,V] (float32 or bfloat16, as in `logprobs`; None: a drafter without a
+        distribution), draft[B,T] int32, draft_len[B] int32 or None, u_accept[B,T] and u_next[B] float32 in [0,1).
+        -> dict: accept_len[B], next[B] (int32), accept_prob[B,T]."""
+        if target.dim() != 3 or draft.dim() != 2:
+            raise TypeError("target must have shape [B, T or T+1, V] and draft [B, T]")
+        B, rows, V = target.shape
+        T = draft.shape[1]
+        if draft.shape[0] != B or rows - T not in (0, 1):
+            raise TypeError("target must have T or T+1 rows for each of draft's sequences")
+        _, ld = self._rows(target, "target")
+        self._per_row(draft, torch.int32, (B, T), "draft")
+        self._per_row(u_accept, torch.float32, (B, T), "u_accept")
+        self._per_row(u_next, torch.float32, (B,), "u_next")
+        self._per_row(draft_len, torch.int32, (B,), "draft_len")
+        draft_dtype, ld_draft = F32, V
+        if draft_logits is not None:
+            if draft_logits.shape != (B, T, V):
+                raise TypeError("draft_logits must have shape [B, T, V]")
+            _, ld_draft = self._rows(draft_logits, "draft_logits")
+            draft_dtype = _DTYPES[draft_logits.dtype]
+        dev = self.device
+        out = dict(accept_len=_empty(B, dtype=torch.int32, device=dev), next=_empty(B, dtype=torch.int32, device=dev),
+                   accept_prob=_empty(B, T, dtype=torch.float32, device=dev))
+        _check(lib().dropmatch_verify_lossless(self._h, _ptr(target), _DTYPES[target.dtype], ld, _ptr(draft_logits),
+                                               draft_dtype, ld_draft, _ptr(draft), _ptr(draft_len), B, T, rows - T, V,
+                                               temperature, draft_temperature, _ptr(u_accept), _ptr(u_next),
+                                               _ptr(out["accept_len"]), _ptr(out["next"]), _ptr(out["accept_prob"]),
+                                               _stream(dev)), "dropmatch_verify_lossless")
+        return out
+
+    # -- dropmatch_dropout / dropmatch_dropout_grad
+    def dropout(self, x, K, p, seed, seq_base=0, out=None):
+        """x[B,T,d] (float32 or bfloat16) -> out[B,T,K,d]: K masked copies of every row, scaled by 1/(1-p), with the
+        masks of the verify calls.  Autograd does not see this call; `dropout_grad` is its gradient."""
+        if x.dim() != 3:
+            raise TypeError("x must have shape [B, T, d]")
+        B, T, d = x.shape
+        _, ld = self._rows(x, "x")
+        if out is None:
+            out, ld_out = _empty(B, T, K, d, dtype=x.dtype, device=self.device), d
+        else:
+            if out.shape != (B, T, K, d) or out.dtype != x.dtype:
+                raise TypeError("out must have shape [B, T, K, d] and x's dtype")
+            ld_out = self._rows(out, "out")[1]
+        _check(lib().dropmatch_dropout(self._h, _ptr(x), _DTYPES[x.dtype], ld, B, T, K, d, p, seed, seq_base, _ptr(out),
+                                       ld_out, _stream(self.device)), "dropmatch_dropout")
+        return out
+
+    def dropout_grad(self, grad, p, seed, seq_base=0, out=None):
+        """grad[B,T,K,d] of `dropout`'s copies -> [B,T,d]: the gradient of x, summed over the copies."""
+        if grad.dim() != 4:
+            raise TypeError("grad must have shape [B, T, K, d]")
+        B, T, K, d = grad.shape
+        _, ld = self._rows(grad, "grad")
+        if out is None:
+            out, ld_out = _empty(B, T, d, dtype=grad.dtype, device=self.device), d
+        else:
+            if out.shape != (B, T, d) or out.dtype != grad.dtype:
+                raise TypeError("out must have shape [B, T, d] and grad's dtype")
+            ld_out = self._rows(out, "out")[1]
+        _check(lib().dropmatch_dropout_grad(self._h, _ptr(grad), _DTYPES[grad.dtype], ld, B, T, K, d, p, seed, seq_base,
+                                            _ptr(out), ld_out, _stream(self.device)), "dropmatch_dropout_grad")
+        return out
 
     # the calls on rows are short: these checks are written for few Python-level operations
     def _on_device(self, t, what):

@@ -5,7 +5,9 @@
 #include <new>
 #include <vector>
 
+#include "dm_dropout.h"
 #include "dm_internal.h"
+#include "dm_lossless.h"
 #include "dm_rows.cuh"
 #include "dm_score.h"
 
@@ -267,6 +269,41 @@ bool grad_target_ok(const void* logits, int64_t ld, const void* grad, int64_t ld
     const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits), a1 = a0 + ((uintptr_t)(n_rows - 1) * (uintptr_t)ld + (uintptr_t)V) * elem;
     const uintptr_t b0 = reinterpret_cast<uintptr_t>(grad), b1 = b0 + ((uintptr_t)(n_rows - 1) * (uintptr_t)ld_grad + (uintptr_t)V) * elem;
     return a1 <= b0 || b1 <= a0;
+}
+
+// [first, last) of rows of `width` entries, one stride apart.
+bool ranges_overlap(const void* a, int64_t ld_a, int64_t rows_a, const void* b, int64_t ld_b, int64_t rows_b, int width, int elem) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), a1 = a0 + ((uintptr_t)(rows_a - 1) * (uintptr_t)ld_a + (uintptr_t)width) * (uintptr_t)elem;
+    const uintptr_t b0 = reinterpret_cast<uintptr_t>(b), b1 = b0 + ((uintptr_t)(rows_b - 1) * (uintptr_t)ld_b + (uintptr_t)width) * (uintptr_t)elem;
+    return a0 < b1 && b0 < a1;
+}
+
+// The two directions of the dropout operator.
+int run_dropout(dm_ctx* c, bool grad, const void* in, int64_t ld_in, void* out, int64_t ld_out, int dtype, int B, int T, int K,
+                int d, float p, uint64_t seed, uint64_t seq_base, void* stream) {
+    if (c == nullptr || (dtype != DM_F32 && dtype != DM_BF16)) return DM_EINVAL;
+    if (B < 0 || T < 0 || K < 1 || K > kMaxK || d < 1 || ld_in < d || ld_out < d) return DM_EINVAL;
+    if ((long long)B * T > 0x3FFFFFFFll / K) return DM_EINVAL;
+    if (d > kRowsMaxV) return DM_EUNSUPPORTED;
+    MaskKey mk;
+    if (!make_mask_key(p, seed, &mk)) return DM_EINVAL;
+    const int64_t rows = (int64_t)B * T;
+    if (rows == 0) return DM_OK;
+    if (!aligned_to_entry(in, dtype) || !aligned_to_entry(out, dtype)) return DM_EINVAL;
+    const bool in_place = in == out && K == 1 && (ld_in == ld_out || rows == 1);
+    if (!in_place && ranges_overlap(in, ld_in, grad ? rows * K : rows, out, ld_out, grad ? rows : rows * K, d, dtype == DM_F32 ? 4 : 2))
+        return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    DropoutParams dp{};
+    dp.in = in; dp.out = out;
+    dp.ld_in = ld_in; dp.ld_out = ld_out; dp.rows = rows;
+    dp.T = T; dp.K = K; dp.d = d;
+    dp.shared_masks = c->mask_mode;
+    dp.seq_base_lo = (uint32_t)seq_base;
+    dp.key0 = mk.key0; dp.key1 = mk.key1; dp.thr = mk.thr; dp.scale = mk.scale;
+    return launch_dropout(dp, dtype, grad, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
@@ -855,6 +892,49 @@ int dropmatch_distill(dm_ctx* c, const void* logits, int dtype, int64_t ld, int 
     rp.out_loss = out_loss;
     rp.out_grad = out_grad; rp.ld_grad = ld_grad;
     return launch_rows_distill(rp, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_verify_lossless(dm_ctx* c, const void* target, int dtype, int64_t ld_target, const void* draft_logits,
+                              int draft_dtype, int64_t ld_draft, const int32_t* draft, const int32_t* draft_len, int B, int T,
+                              int bonus_row, int V, float temperature, float draft_temperature, const float* u_accept,
+                              const float* u_next, int32_t* out_accept_len, int32_t* out_next_token, float* out_accept_prob,
+                              void* stream) {
+    if (c == nullptr || B < 0 || T < 0 || (bonus_row != 0 && bonus_row != 1) || T + bonus_row < 1) return DM_EINVAL;
+    if ((long long)B * ((long long)T + bonus_row) > (1ll << 27)) return DM_EUNSUPPORTED;     // (clusters of one launch)
+    RowsParams rp{}, rq{};
+    int st = rows_common(&rp, dtype, ld_target, B, V, temperature);
+    if (st != DM_OK) return st;
+    if (draft_logits != nullptr) {
+        st = rows_common(&rq, draft_dtype, ld_draft, B, V, draft_temperature);
+        if (st != DM_OK) return st;
+    }
+    if (B == 0) return DM_OK;
+    if (!aligned_to_entry(target, dtype) || u_next == nullptr || out_accept_len == nullptr || out_next_token == nullptr) return DM_EINVAL;
+    if (T > 0 && (draft == nullptr || u_accept == nullptr || out_accept_prob == nullptr)) return DM_EINVAL;
+    if (draft_logits != nullptr && !aligned_to_entry(draft_logits, draft_dtype)) return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    LosslessParams lp{};
+    lp.target = target; lp.ld_target = ld_target;
+    lp.draft_logits = T > 0 ? draft_logits : nullptr; lp.ld_draft = ld_draft;
+    lp.draft = draft; lp.draft_len = draft_len;
+    lp.B = B; lp.T = T; lp.bonus = bonus_row; lp.V = V;
+    lp.inv_temp = rp.inv_temp_d; lp.inv_draft_temp = rq.inv_temp_d;
+    lp.c = rp.c; lp.c_draft = rq.c;
+    lp.u_accept = u_accept; lp.u_next = u_next;
+    lp.out_accept_prob = out_accept_prob; lp.out_accept_len = out_accept_len; lp.out_next = out_next_token;
+    return launch_lossless(lp, dtype, draft_dtype, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_dropout(dm_ctx* c, const void* x, int dtype, int64_t ld, int B, int T, int K, int d, float p, uint64_t seed,
+                      uint64_t seq_base, void* out, int64_t ld_out, void* stream) {
+    return run_dropout(c, false, x, ld, out, ld_out, dtype, B, T, K, d, p, seed, seq_base, stream);
+}
+
+int dropmatch_dropout_grad(dm_ctx* c, const void* grad, int dtype, int64_t ld, int B, int T, int K, int d, float p,
+                           uint64_t seed, uint64_t seq_base, void* out_grad, int64_t ld_out, void* stream) {
+    return run_dropout(c, true, grad, ld, out_grad, ld_out, dtype, B, T, K, d, p, seed, seq_base, stream);
 }
 
 int dropmatch_verify_tree(dm_ctx* c, const void* H, const int32_t* node_token, const int32_t* node_parent,
