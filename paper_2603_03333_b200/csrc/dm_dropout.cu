@@ -97,6 +97,23 @@ struct Place {
     }
 };
 
+// The same value in every lane, and known to be: what follows from it stays out of the lanes' registers and pipes.
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0); }
+
+// Four entries of a lane's vector, kept or zero, as words of two or one entries.
+__device__ __forceinline__ void keep_words(const uint32_t* v, const uint4& w, uint32_t thr, uint32_t* o, float) {
+    o[0] = w.x >= thr ? v[0] : 0u;
+    o[1] = w.y >= thr ? v[1] : 0u;
+    o[2] = w.z >= thr ? v[2] : 0u;
+    o[3] = w.w >= thr ? v[3] : 0u;
+}
+__device__ __forceinline__ void keep_words(const uint32_t* v, const uint4& w, uint32_t thr, uint32_t* o, __nv_bfloat16) {
+    o[0] = w.x >= thr ? v[0] & 0xFFFFu : 0u;
+    if (w.y >= thr) o[0] |= v[0] & 0xFFFF0000u;
+    o[1] = w.z >= thr ? v[1] & 0xFFFFu : 0u;
+    if (w.w >= thr) o[1] |= v[1] & 0xFFFF0000u;
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void round_to(float x, float* out) { *out = x; }
@@ -108,7 +125,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 dropout_kernel(const DropoutParams P) {
     constexpr int Q = sizeof(T) == 2 ? 2 : 1, E = 4 * Q;     // quads and entries of a lane
-    const long long task = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const long long task = (long long)blockIdx.x * kWarps + warp_index();
     if (task >= P.n_tasks) return;                           // (the same for the whole warp)
     const Place<Q> at(P, task);
     const int lane = threadIdx.x & 31;
@@ -135,25 +152,20 @@ dropout_kernel(const DropoutParams P) {
     for (int n = 0; n < E; ++n) round_to(to_float(v[n]) * P.scale, &v[n]);
     T zero;
     round_to(0.0f, &zero);
-#pragma unroll 1
+#pragma unroll 2
     for (int i = at.path0; i < at.path1; ++i, out += P.ld_out) {
         const PhiloxPath path((uint32_t)i, at.t, P.key0);
         if (VEC) {
-            alignas(16) T o[E];
+            uint32_t o[4];
 #pragma unroll
-            for (int r = 0; r < Q; ++r) {
-                const uint4 w = quad[r].words(path, P.key0, P.key1);
-                o[4 * r + 0] = w.x >= P.thr ? v[4 * r + 0] : zero;
-                o[4 * r + 1] = w.y >= P.thr ? v[4 * r + 1] : zero;
-                o[4 * r + 2] = w.z >= P.thr ? v[4 * r + 2] : zero;
-                o[4 * r + 3] = w.w >= P.thr ? v[4 * r + 3] : zero;
-            }
+            for (int r = 0; r < Q; ++r)
+                keep_words(reinterpret_cast<const uint32_t*>(v) + 4 / Q * r, quad[r].words(path, P.key0, P.key1), P.thr, o + 4 / Q * r, zero);
             if (own + E <= P.d) {
-                *reinterpret_cast<uint4*>(out + own) = *reinterpret_cast<const uint4*>(o);
+                *reinterpret_cast<uint4*>(out + own) = make_uint4(o[0], o[1], o[2], o[3]);
             } else {
 #pragma unroll
                 for (int n = 0; n < E; ++n)
-                    if (own + n < P.d) out[own + n] = o[n];
+                    if (own + n < P.d) out[own + n] = reinterpret_cast<const T*>(o)[n];
             }
         } else {
 #pragma unroll
@@ -178,7 +190,7 @@ __global__ void __launch_bounds__(kThreads)
 dropout_grad_kernel(const DropoutParams P) {
     constexpr int Q = sizeof(T) == 2 ? 2 : 1, E = 4 * Q;
     __shared__ float s_part[kWarps][E * 32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
     const int group = warp & (P.n_groups - 1);               // (a power of two, at most kWarps)
     // tasks count chunks of all runs; a block takes kWarps / n_groups chunks
     const long long chunk_id = (long long)blockIdx.x * (kWarps / P.n_groups) + warp / P.n_groups;
@@ -198,7 +210,7 @@ dropout_grad_kernel(const DropoutParams P) {
     float sum[E];
 #pragma unroll
     for (int n = 0; n < E; ++n) sum[n] = 0.0f;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
 #pragma unroll 1
     for (int i0 = path0; i0 < path1; i0 += kAhead) {
         alignas(16) T v[kAhead][E];

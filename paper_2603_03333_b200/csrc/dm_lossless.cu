@@ -8,11 +8,14 @@
 // Two kernels, no workspace.
 // ratio_kernel: a cluster per drafted position reads both rows once (running maximum and sum of each, fp32
 // exponentials, sums of batches joined in fp64) and leaves min(1, p / q) in out_accept_prob.  Bounds: HBM.
-// next_kernel: a cluster per sequence finds n and draws from row n.  Decisions and the place in the cumulative sum
+// next_kernel: a cluster per sequence finds n and draws from row n.  Bounds: fp64 instructions.  Decisions and the place in the cumulative sum
 // are those of 64-bit arithmetic: a position whose u_t lies within 2^-16 of the fp32 ratio (far more than that
 // is off, see kBand) is decided again from fp64 sums, and all sums over row n are fp64 with exponentials good to
 // some 2^-50 (see exp_neg).  In fp32 a token of the flat tail of 100 thousand would come out one place off in about a
 // draw of ten, and two engines with equal random numbers would drift apart.
+#include <math.h>
+#include <string.h>
+
 #include "dm_lossless.h"
 #include "dm_ptx.cuh"
 
@@ -20,14 +23,12 @@ namespace dm {
 
 namespace {
 
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;      // (more than 8 has to be asked for)
 constexpr int kRatioThreads = 256, kRatioWarps = kRatioThreads / 32;
-constexpr int kNextThreads = 512, kNextWarps = kNextThreads / 32;
 // The fp32 ratio is p / q with the sums of two rows.  A term 2^w, w = (x - m) c, has a relative error of at most
 // 2 |w| ln 2 2^-24 (two roundings) + 2^-24 |w| ln 2 (c) + 2^-22 (the instruction); the mean of |w| ln 2 under the
 // row's own distribution is at most ln V <= 21, batches add 7 roundings: below 2^-16 / 4 for each row.
 constexpr float kBand = 1.0f / 65536.0f;
-constexpr double kFloor = -700.0;        // exponents below count as -infinity (e^-700 = 1e-304)
 
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
 __device__ __forceinline__ float ex2(float x) {
@@ -42,104 +43,140 @@ __device__ __forceinline__ void st_cluster_f64(uint32_t addr, double v) {
 __device__ __forceinline__ float entry(const float* row, long long j) { return row[j]; }
 __device__ __forceinline__ float entry(const __nv_bfloat16* row, long long j) { return __bfloat162float(row[j]); }
 
-// Maximum m of some entries of a row and the sum of exp((x - m) / T) over them.  A NaN, and +inf, make s a NaN.
-struct Sum { float m; double s; };
-
 // ---------------------------------------------------------------------------------------- ratios
-
-__device__ __forceinline__ Sum join(const Sum& a, const Sum& b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    const double fa = a.m == m ? 1.0 : (double)ex2((a.m - m) * c), fb = b.m == m ? 1.0 : (double)ex2((b.m - m) * c);
-    return Sum{m, a.s * fa + b.s * fb};
-}
 
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int kN = 4;
+    static constexpr uint32_t kNone = 0xFF800000u;      // -inf
     __device__ static void unpack(const uint4& v, float* x) {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+    }
+    template <int N> __device__ static float max(const uint4 (&v)[N]) {
+        float m = neg_inf();
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(v[i].x), __uint_as_float(v[i].y)), fmaxf(__uint_as_float(v[i].z), __uint_as_float(v[i].w))));
+        return m;
     }
 };
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int kN = 8;
+    static constexpr uint32_t kNone = 0xFF80FF80u;
     __device__ static void unpack(const uint4& v, float* x) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
     }
+    template <int N> __device__ static float max(const uint4 (&v)[N]) {      // two entries per instruction
+        uint32_t m = kNone;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[k]));
+        }
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+    }
 };
 
-template <int N>
-__device__ __forceinline__ void add_batch(Sum& a, const float (&x)[N], float c) {
-    float bm = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) bm = fmaxf(bm, x[i]);
-    if (bm > a.m) {
-        a.s *= (double)ex2((a.m - bm) * c);     // (0 * 0 at the first batch; a NaN stays)
-        a.m = bm;
-    }
-    const float ref = a.m == neg_inf() ? 0.0f : a.m;      // nothing but -inf so far: every term 0
-    const float2 m2 = make_float2(-ref, -ref), c2 = make_float2(c, c);
-    float2 s[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-    for (int i = 0; i < N; i += 2) {
-        const float2 z = __fmul2_rn(__fadd2_rn(make_float2(x[i], x[i + 1]), m2), c2);
-        s[(i >> 1) & 1] = __fadd2_rn(s[(i >> 1) & 1], make_float2(ex2(z.x), ex2(z.y)));
-    }
-    a.s += (double)((s[0].x + s[0].y) + (s[1].x + s[1].y));
-}
+// Maximum of some entries of a row and the sum of exp((x - m) / T) over them, with what additions have lost of it (Kahan: a
+// thread's share of a row may be any number of batches).  A NaN, and +inf, make the sum a NaN.
+struct Sum {
+    float m = neg_inf(), s = 0.0f, lost = 0.0f;
 
-// Entries [lo, hi) of a row by the CTA's threads: 16-byte vectors, and the ragged ends entry by entry.
-template <typename T>
-__device__ __forceinline__ Sum thread_sum(const T* row, int lo, int hi, float c) {
-    constexpr int kN = Vec<T>::kN, kBatch = 4;
-    Sum a{neg_inf(), 0.0};
-    const int off = (int)((reinterpret_cast<uintptr_t>(row + lo) & 15u) / sizeof(T));
-    int head = off == 0 ? 0 : kN - off;
-    head = min(head, hi - lo);
-    const int vecs = (hi - lo - head) / kN, tail = lo + head + vecs * kN;
-    if (threadIdx.x < 2 * kN) {     // at most kN - 1 entries on either side
-        const int j = threadIdx.x < kN ? lo + (int)threadIdx.x : tail + (int)threadIdx.x - kN;
-        const bool have = threadIdx.x < kN ? j < lo + head : j < hi;
-        const float x[2] = {have ? entry(row, j) : neg_inf(), neg_inf()};
-        add_batch(a, x, c);
-    }
-    const uint4* body = reinterpret_cast<const uint4*>(row + lo + head);
-    const uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;      // -inf
-#pragma unroll 1
-    for (int v0 = threadIdx.x; v0 < vecs; v0 += kBatch * kRatioThreads) {
-        uint4 v[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            v[i] = make_uint4(none, none, none, none);
-            if (v0 + i * kRatioThreads < vecs) v[i] = __ldg(body + v0 + i * kRatioThreads);
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N], float bm, float c) {      // N entries whose maximum is bm
+        if (bm > m) {
+            const float f = ex2((m - bm) * c);       // (0 at the first batch; a NaN stays)
+            s *= f;
+            lost *= f;
+            m = bm;
         }
-        float x[kBatch * kN];
+        const float ref = m == neg_inf() ? 0.0f : m;      // nothing but -inf so far: every term 0
+        const float2 m2 = make_float2(-ref, -ref), c2 = make_float2(c, c);
+        float2 t[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) Vec<T>::unpack(v[i], x + i * kN);
-        add_batch(a, x, c);
+        for (int i = 0; i < N; i += 2) {
+            const float2 z = __fmul2_rn(__fadd2_rn(make_float2(x[i], x[i + 1]), m2), c2);
+            t[(i >> 1) & 1] = __fadd2_rn(t[(i >> 1) & 1], make_float2(ex2(z.x), ex2(z.y)));
+        }
+        const float y = ((t[0].x + t[0].y) + (t[1].x + t[1].y)) - lost, sum = s + y;
+        lost = (sum - s) - y;
+        s = sum;
     }
-    return a;
+};
+
+// Entries [lo, hi) of a row: 16-byte vectors, and the ragged ends entry by entry.
+template <typename T>
+struct Share {
+    static constexpr int kN = Vec<T>::kN;
+    const T* row;
+    const uint4* body;
+    int lo, head, vecs, tail, hi;     // entries [lo, head) and [tail, hi) lie outside the vectors: at most kN - 1 each
+    __device__ __forceinline__ Share(const T* r, int l, int h) : row(r), lo(l), hi(h) {
+        const int off = (int)((reinterpret_cast<uintptr_t>(r + l) & 15u) / sizeof(T));
+        head = min(h, l + (off == 0 ? 0 : kN - off));
+        vecs = (h - head) / kN;
+        tail = head + vecs * kN;
+        body = reinterpret_cast<const uint4*>(r + head);
+    }
+    template <int N>
+    __device__ __forceinline__ static void add(Sum& a, const uint4 (&v)[N], float c) {
+        float x[N * kN];
+#pragma unroll
+        for (int i = 0; i < N; ++i) Vec<T>::unpack(v[i], x + i * kN);
+        a.add(x, Vec<T>::max(v), c);
+    }
+    __device__ __forceinline__ void add_ends(Sum& a, float c) const {
+        if (threadIdx.x >= 2 * kN) return;
+        const int j = threadIdx.x < kN ? lo + (int)threadIdx.x : tail + (int)threadIdx.x - kN;
+        const bool have = threadIdx.x < kN ? j < head : j < hi;
+        const float x[2] = {have ? entry(row, j) : neg_inf(), neg_inf()};
+        a.add(x, x[0], c);
+    }
+};
+
+// Sum of exp relative to a maximum above the thread's or warp's own.
+__device__ __forceinline__ float rescaled(float m, float s, float to, float c) { return m == to ? s : s * ex2((m - to) * c); }
+__device__ __forceinline__ float warp_max(float x) {
+    float y;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));      // (leaves a NaN out)
+    return y;
+}
+// Maximum and sum over the lanes of a warp, the same bits in every lane.
+__device__ __forceinline__ float2 join_lanes(float m, float s, float c) {
+    const float top = warp_max(m);
+    s = rescaled(m, s, top, c);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, off);
+    return make_float2(top, s);
+}
+// ... over n <= 32 parts in shared memory, `stride` apart.
+__device__ __forceinline__ float2 join_parts(const float2* part, int n, int stride, float c) {
+    const int lane = threadIdx.x & 31;
+    const float2 p = lane < n ? part[lane * stride] : make_float2(neg_inf(), 0.0f);
+    return join_lanes(p.x, p.y, c);
 }
 
-__device__ __forceinline__ Sum block_sum(Sum a, float c, Sum* s_warp) {
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const Sum o{__shfl_xor_sync(0xFFFFFFFFu, a.m, off), __shfl_xor_sync(0xFFFFFFFFu, a.s, off)};
-        a = (threadIdx.x & off) == 0 ? join(a, o, c) : join(o, a, c);
-    }
-    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = a;
-    __syncthreads();
-    a = s_warp[0];
-    for (int w = 1; w < kRatioWarps; ++w) a = join(a, s_warp[w], c);
-    return a;
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Every thread streams its vectors of the rows through its own slots of a ring in shared memory (no barrier: nobody
+// else reads them), kStages batches ahead.
+template <bool HAS_Q> constexpr int kVecs = HAS_Q ? 2 : 4;       // vectors of a row in a batch
+constexpr int kStages = 4;      // (three or six: 3 to 8 % slower)
+constexpr int kRatioSmem = kStages * 4 * kRatioThreads * 16;
 
 template <typename TP, typename TQ, bool HAS_Q>
 __global__ void __launch_bounds__(kRatioThreads)
 ratio_kernel(const LosslessParams P, int cluster) {
-    __shared__ Sum s_warp[2][kRatioWarps];
-    __shared__ __align__(16) double s_part[kMaxCluster][4];     // of every CTA: m and s of the target's row, of the draft's
+    extern __shared__ __align__(16) unsigned char s_ring[];
+    __shared__ __align__(16) float2 s_warp[kRatioWarps][2];     // maximum and sum of the target's row, of the draft's
+    __shared__ __align__(16) float2 s_part[kMaxCluster][2];     // of every CTA, written by it into the first
     ptx::griddep_launch_dependents();
     const int pos = (int)(blockIdx.x / (unsigned)cluster), rank = (int)(blockIdx.x % (unsigned)cluster);
     const int b = pos / P.T, t = pos - b * P.T;
@@ -152,6 +189,27 @@ ratio_kernel(const LosslessParams P, int cluster) {
     const TP* row_p = static_cast<const TP*>(P.target) + ((long long)b * (P.T + P.bonus) + t) * P.ld_target;
     const TQ* row_q = static_cast<const TQ*>(P.draft_logits) + (long long)pos * P.ld_draft;
     const int lo = (int)min((long long)P.V, (long long)rank * P.share), hi = (int)min((long long)P.V, (long long)lo + P.share);
+    const Share<TP> sp(row_p, lo, hi);
+    const Share<TQ> sq(row_q, lo, HAS_Q ? hi : lo);
+
+    constexpr int kV = kVecs<HAS_Q>, kRows = HAS_Q ? 2 : 1;
+    const uint4* slots = reinterpret_cast<const uint4*>(s_ring) + threadIdx.x;       // [stage][row][vector][thread]
+    const uint32_t slots_smem = ptx::smem_u32(slots);
+    const auto fetch = [&](int batch) {      // (an empty group past the end keeps the count)
+        const uint32_t to = slots_smem + (uint32_t)(batch % kStages) * (kRows * kV * kRatioThreads * 16);
+        const int v0 = batch * kV * kRatioThreads + (int)threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int v = v0 + i * kRatioThreads;
+            if (v < sp.vecs) copy_async(to + i * kRatioThreads * 16, sp.body + v);
+            if (HAS_Q && v < sq.vecs) copy_async(to + (kV + i) * kRatioThreads * 16, sq.body + v);
+        }
+        copies_commit();
+    };
+    const int both = HAS_Q ? min(sp.vecs, sq.vecs) : sp.vecs, most = max(sp.vecs, sq.vecs);
+    const int n_batches = (most + kV * kRatioThreads - 1) / (kV * kRatioThreads);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) fetch(i);
     const int tok = P.draft[pos];
     const bool in_range = (unsigned)tok < (unsigned)P.V;
     float xp = 0.0f, xq = 0.0f;
@@ -159,150 +217,189 @@ ratio_kernel(const LosslessParams P, int cluster) {
         xp = entry(row_p, tok);
         if (HAS_Q) xq = entry(row_q, tok);
     }
-    Sum p = thread_sum(row_p, lo, hi, P.c), q{0.0f, 1.0};
-    if (HAS_Q) q = thread_sum(row_q, lo, hi, P.c_draft);
-    p = block_sum(p, P.c, s_warp[0]);
-    if (HAS_Q) q = block_sum(q, P.c_draft, s_warp[1]);
-    if (cluster > 1) {
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-        if (threadIdx.x == 0) {
-            const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_part[rank][0]), 0);
-            st_cluster_f64(to, (double)p.m);
-            st_cluster_f64(to + 8, p.s);
-            st_cluster_f64(to + 16, (double)q.m);
-            st_cluster_f64(to + 24, q.s);
-        }
-        ptx::cluster_sync_all();
-        if (rank != 0 || threadIdx.x != 0) return;
-        for (int r = 1; r < cluster; ++r) {
-            p = join(p, Sum{(float)s_part[r][0], s_part[r][1]}, P.c);
-            if (HAS_Q) q = join(q, Sum{(float)s_part[r][2], s_part[r][3]}, P.c_draft);
+    Sum p, q;
+    sp.add_ends(p, P.c);
+    if (HAS_Q) sq.add_ends(q, P.c_draft);
+#pragma unroll 1
+    for (int batch = 0; batch < n_batches; ++batch) {
+        fetch(batch + kStages - 1);
+        copies_wait<kStages - 1>();
+        const uint4* at = slots + (batch % kStages) * (kRows * kV * kRatioThreads);
+        const int v0 = batch * kV * kRatioThreads + (int)threadIdx.x;
+        if (v0 + (kV - 1) * kRatioThreads < both) {
+            uint4 v[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) v[i] = at[i * kRatioThreads];
+            sp.add(p, v, P.c);
+            if (HAS_Q) {
+#pragma unroll
+                for (int i = 0; i < kV; ++i) v[i] = at[(kV + i) * kRatioThreads];
+                sq.add(q, v, P.c_draft);
+            }
+        } else {      // the last batch
+#pragma unroll 1
+            for (int i = 0; i < kV; ++i) {
+                if (v0 + i * kRatioThreads < sp.vecs) {
+                    const uint4 v[1] = {at[i * kRatioThreads]};
+                    sp.add(p, v, P.c);
+                }
+                if (HAS_Q && v0 + i * kRatioThreads < sq.vecs) {
+                    const uint4 v[1] = {at[(kV + i) * kRatioThreads]};
+                    sq.add(q, v, P.c_draft);
+                }
+            }
         }
     }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float2 wp = join_lanes(p.m, p.s, P.c), wq = HAS_Q ? join_lanes(q.m, q.s, P.c_draft) : make_float2(0.0f, 1.0f);
+    if (lane == 0) { s_warp[warp][0] = wp; s_warp[warp][1] = wq; }
+    __syncthreads();
+    // warp 0 takes the target's parts, warp 1 the draft's
+    float2 all = make_float2(0.0f, 1.0f);
+    const bool mine = warp < kRows;
+    const float c = warp == 0 ? P.c : P.c_draft;
+    if (mine) all = join_parts(&s_warp[0][warp], kRatioWarps, 2, c);
+    if (cluster > 1) {
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        if (mine && lane == 0) {
+            const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_part[rank][warp]), 0);
+            ptx::st_cluster_u32(to, __float_as_uint(all.x));
+            ptx::st_cluster_u32(to + 4, __float_as_uint(all.y));
+        }
+        __syncwarp();
+        ptx::cluster_sync_all();
+        if (rank != 0) return;
+        if (mine) all = join_parts(&s_part[0][warp], cluster, 2, c);
+    }
+    if (HAS_Q) {
+        __syncthreads();
+        if (warp == 1 && lane == 0) s_warp[0][1] = all;
+        __syncthreads();
+    }
     if (threadIdx.x != 0) return;
+    const float2 other = HAS_Q ? s_warp[0][1] : make_float2(0.0f, 1.0f);
     float ratio = 0.0f;
-    if (isnan(p.s) || isnan(q.s)) {
+    if (isnan(all.y) || isnan(other.y)) {
         ratio = __uint_as_float(0x7FC00000u);
     } else if (in_range && xp > neg_inf()) {          // (a row of nothing but -inf has no such entry)
-        const double lp = ((double)xp - (double)p.m) * P.inv_temp - log(p.s);
-        if (!HAS_Q) ratio = (float)exp(lp);
-        else if (xq == neg_inf()) ratio = 1.0f;
-        else ratio = (float)exp(lp - (((double)xq - (double)q.m) * P.inv_draft_temp - log(q.s)));
-        ratio = fminf(ratio, 1.0f);
+        double l = ((double)xp - (double)all.x) * P.inv_temp - log((double)all.y);
+        if (HAS_Q) l -= ((double)xq - (double)other.x) * P.inv_draft_temp - log((double)other.y);
+        ratio = HAS_Q && xq == neg_inf() ? 1.0f : fminf((float)exp(l), 1.0f);
     }
     P.out_accept_prob[pos] = ratio;
 }
 
 // ------------------------------------------------------------------------------------------ next
 
-// exp(z) for z <= 0 (0 below kFloor; a NaN stays): z = n ln2/16 + r, |r| <= ln2/32, exp(z) = 2^(n div 16) table[n mod 16] e^r
-// with e^r by its Taylor polynomial (r^7/7! < 2^-51): table-driven reduction after Tang, ACM TOMS 15 (1989).  Sixteen
-// doubles lie in as many pairs of banks: lanes never conflict.
-__device__ __forceinline__ double exp_neg(double z, const double* table) {
-    const double shift = 6755399441055744.0;        // 1.5 2^52: the sum's low word holds the rounded quotient
-    const double k = fma(z, 23.083120654223414, shift);
-    const int n = __double2loint(k);
-    const double r = fma(k - shift, -0.043321698784996581, z);
-    double e = fma(r, 1.0 / 720.0, 1.0 / 120.0);
-    e = fma(r, e, 1.0 / 24.0);
-    e = fma(r, e, 1.0 / 6.0);
-    e = fma(r, e, 0.5);
+// exp((x - m) / T) for x <= m in fp64, up to a factor that is the same for all entries of a row, straight through: with
+// k = round(16 log2(e) x / T) and r = x - k T ln2/16 it is 2^((k - k0)/16) e^(r/T), k0 the row's (that of its maximum), so that
+// 2^((k - k0)/16) = 2^e table[j], j the low four bits of k - k0; e^(r/T) by its Taylor polynomial, the powers of
+// 1/T and the factorials in the coefficients: table-driven reduction after Tang, ACM TOMS 15 (1989).  |r/T| <= ln2/32, so
+// what the polynomial leaves out is below 2^-42 of the value.  Twenty instructions, eight of them fp64; with a
+// polynomial for |r/T| <= ln2/2 that needs no table, three fp64 instructions more.  Sixteen doubles lie in as many pairs of banks: lanes never
+// conflict.  Where k would be beyond 2^17, x - m takes x's place: fp32 holds it exactly for every entry that counts.
+// x = -inf: 0.  A NaN, or +inf (then m is +inf too): NaN.  Below e^-700 of the maximum: 0.
+struct Row64 {
+    float ref, bias;      // m or 0; 1.5 2^23 - k0
+    double offset;        // 2^52 + (bits of 1.5 2^23) - k0
+    double base;          // the x of weight 1
+    __device__ __forceinline__ Row64() {}
+    __device__ __forceinline__ Row64(float m, const Exp64& E) {
+        const bool far = fabsf(m) * E.c16 >= 131072.0f, none = m == neg_inf();
+        ref = far && !none ? m : 0.0f;
+        const float k0 = far ? 0.0f : rintf(m * E.c16);
+        bias = 12582912.0f - k0;
+        offset = 4503599627370496.0 + 1262485504.0 - (double)k0;
+        base = (double)ref + (double)k0 * E.step;
+    }
+};
+__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table) {
+    const float d = x - R.ref, kf = fmaf(d, E.c16, R.bias);      // 1.5 2^23 + (k - k0): rounded to whole numbers, in the low bits
+    const int bits = __float_as_int(fmaxf(kf, 12582912.0f - 16300.0f));
+    const double k = __hiloint2double(0x43300000, bits) - R.offset;
+    const double r = fma(-k, E.step, (double)d);
+    double e = fma(r, E.a[4], E.a[3]);
+    e = fma(r, e, E.a[2]);
+    e = fma(r, e, E.a[1]);
+    e = fma(r, e, E.a[0]);
     e = fma(r, e, 1.0);
-    e = fma(r, e, 1.0) * table[n & 15];
-    e = __hiloint2double(__double2hiint(e) + (n >> 4) * 1048576, __double2loint(e));
-    return z < kFloor ? 0.0 : e;
+    const double t = table[bits & 15];       // (its high word is less j 2^16, so that adding all of k - k0 there adds the exponent)
+    e *= __hiloint2double((int)((uint32_t)__double2hiint(t) + ((uint32_t)bits << 16)), __double2loint(t));
+    return kf < 12582912.0f - 16160.0f ? 0.0 : e;
 }
 
-__device__ __forceinline__ Sum join64(const Sum& a, const Sum& b, double inv_temp, const double* table) {
-    const float m = fmaxf(a.m, b.m);
-    const double fa = a.m == m ? 1.0 : exp_neg(((double)a.m - (double)m) * inv_temp, table);
-    const double fb = b.m == m ? 1.0 : exp_neg(((double)b.m - (double)m) * inv_temp, table);
-    return Sum{m, a.s * fa + b.s * fb};
-}
-
-// exp((x - m) / T); m = -inf (a row of nothing else): 0.  x = +inf or NaN: NaN.
-__device__ __forceinline__ double weight(float x, float m, double inv_temp, const double* table) {
-    if (!(x > neg_inf()) && x == x) return 0.0;
-    const double e = exp_neg(((double)x - (double)m) * inv_temp, table);
-    return x == x && x < -neg_inf() ? e : __longlong_as_double(0x7FF8000000000000ll);
-}
-
-// Sum over entries [lo, hi) by a warp, lanes on neighbouring entries.
-template <typename T>
-__device__ __forceinline__ Sum warp_sum64(const T* row, int lo, int hi, double inv_temp, const double* table) {
-    constexpr int kBatch = 8;
+// Which of the lanes' parts (of a CTA, of a warp) holds the place `at` of their cumulative weight; `at` becomes the place
+// within it.  Where rounding (or a random number of 1) leaves none, the last part with any weight, and no place in it is reached.
+__device__ __forceinline__ int part_of(double& at, double w) {
     const int lane = threadIdx.x & 31;
-    Sum a{neg_inf(), 0.0};
-#pragma unroll 1
-    for (int j0 = lo; j0 < hi; j0 += 32 * kBatch) {
-        float x[kBatch];
+    const bool any = w > 0.0;
+    double sum = any ? w : 0.0;
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) x[i] = hi - j0 > 32 * i + lane ? entry(row, j0 + 32 * i + lane) : neg_inf();
-        float bm = x[0];
-#pragma unroll
-        for (int i = 1; i < kBatch; ++i) bm = fmaxf(bm, x[i]);
-        if (bm > a.m) {
-            a.s = a.s == 0.0 ? 0.0 : a.s * exp_neg(((double)a.m - (double)bm) * inv_temp, table);
-            a.m = bm;
-        }
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) a.s += weight(x[i], a.m, inv_temp, table);
+    for (int off = 1; off < 32; off <<= 1) {
+        const double o = __shfl_up_sync(0xFFFFFFFFu, sum, off);
+        if (lane >= off) sum += o;
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const Sum o{__shfl_xor_sync(0xFFFFFFFFu, a.m, off), __shfl_xor_sync(0xFFFFFFFFu, a.s, off)};
-        a = (lane & off) == 0 ? join64(a, o, inv_temp, table) : join64(o, a, inv_temp, table);
+    double before = __shfl_up_sync(0xFFFFFFFFu, sum, 1);
+    if (lane == 0) before = 0.0;
+    const uint32_t with = __ballot_sync(0xFFFFFFFFu, any), reached = __ballot_sync(0xFFFFFFFFu, any && at < sum);
+    if (reached == 0) {
+        at = __longlong_as_double(0x7FF0000000000000ll);
+        return with == 0 ? 0 : 31 - __clz(with);
     }
-    return a;
-}
-
-// Which of `count` parts holds the place `at` of their cumulative weight; `at` becomes the place within it.  Where
-// rounding (or a random number of 1) leaves none, the last part with any weight, and no place in it is reached.
-template <typename F>
-__device__ __forceinline__ int part_of(double& at, int count, F weight_of) {
-    double sum = 0.0;
-    int last = 0;
-    for (int i = 0; i < count; ++i) {
-        const double w = weight_of(i);
-        if (!(w > 0.0)) continue;
-        if (at < sum + w) {
-            at -= sum;
-            return i;
-        }
-        sum += w;
-        last = i;
-    }
-    at = __longlong_as_double(0x7FF0000000000000ll);
-    return last;
+    const int pick = __ffs(reached) - 1;
+    at -= __shfl_sync(0xFFFFFFFFu, before, pick);
+    return pick;
 }
 
 constexpr int kNone = 0x7FFFFFFF;
 
+template <int kNextWarps>
 struct NextShared {
     double table[16];
+    float2 warp_sum[kNextWarps][2];
     double warp_part[kNextWarps][4];
     double part[2][kMaxCluster][4];     // of every CTA, written by it; two sets in turn, so that one barrier per exchange does
     double scan[kNextWarps];
     int found, last;
 };
 
-// Everybody's four numbers for everybody: CTA `rank` writes v into set `set` of all CTAs of the cluster.
-__device__ __forceinline__ void exchange(NextShared& S, int set, int rank, int cluster, const double (&v)[4]) {
+// Lane i of warp 0 hands v to CTA i of the cluster: everybody's four numbers for everybody.
+template <typename S_>
+__device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, const double (&v)[4]) {
     if (threadIdx.x < (unsigned)cluster) {
         const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&S.part[set][rank][0]), threadIdx.x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) st_cluster_f64(to + 8 * i, v[i]);
     }
+    __syncwarp();
     ptx::cluster_sync_all();
 }
+// Sums over the lanes, the same bits in every lane.
+__device__ __forceinline__ void add_lanes(double (&a)[4]) {
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] += __shfl_xor_sync(0xFFFFFFFFu, a[i], off);
+}
 
-template <typename TP, typename TQ, bool HAS_Q>
-__global__ void __launch_bounds__(kNextThreads)
+// The row that a token is drawn from.  Weights of entry v, in units of 1 / sum p:
+//   p(v) = exp(x / T) up to a factor (see Row64),  q(v) likewise,  r(v) = max(p(v) - rho q(v), 0)  with rho = sum p / sum q.
+// Sums over r need rho, which needs the sums over p and q: one pass takes all of them, with the entries that count
+// decided by an fp32 rho (off by some 2^-20) that a quick pass over the row has left behind.  Sums A of p and D of q over
+// those entries then give sum r = A - rho D for the rho that came out: an entry on the wrong side of the
+// border is off by less than |rho - rho~| q(v), and only entries that close to the border are, so that the sum
+// is off by the square of that, unless there is little but such entries: then the pass is done once more.
+// (Two passes, the first for rho, are as exact and took 40 % longer.)
+
+// THREADS: 256, three CTAs per SM, or 512 where there are fewer CTAs than SMs.
+template <typename TP, typename TQ, bool HAS_Q, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
 next_kernel(const LosslessParams P, int cluster) {
-    __shared__ NextShared S;
+    constexpr int kNextThreads = THREADS, kNextWarps = THREADS / 32;
+    __shared__ NextShared<kNextWarps> S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = (int)(blockIdx.x / (unsigned)cluster), rank = (int)(blockIdx.x % (unsigned)cluster);
-    if (threadIdx.x < 16) S.table[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    if (threadIdx.x < 16) S.table[threadIdx.x] = P.table[threadIdx.x];
     if (threadIdx.x == 0) { S.found = kNone; S.last = -1; }
     ptx::cluster_sync_all();      // (the other CTAs have started: their shared memory may be written)
     ptx::griddep_wait();
@@ -316,30 +413,115 @@ next_kernel(const LosslessParams P, int cluster) {
     const TQ* draft_rows = static_cast<const TQ*>(P.draft_logits) + (long long)b * P.T * P.ld_draft;
     int set = 0;
 
-    Sum p{neg_inf(), 0.0}, q{neg_inf(), 0.0};
-    auto sums = [&](int t, bool with_q) {       // fp64 sums of row t of both models, known to every thread of the cluster
-        Sum a = warp_sum64(target + (long long)t * P.ld_target, w_lo, w_hi, P.inv_temp, S.table), o{neg_inf(), 0.0};
-        if (HAS_Q && with_q) o = warp_sum64(draft_rows + (long long)t * P.ld_draft, w_lo, w_hi, P.inv_draft_temp, S.table);
-        if (lane == 0) { S.warp_part[warp][0] = a.m; S.warp_part[warp][1] = a.s; S.warp_part[warp][2] = o.m; S.warp_part[warp][3] = o.s; }
+    // What every thread of the cluster knows about a row.
+    Row64 at_p, at_q;
+    double rho = 0.0, sum_p = 0.0, sum_q = 0.0, sum_a = 0.0, sum_d = 0.0;
+    const TP* row_p = target;
+    const TQ* row_q = draft_rows;
+
+    // fp64 sums over the row; entry `skip` of p counts as masked.  The warps' and CTAs' sums of p, q, A, D stay in warp_part
+    // and part[set ^ 1].
+    auto sums = [&](bool with_q, int skip) {
+        double a[4] = {};
+        const auto add = [&](float x, float y) {
+            const double p = weight(x, at_p, P.e, S.table);
+            a[0] += p;
+            if (HAS_Q && with_q) {
+                const double q = weight(y, at_q, P.e_draft, S.table);
+                a[1] += q;
+                if (fma(-rho, q, p) > 0.0) {
+                    a[2] += p;
+                    a[3] += q;
+                }
+            }
+        };
+        constexpr int kAhead = 4;
+        const TP* at_x = row_p + w_lo + lane;
+        const TQ* at_y = row_q + w_lo + lane;
+        int left = w_hi - w_lo - lane, off = skip - w_lo - lane;      // entries from the lane's on; where the one to skip is
+        const auto load = [&](float (&x)[kAhead], float (&y)[kAhead]) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                x[i] = entry(at_x, 32 * i);
+                if (HAS_Q && with_q) y[i] = entry(at_y, 32 * i);
+                else if (off == 32 * i) x[i] = neg_inf();
+            }
+            at_x += 32 * kAhead;
+            at_y += 32 * kAhead;
+            left -= 32 * kAhead;
+            off -= 32 * kAhead;
+        };
+        float x[kAhead], y[kAhead] = {}, x2[kAhead], y2[kAhead] = {};
+        bool more = left > 32 * (kAhead - 1);
+        if (more) load(x, y);
+#pragma unroll 1
+        while (more) {       // two batches of loads on their way
+            more = left > 32 * (kAhead - 1);
+            if (more) load(x2, y2);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) add(x[i], y[i]);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) { x[i] = x2[i]; y[i] = y2[i]; }
+        }
+#pragma unroll 1
+        for (; left > 0; left -= 32, off -= 32, at_x += 32, at_y += 32)
+            add(off == 0 ? neg_inf() : entry(at_x, 0), HAS_Q && with_q ? entry(at_y, 0) : 0.0f);
+        __syncwarp();
+        add_lanes(a);
+        if (lane < 4) S.warp_part[warp][lane] = lane == 0 ? a[0] : lane == 1 ? a[1] : lane == 2 ? a[2] : a[3];
         __syncthreads();
-        p = q = Sum{neg_inf(), 0.0};
-        for (int w = 0; w < kNextWarps; ++w) {
-            p = join64(p, Sum{(float)S.warp_part[w][0], S.warp_part[w][1]}, P.inv_temp, S.table);
-            if (HAS_Q && with_q) q = join64(q, Sum{(float)S.warp_part[w][2], S.warp_part[w][3]}, P.inv_draft_temp, S.table);
+        if (warp == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = lane < kNextWarps ? S.warp_part[lane][i] : 0.0;
+            add_lanes(a);
         }
-        const double v[4] = {(double)p.m, p.s, (double)q.m, q.s};
-        exchange(S, set, rank, cluster, v);
-        p = q = Sum{neg_inf(), 0.0};
-        for (int r = 0; r < cluster; ++r) {
-            const double* o4 = S.part[set][r];
-            p = join64(p, Sum{(float)o4[0], o4[1]}, P.inv_temp, S.table);
-            if (HAS_Q && with_q) q = join64(q, Sum{(float)o4[2], o4[3]}, P.inv_draft_temp, S.table);
-        }
+        exchange(S, set, rank, cluster, a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = lane < cluster ? S.part[set][lane][i] : 0.0;
+        add_lanes(a);
+        sum_p = a[0]; sum_q = a[1]; sum_a = a[2]; sum_d = a[3];
         set ^= 1;
+    };
+    // Row t: the maxima and an fp32 rho, then the sums.
+    auto look_at = [&](int t, bool with_q, int skip) {
+        row_p = target + (long long)t * P.ld_target;
+        row_q = draft_rows + (long long)t * P.ld_draft;
+        const bool two = HAS_Q && with_q;
+        Sum p, q;
+        const Share<TP> sp(row_p, lo, hi);
+        const Share<TQ> sq(row_q, lo, two ? hi : lo);
+#pragma unroll 1
+        for (int v0 = threadIdx.x; v0 < max(sp.vecs, sq.vecs); v0 += kNextThreads) {
+            uint4 v[1] = {make_uint4(Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone)};
+            uint4 w[1] = {make_uint4(Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone)};
+            if (v0 < sp.vecs) v[0] = sp.body[v0];
+            if (v0 < sq.vecs) w[0] = sq.body[v0];
+            sp.add(p, v, P.c);
+            if (two) sq.add(q, w, P.c_draft);
+        }
+        sp.add_ends(p, P.c);
+        if (two) sq.add_ends(q, P.c_draft);
+        const float2 wp = join_lanes(p.m, p.s, P.c), wq = join_lanes(q.m, q.s, P.c_draft);
+        if (lane == 0) { S.warp_sum[warp][0] = wp; S.warp_sum[warp][1] = wq; }
+        __syncthreads();
+        double v[4] = {};
+        if (warp == 0) {
+            const float2 cp = join_parts(&S.warp_sum[0][0], kNextWarps, 2, P.c), cq = join_parts(&S.warp_sum[0][1], kNextWarps, 2, P.c_draft);
+            v[0] = cp.x; v[1] = cp.y; v[2] = cq.x; v[3] = cq.y;
+        }
+        exchange(S, set, rank, cluster, v);
+        const double* part = S.part[set][lane < cluster ? lane : 0];
+        const float2 ap = join_lanes((float)part[0], lane < cluster ? (float)part[1] : 0.0f, P.c);
+        const float2 aq = join_lanes((float)part[2], lane < cluster ? (float)part[3] : 0.0f, P.c_draft);
+        at_p = Row64(ap.x, P.e);
+        at_q = Row64(aq.x, P.e_draft);
+        rho = aq.y > 0.0f ? (double)ap.y * weight(ap.x, at_p, P.e, S.table) / ((double)aq.y * weight(aq.x, at_q, P.e_draft, S.table)) : 0.0;
+        set ^= 1;
+        sums(with_q, skip);
     };
 
     // the accepted prefix: the first position that is not surely accepted, decided in 64 bits if it may be
-    int n = 0, known = -1;       // known: the row whose sums are in p and q
+    int n = 0, known = -1;       // known: the row whose sums these are
     while (n < len) {
         const int t = n + lane;
         float a = 1.0f, u = 0.0f;
@@ -353,14 +535,14 @@ next_kernel(const LosslessParams P, int cluster) {
         if (u > a * (1.0f + kBand)) break;
         const int tok = P.draft[(long long)b * P.T + n];
         if ((unsigned)tok >= (unsigned)P.V) break;
-        sums(n, true);
+        look_at(n, true, -1);
         known = n;
-        const float xp = entry(target + (long long)n * P.ld_target, tok), xq = HAS_Q ? entry(draft_rows + (long long)n * P.ld_draft, tok) : 0.0f;
-        if (!(xp > neg_inf()) || !(p.s > 0.0) || !(HAS_Q ? q.s >= 0.0 : true)) break;     // p(x) = 0, or a NaN or +inf in a row
+        const float xp = entry(row_p, tok), xq = HAS_Q ? entry(row_q, tok) : 0.0f;
+        if (!(xp > neg_inf()) || !(sum_p > 0.0) || (HAS_Q && !(sum_q >= 0.0))) break;     // p(x) = 0, or a NaN or +inf in a row
         if (!HAS_Q || xq > neg_inf()) {      // (q(x) = 0 otherwise)
             // by logarithms: p(x) and q(x) may both lie below fp64's range
-            double l = ((double)xp - (double)p.m) * P.inv_temp - log(p.s);
-            if (HAS_Q) l -= ((double)xq - (double)q.m) * P.inv_draft_temp - log(q.s);
+            double l = ((double)xp - at_p.base) * P.inv_temp - log(sum_p);
+            if (HAS_Q) l -= ((double)xq - at_q.base) * P.inv_draft_temp - log(sum_q);
             if (!(u <= 0.0f || (double)u < exp(l))) break;
         }
         ++n;
@@ -371,54 +553,40 @@ next_kernel(const LosslessParams P, int cluster) {
         return;
     }
 
-    // weights of row n: r = max(p - q, 0) if a token was rejected there, else p; p too, where r leaves nothing
+    // Row n: weights r where a token was rejected against a distribution; p without the token where it was rejected by a
+    // drafter that has none; else p.
     const bool rejected = n < len;
-    if (known != n) sums(n, rejected);
-    const int tok = rejected ? P.draft[(long long)b * P.T + n] : -1;
-    const TP* row_p = target + (long long)n * P.ld_target;
-    const TQ* row_q = draft_rows + (long long)n * P.ld_draft;
-    const double inv_p = 1.0 / p.s, inv_q = HAS_Q && rejected && q.s != 0.0 ? 1.0 / q.s : 0.0;
-    auto weights = [&](int j, double& all, double& rest) {
-        all = weight(entry(row_p, j), p.m, P.inv_temp, S.table) * inv_p;
-        rest = all;
-        if (!rejected) return;
-        if (HAS_Q) {
-            const double other = weight(entry(row_q, j), q.m, P.inv_draft_temp, S.table) * inv_q;
-            rest = other >= all ? 0.0 : all - other;      // (a NaN in either stays)
-        } else if (j == tok) {
-            rest = 0.0;
+    const int skip = rejected && !HAS_Q ? P.draft[(long long)b * P.T + n] : -1;
+    bool against_q = HAS_Q && rejected;
+    if (known != n || skip >= 0) look_at(n, against_q, skip);
+    double total = sum_p;
+    if (against_q) {
+        const double guess = rho;
+        rho = sum_q > 0.0 ? sum_p / sum_q : 0.0;
+        total = sum_a - rho * sum_d;
+        if (rho != guess && !(total > sum_p * 0.0009765625)) {      // p and q nearly equal (or not numbers): with the rho that came out
+            sums(true, -1);
+            total = sum_a - rho * sum_d;
         }
-    };
-    double sum_all = 0.0, sum_rest = 0.0;
-#pragma unroll 4
-    for (int j = w_lo + lane; j < w_hi; j += 32) {
-        double all, rest;
-        weights(j, all, rest);
-        sum_all += all;
-        sum_rest += rest;
+        if (total == 0.0) {       // p - q leaves nothing: p
+            against_q = false;
+            total = sum_p;
+        }
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        sum_all += __shfl_xor_sync(0xFFFFFFFFu, sum_all, off);
-        sum_rest += __shfl_xor_sync(0xFFFFFFFFu, sum_rest, off);
-    }
-    if (lane == 0) { S.warp_part[warp][0] = sum_all; S.warp_part[warp][1] = sum_rest; }
-    __syncthreads();
-    double v[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int w = 0; w < kNextWarps; ++w) { v[0] += S.warp_part[w][0]; v[1] += S.warp_part[w][1]; }
-    exchange(S, set, rank, cluster, v);
-    double total[2] = {0.0, 0.0};
-    for (int r = 0; r < cluster; ++r) { total[0] += S.part[set][r][0]; total[1] += S.part[set][r][1]; }
     // (no CTA writes to another from here on: each may leave when it is done)
-    const int use = total[1] > 0.0 ? 1 : 0;
-    if (!(total[use] > 0.0)) {      // nothing to draw from, or a NaN or +inf in a row
+    if (!(total > 0.0) || (HAS_Q && rejected && !(sum_q >= 0.0))) {      // nothing to draw from, or a NaN or +inf in a row
         if (rank == 0 && threadIdx.x == 0) P.out_next[b] = -1;
         return;
     }
+    const auto entry_weight = [&](int j) {
+        const double p = j == skip ? 0.0 : weight(entry(row_p, j), at_p, P.e, S.table);
+        return HAS_Q && against_q ? fmax(fma(-rho, weight(entry(row_q, j), at_q, P.e_draft, S.table), p), 0.0) : p;
+    };
+    const auto part_weight = [&](const double* part) { return against_q ? part[2] - rho * part[3] : part[0]; };
     // the part that holds the place u_next * total: a CTA's, then a warp's
-    double place = (double)P.u_next[b] * total[use];
-    if (part_of(place, cluster, [&](int r) { return S.part[set][r][use]; }) != rank) return;
-    const int pick = part_of(place, kNextWarps, [&](int w) { return S.warp_part[w][use]; });
+    double place = (double)P.u_next[b] * total;
+    if (part_of(place, lane < cluster ? part_weight(S.part[set ^ 1][lane]) : 0.0) != rank) return;
+    const int pick = part_of(place, lane < kNextWarps ? part_weight(S.warp_part[lane]) : 0.0);
     // the entry within that: the whole block, a run of four entries per thread
     const int p_lo = (int)min((long long)hi, (long long)lo + (long long)pick * per_warp), p_hi = (int)min((long long)hi, (long long)p_lo + per_warp);
     double base = 0.0;
@@ -429,9 +597,7 @@ next_kernel(const LosslessParams P, int cluster) {
         const int first = j0 + 4 * (int)threadIdx.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            double all = 0.0, rest = 0.0;
-            if (first + i < p_hi) weights(first + i, all, rest);
-            r[i] = use ? rest : all;
+            r[i] = first + i < p_hi ? entry_weight(first + i) : 0.0;
             run += r[i];
             if (r[i] > 0.0) last = first + i;
         }
@@ -444,8 +610,11 @@ next_kernel(const LosslessParams P, int cluster) {
         if (lane == 31) S.scan[warp] = incl;
         __syncthreads();
         double cum = base + (incl - run);
-        for (int w = 0; w < warp; ++w) cum += S.scan[w];
-        for (int w = 0; w < kNextWarps; ++w) base += S.scan[w];
+#pragma unroll 1
+        for (int w = 0; w < kNextWarps; ++w) {
+            if (w < warp) cum += S.scan[w];
+            base += S.scan[w];
+        }
         int found = kNone;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -463,37 +632,48 @@ next_kernel(const LosslessParams P, int cluster) {
 
 template <typename TP, typename TQ, bool HAS_Q>
 int launch(LosslessParams& P, cudaStream_t stream) {
-    const auto config = [&](cudaLaunchAttribute* attrs, int positions, int cluster, int threads, bool behind) {
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)positions * (unsigned)cluster);
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.stream = stream;
-        cfg.attrs = attrs;
+    // CTAs that share a row: at most `most` on the GPU in all, with at least 2048 entries each; parts are whole 16-byte vectors
+    const auto cut = [&](long long rows, long long most) {
+        int cluster = 1;
+        while (cluster < kMaxCluster && P.V / (2 * cluster) >= 2048 && 2 * rows * cluster <= most) cluster *= 2;
+        P.share = ((P.V + cluster - 1) / cluster + 7) & ~7;
+        return cluster;
+    };
+    const auto run = [&](auto* kernel, int positions, int cluster, int threads, int smem, bool behind) {
+        if ((smem > 47 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) ||
+            (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
+            cudaGetLastError();
+            return DM_ECUDA;
+        }
+        cudaLaunchAttribute attrs[2]{};
         attrs[0].id = cudaLaunchAttributeClusterDimension;
         attrs[0].val.clusterDim.x = (unsigned)cluster; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
         attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attrs[1].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)positions * (unsigned)cluster);
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = stream;
+        cfg.attrs = attrs;
         cfg.numAttrs = behind ? 2 : 1;
-        return cfg;
+        if (cudaLaunchKernelEx(&cfg, kernel, P, cluster) != cudaSuccess || cudaGetLastError() != cudaSuccess) {
+            cudaGetLastError();
+            return DM_ECUDA;
+        }
+        return DM_OK;
     };
-    // CTAs of a row: as many as have at least 2048 entries each, whole 16-byte vectors
-    const auto cut = [&](int least) {
-        int cluster = kMaxCluster;
-        while (cluster > 1 && P.V / cluster < least) cluster /= 2;
-        P.share = ((P.V + cluster - 1) / cluster + 7) & ~7;
-        return cluster;
-    };
-    cudaLaunchAttribute attrs[2]{};
     if (P.T > 0) {
-        const int cluster = cut(2048);
-        const cudaLaunchConfig_t cfg = config(attrs, P.B * P.T, cluster, kRatioThreads, false);
-        if (cudaLaunchKernelEx(&cfg, ratio_kernel<TP, TQ, HAS_Q>, P, cluster) != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+        // (96 x 7 rows of 151936: 2 or 4 CTAs each the same, 8: 8 % slower, 16: 40 %; 5 rows: 16 the fastest)
+        const int cluster = cut((long long)P.B * P.T, 2800);
+        const int st = run(ratio_kernel<TP, TQ, HAS_Q>, P.B * P.T, cluster, kRatioThreads, kRatioSmem, false);
+        if (st != DM_OK) return st;
     }
-    const int cluster = cut(2048);
+    // (96 sequences of 151936: 8 CTAs each 168 us in all, 4: 175, 16: 190; one sequence: 16 the fastest)
+    const int cluster = cut(P.B, 888);
     // (behind the ratios: the kernel waits for them before it reads anything)
-    const cudaLaunchConfig_t cfg = config(attrs, P.B, cluster, kNextThreads, P.T > 0);
-    if (cudaLaunchKernelEx(&cfg, next_kernel<TP, TQ, HAS_Q>, P, cluster) != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
-    return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ECUDA;
+    return P.B * cluster <= 148 ? run(next_kernel<TP, TQ, HAS_Q, 512>, P.B, cluster, 512, 0, P.T > 0)
+                                : run(next_kernel<TP, TQ, HAS_Q, 256>, P.B, cluster, 256, 0, P.T > 0);
 }
 
 template <typename TP>
@@ -506,6 +686,23 @@ int launch_target(LosslessParams& P, int draft_dtype, cudaStream_t stream) {
 }  // namespace
 
 int launch_lossless(LosslessParams P, int dtype, int draft_dtype, cudaStream_t stream) {
+    const auto constants = [](double inv_temp) {
+        Exp64 e{};
+        e.c16 = (float)(16.0 * 1.4426950408889634074 * inv_temp);
+        e.step = 0.69314718055994530942 / 16.0 / inv_temp;
+        double a = 1.0;
+        for (int n = 1; n <= 5; ++n) e.a[n - 1] = a *= inv_temp / n;
+        return e;
+    };
+    P.e = constants(P.inv_temp);
+    if (P.draft_logits != nullptr) P.e_draft = constants(P.inv_draft_temp);
+    for (int j = 0; j < 16; ++j) {
+        const double t = exp2(j / 16.0);
+        uint64_t bits;
+        memcpy(&bits, &t, sizeof bits);
+        bits -= (uint64_t)j << 48;
+        memcpy(&P.table[j], &bits, sizeof bits);
+    }
     if (dtype == DM_F32) return launch_target<float>(P, draft_dtype, stream);
     return launch_target<__nv_bfloat16>(P, draft_dtype, stream);
 }

@@ -6,6 +6,13 @@ namespace dm {
 
 constexpr int kLosslessMaxV = 1 << 30;
 
+// Constants of exp(x / T) in fp64 (see weight() in dm_lossless.cu).
+struct Exp64 {
+    float c16;       // 16 log2(e) / T
+    double step;     // T ln2 / 16
+    double a[5];     // 1 / (n! T^n), n = 1..5
+};
+
 struct LosslessParams {
     const void *target, *draft_logits;   // [B][T + bonus][ld_target], [B][T][ld_draft] or null
     long long ld_target, ld_draft;
@@ -16,7 +23,9 @@ struct LosslessParams {
     const float *u_accept, *u_next;      // [B][T], [B]
     float* out_accept_prob;              // [B][T]
     int32_t *out_accept_len, *out_next;  // [B]
-    int share;                           // entries of a CTA's part of a row (set by the launch)
+    Exp64 e, e_draft;                    // (the rest is set by the launch)
+    double table[16];                    // 2^(j/16), j 2^16 taken from the high word
+    int share;                           // entries of a CTA's part of a row
 };
 
 // Storage types DM_F32 or DM_BF16; draft_dtype is not looked at without draft logits.

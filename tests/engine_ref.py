@@ -96,7 +96,7 @@ def lossless(target, draft, u_accept, u_next, draft_logits=None, draft_len=None,
                 r = p.clone()
                 if 0 <= x < V:
                     r[x] = 0.0
-        if not float(r.sum()) > 0:
+        if float(r.sum()) == 0:      # (a NaN in either row: nothing to draw from)
             r = p
         total = r.sum()
         if not float(total) > 0:
