@@ -343,6 +343,34 @@ int dropmatch_dropout(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int B, 
 int dropmatch_dropout_grad(dm_ctx* ctx, const void* grad, int dtype, int64_t ld, int B, int T, int K, int d, float p,
                            uint64_t seed, uint64_t seq_base, void* out_grad, int64_t ld_out, void* stream);
 
+/* ---- a head in 8-bit integers ----------------------------------------------------------------------
+ * Projections through a matrix W[V,d] held in 8-bit integers with a scale for each row (vocabulary entry, channel), of
+ * rows quantised to 8 bits with a scale for each row (token): half the bytes of a bf16 head, which bound most calls.
+ * The logits go where any logits go (dropmatch_verify_lossless, _logprobs, _distill).
+ *   dropmatch_quantize_i8  x[n_rows][ld] (DM_F32 or DM_BF16) -> out_q[n_rows][ld_q], out_scale[n_rows]:
+ *                          scale = max(max_j |x[j]| / 127, 2^-126),  q[j] = x[j] / scale rounded to the nearest whole number,
+ *                          ties to even; both quotients in fp32.  For W once and for tokens at every call.  A row that
+ *                          holds a NaN or an infinity: scale NaN, q = 0 (its products are NaN).
+ *   dropmatch_matmul_i8    out[r, v] = a_scale[r] * w_scale[v] * sum_j a[r, j] * w[v, j], out[n_rows][ld_out] in out_dtype
+ *                          (DM_F32 or DM_BF16).  The sum is exact (32-bit integers); it is converted to fp32, multiplied
+ *                          by w_scale, then by a_scale, and rounded once to out_dtype.
+ *   dropmatch_linear_i8    both: quantises x into out_q / out_scale (the caller's, contents of no further use) and
+ *                          multiplies; W and w_scale must be complete before the call is enqueued or be written by
+ *                          earlier work of the same stream.
+ * 8-bit matrices: any value in [-128, 127], 16-byte aligned, row strides (bytes) a multiple of 16; bytes d..ld of a row are
+ * neither read nor written.  x, scales and out are aligned to one entry, strides at least the row's length; columns V..ld_out
+ * are left as they are.  d <= 131071 (matrix products), V <= 2^30, else DM_EUNSUPPORTED.  Outputs must not overlap inputs.
+ * n_rows = 0 is allowed and does nothing.  Need no head and no workspace: calls of one context may overlap (linear's with
+ * their own out_q and out_scale).  If a kernel gives up on a wait (dm_device_error), outputs that it did not reach are NaN. */
+int dropmatch_quantize_i8(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int n_rows, int n, int8_t* out_q,
+                          int64_t ld_q, float* out_scale, void* stream);
+int dropmatch_matmul_i8(dm_ctx* ctx, const int8_t* a, int64_t ld_a, const float* a_scale, int n_rows, const int8_t* w,
+                        int64_t ld_w, const float* w_scale, int V, int d, void* out, int out_dtype, int64_t ld_out,
+                        void* stream);
+int dropmatch_linear_i8(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int n_rows, const int8_t* w, int64_t ld_w,
+                        const float* w_scale, int V, int d, int8_t* out_q, int64_t ld_q, float* out_scale, void* out,
+                        int out_dtype, int64_t ld_out, void* stream);
+
 /* Vocabulary-sharded heads (the deployment of Sec. 4.1 is tensor-parallel: every GPU holds a
  * slice of the LM head).  A context whose head is rows [offset, offset+V) of the full head reports
  * global token ids after dm_set_vocab_offset(ctx, offset) (call it after dm_set_head; default 0).

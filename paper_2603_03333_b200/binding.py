@@ -56,6 +56,9 @@ SIGNATURES = {
                                         _vp, _vp, _vp, _vp]),
     "dropmatch_dropout": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _vp, _i64, _vp]),
     "dropmatch_dropout_grad": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _vp, _i64, _vp]),
+    "dropmatch_quantize_i8": (_ci, [_vp, _vp, _ci, _i64, _ci, _ci, _vp, _i64, _vp, _vp]),
+    "dropmatch_matmul_i8": (_ci, [_vp, _vp, _i64, _vp, _ci, _vp, _i64, _vp, _ci, _ci, _vp, _ci, _i64, _vp]),
+    "dropmatch_linear_i8": (_ci, [_vp, _vp, _ci, _i64, _ci, _vp, _i64, _vp, _ci, _ci, _vp, _i64, _vp, _vp, _ci, _i64, _vp]),
     "dropmatch_verify_tree": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
                                     _vp, _vp, _vp, _vp, _vp, _vp]),
     "dropmatch_verify_tree_next": (_ci, [_vp, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _ci, _cf, _u64, _u64, _ci,
@@ -463,6 +466,67 @@ class Context:
                                             _ptr(out), ld_out, _stream(self.device)), "dropmatch_dropout_grad")
         return out
 
+    # -- dropmatch_quantize_i8 / dropmatch_matmul_i8 / dropmatch_linear_i8
+    def quantize_i8(self, x):
+        """x[..., n] (float32 or bfloat16, as in `logprobs`) -> (q[..., n] int8, scale[...] float32): a scale for each row.
+        q's rows start 16 bytes apart at least, as the products want them (q is a view of whole 16-byte rows)."""
+        rows, ld = self._rows(x, "x")
+        n = x.shape[-1]
+        ld_q = -(-n // 16) * 16
+        q = _empty(*x.shape[:-1], ld_q, dtype=torch.int8, device=self.device)
+        scale = _empty(*x.shape[:-1], dtype=torch.float32, device=self.device)
+        _check(lib().dropmatch_quantize_i8(self._h, _ptr(x), _DTYPES[x.dtype], ld, rows, n, _ptr(q), ld_q, _ptr(scale),
+                                           _stream(self.device)), "dropmatch_quantize_i8")
+        return q[..., :n], scale
+
+    def matmul_i8(self, q, q_scale, W, w_scale, dtype=torch.float32):
+        """q[..., d] and q_scale[...], W[V, d] and w_scale[V], as quantize_i8 gives them -> q W^T with the scales applied,
+        [..., V] in `dtype` (float32 or bfloat16)."""
+        rows, ld = self._rows_i8(q, "q")
+        V, ld_w = self._weights_i8(W, w_scale, q.shape[-1])
+        self._per_row(q_scale, torch.float32, q.shape[:-1], "q_scale")
+        out = self._product(q.shape[:-1], V, dtype)
+        _check(lib().dropmatch_matmul_i8(self._h, _ptr(q), ld, _ptr(q_scale), rows, _ptr(W), ld_w, _ptr(w_scale), V, q.shape[-1],
+                                         _ptr(out), _DTYPES[dtype], V, _stream(self.device)), "dropmatch_matmul_i8")
+        return out
+
+    def linear_i8(self, x, W, w_scale, dtype=None):
+        """x[..., d] (float32 or bfloat16) through W[V, d], w_scale[V] as quantize_i8 gives them: x is quantised row by row,
+        then multiplied.  -> [..., V] in `dtype` (x's by default)."""
+        rows, ld = self._rows(x, "x")
+        d = x.shape[-1]
+        V, ld_w = self._weights_i8(W, w_scale, d)
+        ld_q = -(-d // 16) * 16
+        scratch = _empty(rows * (ld_q + 4), dtype=torch.int8, device=self.device)      # the rows, then their scales
+        out = self._product(x.shape[:-1], V, x.dtype if dtype is None else dtype)
+        _check(lib().dropmatch_linear_i8(self._h, _ptr(x), _DTYPES[x.dtype], ld, rows, _ptr(W), ld_w, _ptr(w_scale), V, d,
+                                         _ptr(scratch), ld_q, scratch.data_ptr() + rows * ld_q, _ptr(out), _DTYPES[out.dtype], V,
+                                         _stream(self.device)), "dropmatch_linear_i8")
+        return out
+
+    def _rows_i8(self, t, what):
+        """(rows, row stride) of int8 rows one stride apart."""
+        if not t.is_cuda or t.dtype != torch.int8 or t.dim() < 2:
+            raise TypeError(f"{what} must be a CUDA tensor [..., d] of int8")
+        rows, ld = self._strided_rows(self._on_device(t, what), what)
+        if rows == 1:
+            ld = -(-ld // 16) * 16
+        if ld % 16 or t.data_ptr() % 16:
+            raise TypeError(f"{what} must have rows that start on 16-byte boundaries (see quantize_i8)")
+        return rows, ld
+
+    def _weights_i8(self, W, w_scale, d):
+        if W.dim() != 2 or W.shape[1] != d:
+            raise TypeError(f"W must have shape [V, {d}]")
+        V, ld_w = self._rows_i8(W, "W")
+        self._per_row(w_scale, torch.float32, (V,), "w_scale")
+        return V, ld_w
+
+    def _product(self, lead, V, dtype):
+        if dtype not in _DTYPES:
+            raise TypeError("the product's dtype must be float32 or bfloat16")
+        return _empty(*lead, V, dtype=dtype, device=self.device)
+
     # the calls on rows are short: these checks are written for few Python-level operations
     def _on_device(self, t, what):
         if t.get_device() != self.device.index:
@@ -473,7 +537,10 @@ class Context:
         """(rows, row stride) of a tensor [..., V] whose rows lie one stride apart."""
         if not t.is_cuda or t.dtype not in _DTYPES or t.dim() < 2:
             raise TypeError(f"{what} must be a CUDA tensor [..., V] of float32 or bfloat16")
-        self._on_device(t, what)
+        return self._strided_rows(self._on_device(t, what), what)
+
+    @staticmethod
+    def _strided_rows(t, what):
         V = t.shape[-1]
         if t.is_contiguous():
             return (t.numel() // V if V else 0), V

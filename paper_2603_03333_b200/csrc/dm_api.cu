@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "dm_dropout.h"
+#include "dm_i8.h"
 #include "dm_internal.h"
 #include "dm_lossless.h"
 #include "dm_rows.cuh"
@@ -271,11 +272,49 @@ bool grad_target_ok(const void* logits, int64_t ld, const void* grad, int64_t ld
     return a1 <= b0 || b1 <= a0;
 }
 
-// [first, last) of rows of `width` entries, one stride apart.
-bool ranges_overlap(const void* a, int64_t ld_a, int64_t rows_a, const void* b, int64_t ld_b, int64_t rows_b, int width, int elem) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), a1 = a0 + ((uintptr_t)(rows_a - 1) * (uintptr_t)ld_a + (uintptr_t)width) * (uintptr_t)elem;
-    const uintptr_t b0 = reinterpret_cast<uintptr_t>(b), b1 = b0 + ((uintptr_t)(rows_b - 1) * (uintptr_t)ld_b + (uintptr_t)width) * (uintptr_t)elem;
+// Do two sets of rows overlap, from the first byte of the first to the last byte of the last?  Strides and widths in bytes.
+bool ranges_overlap(const void* a, int64_t ld_a, int64_t rows_a, int64_t width_a, const void* b, int64_t ld_b, int64_t rows_b, int64_t width_b) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), a1 = a0 + (uintptr_t)((rows_a - 1) * ld_a + width_a);
+    const uintptr_t b0 = reinterpret_cast<uintptr_t>(b), b1 = b0 + (uintptr_t)((rows_b - 1) * ld_b + width_b);
     return a0 < b1 && b0 < a1;
+}
+
+// Rows of 8-bit integers as the tensor maps take them.
+bool i8_rows_ok(const int8_t* p, int64_t ld, int d) {
+    return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld & 15) == 0 && ld >= d;
+}
+
+int check_quantize(const void* x, int dtype, int64_t ld, int n_rows, int n, const int8_t* q, int64_t ld_q, const float* scale) {
+    if ((dtype != DM_F32 && dtype != DM_BF16) || n_rows < 0 || n < 1 || ld < n) return DM_EINVAL;
+    if (n > kRowsMaxV) return DM_EUNSUPPORTED;
+    if (n_rows == 0) return DM_OK;
+    if (!aligned_to_entry(x, dtype) || !aligned_to_entry(scale, DM_F32) || !i8_rows_ok(q, ld_q, n)) return DM_EINVAL;
+    if (ranges_overlap(x, ld * (dtype == DM_F32 ? 4 : 2), n_rows, n * (int64_t)(dtype == DM_F32 ? 4 : 2), q, ld_q, n_rows, n)) return DM_EINVAL;
+    return DM_OK;
+}
+
+int check_matmul_i8(const int8_t* w, int64_t ld_w, const float* w_scale, int n_rows, int V, int d, const void* out, int out_dtype,
+                    int64_t ld_out) {
+    if (n_rows < 0 || V < 1 || d < 1 || (out_dtype != DM_F32 && out_dtype != DM_BF16) || ld_out < V) return DM_EINVAL;
+    if (V > kRowsMaxV || d > kI8MaxDepth) return DM_EUNSUPPORTED;
+    if (n_rows == 0) return DM_OK;
+    if (!i8_rows_ok(w, ld_w, d) || !aligned_to_entry(w_scale, DM_F32) || !aligned_to_entry(out, out_dtype)) return DM_EINVAL;
+    const int64_t elem = out_dtype == DM_F32 ? 4 : 2;
+    if (ranges_overlap(w, ld_w, V, d, out, ld_out * elem, n_rows, V * elem)) return DM_EINVAL;
+    return DM_OK;
+}
+
+int run_matmul_i8(dm_ctx* c, const int8_t* a, int64_t ld_a, const float* a_scale, int n_rows, const int8_t* w, int64_t ld_w,
+                  const float* w_scale, int V, int d, void* out, int out_dtype, int64_t ld_out, bool behind_quantize, cudaStream_t stream) {
+    I8Args args{};
+    args.a = a; args.ld_a = ld_a; args.a_scale = a_scale;
+    args.w = w; args.ld_w = ld_w; args.w_scale = w_scale;
+    args.n_rows = n_rows; args.V = V; args.d = d;
+    args.out = out; args.out_dtype = out_dtype; args.ld_out = ld_out;
+    args.err = c->err;
+    args.wait_limit = c->wait_limit;
+    args.behind_quantize = behind_quantize;
+    return launch_matmul_i8(args, stream);
 }
 
 // The two directions of the dropout operator.
@@ -291,7 +330,8 @@ int run_dropout(dm_ctx* c, bool grad, const void* in, int64_t ld_in, void* out, 
     if (rows == 0) return DM_OK;
     if (!aligned_to_entry(in, dtype) || !aligned_to_entry(out, dtype)) return DM_EINVAL;
     const bool in_place = in == out && K == 1 && (ld_in == ld_out || rows == 1);
-    if (!in_place && ranges_overlap(in, ld_in, grad ? rows * K : rows, out, ld_out, grad ? rows : rows * K, d, dtype == DM_F32 ? 4 : 2))
+    const int64_t elem = dtype == DM_F32 ? 4 : 2;
+    if (!in_place && ranges_overlap(in, ld_in * elem, grad ? rows * K : rows, d * elem, out, ld_out * elem, grad ? rows : rows * K, d * elem))
         return DM_EINVAL;
     DeviceGuard g(c->device);
     if (!g.ok) return DM_ECUDA;
@@ -935,6 +975,50 @@ int dropmatch_dropout(dm_ctx* c, const void* x, int dtype, int64_t ld, int B, in
 int dropmatch_dropout_grad(dm_ctx* c, const void* grad, int dtype, int64_t ld, int B, int T, int K, int d, float p,
                            uint64_t seed, uint64_t seq_base, void* out_grad, int64_t ld_out, void* stream) {
     return run_dropout(c, true, grad, ld, out_grad, ld_out, dtype, B, T, K, d, p, seed, seq_base, stream);
+}
+
+int dropmatch_quantize_i8(dm_ctx* c, const void* x, int dtype, int64_t ld, int n_rows, int n, int8_t* out_q, int64_t ld_q,
+                          float* out_scale, void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    const int st = check_quantize(x, dtype, ld, n_rows, n, out_q, ld_q, out_scale);
+    if (st != DM_OK || n_rows == 0) return st;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    return launch_quantize_i8(QuantizeParams{x, ld, n_rows, n, out_q, ld_q, out_scale}, dtype, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_matmul_i8(dm_ctx* c, const int8_t* a, int64_t ld_a, const float* a_scale, int n_rows, const int8_t* w, int64_t ld_w,
+                        const float* w_scale, int V, int d, void* out, int out_dtype, int64_t ld_out, void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    const int st = check_matmul_i8(w, ld_w, w_scale, n_rows, V, d, out, out_dtype, ld_out);
+    if (st != DM_OK || n_rows == 0) return st;
+    const int64_t elem = out_dtype == DM_F32 ? 4 : 2;
+    if (!i8_rows_ok(a, ld_a, d) || !aligned_to_entry(a_scale, DM_F32) || ranges_overlap(a, ld_a, n_rows, d, out, ld_out * elem, n_rows, V * elem))
+        return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    return run_matmul_i8(c, a, ld_a, a_scale, n_rows, w, ld_w, w_scale, V, d, out, out_dtype, ld_out, false, static_cast<cudaStream_t>(stream));
+}
+
+int dropmatch_linear_i8(dm_ctx* c, const void* x, int dtype, int64_t ld, int n_rows, const int8_t* w, int64_t ld_w, const float* w_scale,
+                        int V, int d, int8_t* out_q, int64_t ld_q, float* out_scale, void* out, int out_dtype, int64_t ld_out,
+                        void* stream) {
+    if (c == nullptr) return DM_EINVAL;
+    int st = check_matmul_i8(w, ld_w, w_scale, n_rows, V, d, out, out_dtype, ld_out);
+    if (st == DM_OK) st = check_quantize(x, dtype, ld, n_rows, d, out_q, ld_q, out_scale);
+    if (st != DM_OK || n_rows == 0) return st;
+    const int64_t elem = out_dtype == DM_F32 ? 4 : 2;
+    if (ranges_overlap(out_q, ld_q, n_rows, d, out, ld_out * elem, n_rows, V * elem) || ranges_overlap(out_q, ld_q, n_rows, d, w, ld_w, V, d))
+        return DM_EINVAL;
+    DeviceGuard g(c->device);
+    if (!g.ok) return DM_ECUDA;
+    if (cudaPeekAtLastError() != cudaSuccess) { cudaGetLastError(); return DM_ECUDA; }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    st = launch_quantize_i8(QuantizeParams{x, ld, n_rows, d, out_q, ld_q, out_scale}, dtype, s);
+    if (st != DM_OK) return st;
+    return run_matmul_i8(c, out_q, ld_q, out_scale, n_rows, w, ld_w, w_scale, V, d, out, out_dtype, ld_out, true, s);
 }
 
 int dropmatch_verify_tree(dm_ctx* c, const void* H, const int32_t* node_token, const int32_t* node_parent,

@@ -76,6 +76,8 @@ size_t finalize_smem_bytes(int T, int K, int N);
 struct FusedState;
 // Tensor map over rows[rows][d] of bf16, boxes of 64 elements x box_rows rows, 128-byte swizzle.
 bool tensor_map_bf16(CUtensorMap* map, const void* base, int rows, int d, int box_rows);
+// Tensor map over rows[rows][ld] of bytes, `width` of them in use, boxes of 128 bytes x box_rows rows, 128-byte swizzle.
+bool tensor_map_u8(CUtensorMap* map, const void* base, int rows, int width, long long ld, int box_rows);
 bool fused_supported(const HeadDesc& head, int rows);
 int fused_create(FusedState** out, const HeadDesc& head, int max_rows, int max_hidden_rows, size_t* bytes);
 void fused_destroy(FusedState* fs);
