@@ -127,6 +127,7 @@ constexpr int kPollNs = 32, kIdlePollNs = 200;
 struct I8Params {
     int V, rows;
     int kb_count;
+    int tile_m;                          // rows of W that a CTA's tile takes up (the operand always has kTileM; what no load fills is not stored)
     int tile_n, n_tiles_n, n_tiles;      // tokens of a tile (a multiple of 32), tiles along the tokens, tiles in all
     int n_steps;
     uint32_t step_bytes, off_bar;
@@ -212,7 +213,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         if (lane != 0) return;
         const uint64_t w_policy = P.once ? ptx::l2_policy_evict_first() : ptx::l2_policy_evict_normal();
         const int a_rows = P.tile_n / kCtas;
-        const uint32_t tx = (uint32_t)(kCtas * kWBytes + P.tile_n * kBlockK);              // of all CTAs of the cluster
+        const uint32_t tx = (uint32_t)((kCtas * P.tile_m + P.tile_n) * kBlockK);              // of all CTAs of the cluster
         const uint32_t bar_map = kPair ? ptx::map_to_cta(full, 0) : full;                  // the leader's barriers
         const int my_tiles = unit < P.n_tiles ? (P.n_tiles - unit + units - 1) / units : 0;
         const int total = my_tiles * P.kb_count;
@@ -221,7 +222,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
         auto load_w = [&](int stage) {
             if (rank == 0) ptx::mbar_arrive_expect_tx(full + 8 * stage, tx);
             const uint32_t dst = smem_base + (uint32_t)stage * P.step_bytes;
-            const int y = ((w_tile / P.n_tiles_n) * kCtas + (int)rank) * kTileM;
+            const int y = ((w_tile / P.n_tiles_n) * kCtas + (int)rank) * P.tile_m;
             if (kPair) ptx::tma_load_2d_pair_hint(dst, &tmap_w, w_kb * kBlockK, y, bar_map + 8 * stage, w_policy);
             else ptx::tma_load_2d_hint(dst, &tmap_w, w_kb * kBlockK, y, full + 8 * stage, w_policy);
             if (++w_kb == P.kb_count) { w_kb = 0; w_tile += units; }
@@ -303,7 +304,7 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
     uint32_t parity = 0;
     for (int tile = unit; tile < P.n_tiles; tile += units) {
         const int tile_m = tile / P.n_tiles_n;
-        const int v = (tile_m * kCtas + (int)rank) * kTileM + quarter * 32 + lane;
+        const int m = quarter * 32 + lane, v = m < P.tile_m ? (tile_m * kCtas + (int)rank) * P.tile_m + m : P.V;
         const int n_first = (tile - tile_m * P.n_tiles_n) * P.tile_n, n_here = min(P.tile_n, P.rows - n_first);
         const float w_scale = v < P.V ? P.w_scale[v] : 0.0f;
         if (!dead && !ptx::mbar_wait_warp<kIdlePollNs>(acc_full + 8 * slot, parity, s_abort, P.wait_limit)) {
@@ -362,25 +363,35 @@ matmul_i8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_consta
 template <bool kPair, typename OUT>
 int launch(const I8Args& A, I8Params& P, int sms, cudaStream_t stream) {
     constexpr int kCtas = kPair ? 2 : 1;
-    const int tiles_m = (A.V + kCtas * kTileM - 1) / (kCtas * kTileM);
+    const int all = sms / kCtas;
+    int tiles_m = (A.V + kCtas * kTileM - 1) / (kCtas * kTileM);
+    P.tile_m = kTileM;
     P.n_tiles_n = (A.n_rows + kTileN - 1) / kTileN;
     P.tile_n = ((A.n_rows + P.n_tiles_n - 1) / P.n_tiles_n + 31) & ~31;      // (UMMA N: steps of 32 for a pair)
     P.n_tiles_n = (A.n_rows + P.tile_n - 1) / P.tile_n;
+    P.once = P.n_tiles_n == 1;
+    if (P.once && tiles_m > all) {
+        // W is read once and bounds the call: the same number of rows for everybody, in equal tiles (one token against
+        // 128256 x 4096, 6.8 tiles of 128 rows for each CTA: FIG us in 7 tiles of 124, FIG in up to 7 of 128)
+        const int rounds = (tiles_m + all - 1) / all;
+        const long long share = (long long)all * kCtas * rounds;
+        P.tile_m = (int)((((long long)A.V + share - 1) / share + 3) & ~3ll);
+        tiles_m = (int)(((long long)A.V + kCtas * P.tile_m - 1) / (kCtas * P.tile_m));
+    }
     if ((long long)tiles_m * P.n_tiles_n > 0x3FFFFFFFll) return DM_EUNSUPPORTED;
     P.n_tiles = tiles_m * P.n_tiles_n;
-    P.once = P.n_tiles_n == 1;
     P.step_bytes = (uint32_t)(kWBytes + P.tile_n / kCtas * kBlockK);
     P.n_steps = (int)((kSmemLimit - 1024 - kBarBytes) / P.step_bytes);
     if (P.n_steps > kMaxSteps) P.n_steps = kMaxSteps;
     P.off_bar = (uint32_t)P.n_steps * P.step_bytes;
     CUtensorMap tmap_w, tmap_a;
-    if (!tensor_map_u8(&tmap_w, A.w, A.V, A.d, A.ld_w, kTileM) || !tensor_map_u8(&tmap_a, A.a, A.n_rows, A.d, A.ld_a, P.tile_n / kCtas))
+    if (!tensor_map_u8(&tmap_w, A.w, A.V, A.d, A.ld_w, P.tile_m) || !tensor_map_u8(&tmap_a, A.a, A.n_rows, A.d, A.ld_a, P.tile_n / kCtas))
         return DM_ECUDA;
     if (cudaFuncSetAttribute(matmul_i8_kernel<kPair, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) {
         cudaGetLastError();
         return DM_ECUDA;
     }
-    const int units = P.n_tiles < sms / kCtas ? P.n_tiles : sms / kCtas;
+    const int units = P.n_tiles < all ? P.n_tiles : all;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(units * kCtas));
     cfg.blockDim = dim3(kThreads);
