@@ -342,8 +342,7 @@ int run_dropout(dm_ctx* c, bool grad, const void* in, int64_t ld_in, void* out, 
     dp.T = T; dp.K = K; dp.d = d;
     dp.shared_masks = c->mask_mode;
     dp.seq_base_lo = (uint32_t)seq_base;
-    dp.key0 = mk.key0; dp.key1 = mk.key1; dp.thr = mk.thr; dp.scale = mk.scale;
-    return launch_dropout(dp, dtype, grad, static_cast<cudaStream_t>(stream));
+    return launch_dropout(dp, mk, dtype, grad, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace

@@ -12,21 +12,21 @@
 // neighbouring entries, the flags handed over by shuffles (a quad that straddles two vectors would
 // otherwise be generated twice).
 //
-// What bounds it: HBM and the generator alike.  Ten rounds are 20 widening multiplies per quad; in a loop over paths
-// five of them stay the same (see PhiloxQuad), which leaves about 43 instructions per 8 bytes of bf16.
+// What bounds it: the generator, then HBM.  Ten rounds are 20 widening multiplies per quad, at a quarter of the issue rate; in a
+// loop over paths a quarter of them stays the same (see PhiloxQuad).  What is left keeps that pipe 72 % and the ALU 57 % busy.
+// Measured: 4096 rows of 4096 bf16 under 8 paths (302 MB) 92-94 us, where the multiplies alone take 58 and HBM 46;
+// the gradient of 976 x 16 rows of 8192 bf16 (272 MB) 98 us; 4084 rows of 5003 fp32 (163 MB, rows off 16-byte boundaries) 39-41 us.
+// Round keys as constants, two vectors a lane, divisions by multiplication: 103, 107 and 56 us before.
 #include "dm_dropout.h"
-
 namespace dm {
 
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr uint32_t kMulA = 0xD2511F53u, kMulB = 0xCD9E8D57u, kKeyA = 0x9E3779B9u, kKeyB = 0xBB67AE85u;
+constexpr uint32_t kMulA = 0xD2511F53u, kMulB = 0xCD9E8D57u;
 
 __device__ __forceinline__ void mul_wide(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& lo) {
-    const unsigned long long p = (unsigned long long)a * b;
-    hi = (uint32_t)(p >> 32);
-    lo = (uint32_t)p;
+    asm("{\n\t.reg .u64 p;\n\tmul.wide.u32 p, %2, %3;\n\tmov.b64 {%0, %1}, p;\n\t}" : "=r"(lo), "=r"(hi) : "r"(a), "r"(b));
 }
 
 // Philox4x32-10 at the counter (quad, path, t, s), cut at what does not change from path to path.
@@ -35,65 +35,45 @@ __device__ __forceinline__ void mul_wide(uint32_t a, uint32_t b, uint32_t& hi, u
 // are the quad's, and A x of round 2 is the path's.
 struct PhiloxPath {       // the same for all quads of a row
     uint32_t hi2, lo2;    // A x of round 2
-    __device__ __forceinline__ PhiloxPath(uint32_t path, uint32_t t, uint32_t k0) {
+    __device__ __forceinline__ PhiloxPath(uint32_t path, uint32_t t, const DropoutParams& P) {
         uint32_t hi, lo;
         mul_wide(kMulB, t, hi, lo);
-        mul_wide(kMulA, hi ^ path ^ k0, hi2, lo2);
+        mul_wide(kMulA, hi ^ path ^ P.key[0][0], hi2, lo2);
     }
 };
 struct PhiloxQuad {       // the same for all paths
     uint32_t z2, y2, z3, w3;
     __device__ __forceinline__ PhiloxQuad() {}
-    __device__ __forceinline__ PhiloxQuad(uint32_t quad, uint32_t t, uint32_t s, uint32_t k0, uint32_t k1) {
+    __device__ __forceinline__ PhiloxQuad(uint32_t quad, uint32_t t, uint32_t s, const DropoutParams& P) {
         uint32_t hi_t, lo_t, hi, w1, x2;
         mul_wide(kMulB, t, hi_t, lo_t);
         mul_wide(kMulA, quad, hi, w1);
-        mul_wide(kMulB, hi ^ s ^ k1, x2, y2);
-        x2 ^= lo_t ^ (k0 + kKeyA);
-        z2 = w1 ^ (k1 + kKeyB);
+        mul_wide(kMulB, hi ^ s ^ P.key[0][1], x2, y2);
+        x2 ^= lo_t ^ P.key[1][0];
+        z2 = w1 ^ P.key[1][1];
         mul_wide(kMulA, x2, z3, w3);
-        z3 ^= k1 + 2 * kKeyB;
-        y2 ^= k0 + 2 * kKeyA;
+        z3 ^= P.key[2][1];
+        y2 ^= P.key[2][0];
     }
-    __device__ __forceinline__ uint4 words(const PhiloxPath& p, uint32_t k0, uint32_t k1) const {
+    __device__ __forceinline__ uint4 words(const PhiloxPath& p, const DropoutParams& P) const {
         uint4 c;
         mul_wide(kMulB, p.hi2 ^ z2, c.x, c.y);      // round 3
         c.x ^= y2;
         c.z = z3 ^ p.lo2;
         c.w = w3;
 #pragma unroll
-        for (uint32_t r = 3; r < 10; ++r) {
+        for (int r = 3; r < 10; ++r) {
             uint32_t hi_a, lo_a, hi_b, lo_b;
             mul_wide(kMulA, c.x, hi_a, lo_a);
             mul_wide(kMulB, c.z, hi_b, lo_b);
-            c = make_uint4(hi_b ^ c.y ^ (k0 + r * kKeyA), lo_b, hi_a ^ c.w ^ (k1 + r * kKeyB), lo_a);
+            c = make_uint4(hi_b ^ c.y ^ P.key[r][0], lo_b, hi_a ^ c.w ^ P.key[r][1], lo_a);
         }
         return c;
     }
-    __device__ __forceinline__ uint32_t keep(const PhiloxPath& p, uint32_t k0, uint32_t k1, uint32_t thr) const {
-        const uint4 w = words(p, k0, k1);
+    __device__ __forceinline__ uint32_t keep(const PhiloxPath& p, const DropoutParams& P) const {
+        const uint4 w = words(p, P);
+        const uint32_t thr = P.thr;
         return (w.x >= thr ? 1u : 0u) | (w.y >= thr ? 2u : 0u) | (w.z >= thr ? 4u : 0u) | (w.w >= thr ? 8u : 0u);
-    }
-};
-
-// Where a warp stands: hidden row, first quad of its chunk, its paths.
-template <int Q>   // quads of a lane
-struct Place {
-    long long row;
-    int first;          // first entry of the chunk
-    int path0, path1;
-    uint32_t t, s;
-    __device__ __forceinline__ Place(const DropoutParams& P, long long task) {
-        const int chunk = (int)(task % P.n_chunks);
-        const long long rest = task / P.n_chunks;
-        const int group = (int)(rest % P.n_groups);
-        row = rest / P.n_groups;
-        first = chunk * (32 * 4 * Q);
-        path0 = group * P.group_paths;
-        path1 = min(P.K, path0 + P.group_paths);
-        const long long b = row / P.T;
-        t = P.shared_masks ? 0u : (uint32_t)(row - b * P.T);
-        s = P.seq_base_lo + (uint32_t)b;
     }
 };
 
@@ -116,140 +96,161 @@ __device__ __forceinline__ void keep_words(const uint32_t* v, const uint4& w, ui
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void add_to(float& sum, float x) { sum += x; }
+__device__ __forceinline__ void add_to(float& sum, __nv_bfloat16 x) {
+    asm("add.rn.f32.bf16 %0, %1, %0;" : "+f"(sum) : "h"(__bfloat16_as_ushort(x)));      // (exact conversion, one rounding)
+}
 __device__ __forceinline__ void round_to(float x, float* out) { *out = x; }
 __device__ __forceinline__ void round_to(float x, __nv_bfloat16* out) { *out = __float2bfloat16_rn(x); }
 
-// T: storage type.  VEC: every row starts on a 16-byte boundary (entries past the last whole vector of a row
-// are then read and written one by one by the same lane).
-template <typename T, bool VEC>
+// Quads and entries of a lane: NV vectors of 16 bytes.
+template <typename T, int NV> constexpr int kQuads = NV * 4 / (int)sizeof(T);
+template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
+
+// T: storage type.  VEC: every row starts on a 16-byte boundary; lane l's vector i is the chunk's vector 32 i + l (entries past
+// the last whole vector of a row are then read and written one by one by the same lane).  Otherwise lane l generates the
+// quads 32 r + l and reads and writes the entries 32 n + l.
+template <typename T, bool VEC, int NV>
 __global__ void __launch_bounds__(kThreads)
-dropout_kernel(const DropoutParams P) {
-    constexpr int Q = sizeof(T) == 2 ? 2 : 1, E = 4 * Q;     // quads and entries of a lane
-    const long long task = (long long)blockIdx.x * kWarps + warp_index();
+dropout_kernel(const __grid_constant__ DropoutParams P) {
+    constexpr int Q = kQuads<T, NV>, E = 4 * Q, V = kVec<T>;
+    const uint32_t task = blockIdx.x * kWarps + warp_index();
     if (task >= P.n_tasks) return;                           // (the same for the whole warp)
-    const Place<Q> at(P, task);
-    const int lane = threadIdx.x & 31;
-    const T* x = static_cast<const T*>(P.in) + at.row * P.ld_in;
-    T* out = static_cast<T*>(P.out) + (at.row * P.K + at.path0) * P.ld_out;
+    const uint32_t run = P.by_chunks.div(task), row = P.by_groups.div(run), b = P.by_T.div(row);
+    const int first = (int)(task - run * P.by_chunks.d) * (32 * E), path0 = (int)(run - row * P.by_groups.d) * P.group_paths;
+    const int path1 = min(P.K, path0 + P.group_paths), lane = threadIdx.x & 31;
+    const uint32_t t = P.shared_masks ? 0u : row - b * P.by_T.d, s = P.seq_base_lo + b;
+    const T* x = static_cast<const T*>(P.in) + row * P.ld_in;
+    T* out = static_cast<T*>(P.out) + ((long long)row * P.K + path0) * P.ld_out;
     PhiloxQuad quad[Q];
-    const uint32_t quad0 = (uint32_t)at.first / 4;
 #pragma unroll
     for (int r = 0; r < Q; ++r)
-        quad[r] = PhiloxQuad(quad0 + (VEC ? Q * lane + r : 32 * r + lane), at.t, at.s, P.key0, P.key1);
-    alignas(16) T v[E];      // x / (1 - p), rounded once; entry n of the lane's own vector, or entry 32 n + lane of the chunk
-    const int own = at.first + E * lane;
-    if (VEC && own + E <= P.d) {
-        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(x + own);
-    } else {
+        quad[r] = PhiloxQuad((uint32_t)first / 4 + (VEC ? (32 * (r / (V / 4)) + lane) * (V / 4) + r % (V / 4) : 32 * r + lane), t, s, P);
+    alignas(16) T v[E];      // x / (1 - p), rounded once
+    const auto at = [&](int n) { return VEC ? first + V * (32 * (n / V) + lane) + n % V : first + 32 * n + lane; };      // of the lane's entry n
 #pragma unroll
-        for (int n = 0; n < E; ++n) {
-            const int j = VEC ? own + n : at.first + 32 * n + lane;
-            round_to(0.0f, &v[n]);
-            if (j < P.d) v[n] = x[j];
+    for (int n = 0; n < E; n += V) {
+        if (VEC && at(n) + V <= P.d) {
+            *reinterpret_cast<uint4*>(v + n) = *reinterpret_cast<const uint4*>(x + at(n));
+        } else {
+#pragma unroll
+            for (int k = n; k < n + V; ++k) {
+                round_to(0.0f, &v[k]);
+                if (at(k) < P.d) v[k] = x[at(k)];
+            }
         }
     }
 #pragma unroll
     for (int n = 0; n < E; ++n) round_to(to_float(v[n]) * P.scale, &v[n]);
     T zero;
     round_to(0.0f, &zero);
-#pragma unroll 2
-    for (int i = at.path0; i < at.path1; ++i, out += P.ld_out) {
-        const PhiloxPath path((uint32_t)i, at.t, P.key0);
+#pragma unroll 1
+    for (int i = path0; i < path1; ++i, out += P.ld_out) {
+        const PhiloxPath path((uint32_t)i, t, P);
         if (VEC) {
-            uint32_t o[4];
+            alignas(16) uint32_t o[E * sizeof(T) / 4];
 #pragma unroll
             for (int r = 0; r < Q; ++r)
-                keep_words(reinterpret_cast<const uint32_t*>(v) + 4 / Q * r, quad[r].words(path, P.key0, P.key1), P.thr, o + 4 / Q * r, zero);
-            if (own + E <= P.d) {
-                *reinterpret_cast<uint4*>(out + own) = make_uint4(o[0], o[1], o[2], o[3]);
-            } else {
+                keep_words(reinterpret_cast<const uint32_t*>(v) + sizeof(T) * r, quad[r].words(path, P), P.thr, o + sizeof(T) * r, zero);
 #pragma unroll
-                for (int n = 0; n < E; ++n)
-                    if (own + n < P.d) out[own + n] = reinterpret_cast<const T*>(o)[n];
+            for (int n = 0; n < E; n += V) {
+                if (at(n) + V <= P.d) {
+                    *reinterpret_cast<uint4*>(out + at(n)) = reinterpret_cast<const uint4*>(o)[n / V];
+                } else {
+#pragma unroll
+                    for (int k = n; k < n + V; ++k)
+                        if (at(k) < P.d) out[at(k)] = reinterpret_cast<const T*>(o)[k];
+                }
             }
         } else {
 #pragma unroll
             for (int r = 0; r < Q; ++r) {
-                const uint32_t flags = quad[r].keep(path, P.key0, P.key1, P.thr);
+                const uint32_t flags = quad[r].keep(path, P);
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {      // entries 128 r + 32 n + lane: quad 8 n + lane / 4 of the 32
                     const uint32_t f = __shfl_sync(0xFFFFFFFFu, flags, 8 * n + (lane >> 2));
-                    const int j = at.first + 128 * r + 32 * n + lane;
-                    if (j < P.d) out[j] = (f >> (lane & 3)) & 1u ? v[4 * r + n] : zero;
+                    if (at(4 * r + n) < P.d) out[at(4 * r + n)] = (f >> (lane & 3)) & 1u ? v[4 * r + n] : zero;
                 }
             }
         }
     }
 }
 
-// Sums over the paths: fp32, paths in order within a run of them; long sums are cut into P.n_groups runs that
+// Sums over the paths: fp32, paths in order within a run of them; long sums are cut into n_groups runs that
 // neighbouring warps of a block take and the first of them joins in order.  The cut follows from K alone, so that
 // a row's result does not depend on the others.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads)
-dropout_grad_kernel(const DropoutParams P) {
-    constexpr int Q = sizeof(T) == 2 ? 2 : 1, E = 4 * Q;
+template <typename T, bool VEC, int NV>
+__global__ void __launch_bounds__(kThreads, 3)
+dropout_grad_kernel(const __grid_constant__ DropoutParams P) {
+    constexpr int Q = kQuads<T, NV>, E = 4 * Q, V = kVec<T>;
     __shared__ float s_part[kWarps][E * 32];
-    const int warp = warp_index(), lane = threadIdx.x & 31;
-    const int group = warp & (P.n_groups - 1);               // (a power of two, at most kWarps)
-    // tasks count chunks of all runs; a block takes kWarps / n_groups chunks
-    const long long chunk_id = (long long)blockIdx.x * (kWarps / P.n_groups) + warp / P.n_groups;
-    const bool live = chunk_id < P.n_tasks;
-    const long long row = live ? chunk_id / P.n_chunks : 0;
-    const int first = live ? (int)(chunk_id - row * P.n_chunks) * (32 * E) : 0;
+    const int warp = warp_index(), lane = threadIdx.x & 31, n_groups = (int)P.by_groups.d;
+    const int group = warp & (n_groups - 1);                 // (a power of two, at most kWarps)
+    const uint32_t task = blockIdx.x * (uint32_t)(kWarps / n_groups) + P.by_groups.div(warp);
+    const bool live = task < P.n_tasks;
+    const uint32_t row = live ? P.by_chunks.div(task) : 0u, b = P.by_T.div(row);
+    const int first = live ? (int)(task - row * P.by_chunks.d) * (32 * E) : 0;
     const int path0 = min(P.K, group * P.group_paths), path1 = live ? min(P.K, path0 + P.group_paths) : path0;
-    const long long b = row / P.T;
-    const uint32_t t = P.shared_masks ? 0u : (uint32_t)(row - b * P.T), s = P.seq_base_lo + (uint32_t)b;
+    const uint32_t t = P.shared_masks ? 0u : row - b * P.by_T.d, s = P.seq_base_lo + b;
     PhiloxQuad quad[Q];
 #pragma unroll
     for (int r = 0; r < Q; ++r)
-        quad[r] = PhiloxQuad((uint32_t)first / 4 + (VEC ? Q * lane + r : 32 * r + lane), t, s, P.key0, P.key1);
-    const T* g = static_cast<const T*>(P.in) + (row * P.K + path0) * P.ld_in;
-    const int own = first + E * lane;
-    const bool whole = VEC && own + E <= P.d;
+        quad[r] = PhiloxQuad((uint32_t)first / 4 + (VEC ? (32 * (r / (V / 4)) + lane) * (V / 4) + r % (V / 4) : 32 * r + lane), t, s, P);
+    const T* g = static_cast<const T*>(P.in) + ((long long)row * P.K + path0) * P.ld_in;
+    const auto at = [&](int n) { return VEC ? first + V * (32 * (n / V) + lane) + n % V : first + 32 * n + lane; };
     float sum[E];
 #pragma unroll
     for (int n = 0; n < E; ++n) sum[n] = 0.0f;
-    constexpr int kAhead = 2;
-#pragma unroll 1
-    for (int i0 = path0; i0 < path1; i0 += kAhead) {
-        alignas(16) T v[kAhead][E];
+    alignas(16) T v[2][E];       // the next path's entries are on their way while one is added
+    const auto load = [&](T (&to)[E]) {
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            if (i0 + a >= path1) break;
-            const T* gi = g + (long long)(i0 - path0 + a) * P.ld_in;
-            if (whole) {
-                *reinterpret_cast<uint4*>(v[a]) = *reinterpret_cast<const uint4*>(gi + own);
+        for (int n = 0; n < E; n += V) {
+            if (VEC && at(n) + V <= P.d) {
+                *reinterpret_cast<uint4*>(to + n) = *reinterpret_cast<const uint4*>(g + at(n));
             } else {
 #pragma unroll
-                for (int n = 0; n < E; ++n) {
-                    const int j = VEC ? own + n : first + 32 * n + lane;
-                    round_to(0.0f, &v[a][n]);
-                    if (j < P.d) v[a][n] = gi[j];
+                for (int k = n; k < n + V; ++k) {
+                    round_to(0.0f, &to[k]);
+                    if (at(k) < P.d) to[k] = g[at(k)];
                 }
             }
         }
+        g += P.ld_in;
+    };
+    const auto add = [&](int i, const T (&from)[E]) {
+        const PhiloxPath path((uint32_t)i, t, P);
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            if (i0 + a >= path1) break;
-            const PhiloxPath path((uint32_t)(i0 + a), t, P.key0);
-#pragma unroll
-            for (int r = 0; r < Q; ++r) {
-                const uint32_t flags = quad[r].keep(path, P.key0, P.key1, P.thr);
+        for (int r = 0; r < Q; ++r) {
+            if (VEC) {
+                const uint4 w = quad[r].words(path, P);
+                if (w.x >= P.thr) add_to(sum[4 * r + 0], from[4 * r + 0]);      // (a dropped NaN stays out)
+                if (w.y >= P.thr) add_to(sum[4 * r + 1], from[4 * r + 1]);
+                if (w.z >= P.thr) add_to(sum[4 * r + 2], from[4 * r + 2]);
+                if (w.w >= P.thr) add_to(sum[4 * r + 3], from[4 * r + 3]);
+            } else {
+                const uint32_t flags = quad[r].keep(path, P);
 #pragma unroll
                 for (int n = 0; n < 4; ++n) {
-                    const uint32_t f = VEC ? flags >> n : __shfl_sync(0xFFFFFFFFu, flags, 8 * n + (lane >> 2)) >> (lane & 3);
-                    if (f & 1u) sum[4 * r + n] += to_float(v[a][4 * r + n]);    // (a dropped NaN stays out)
+                    const uint32_t f = __shfl_sync(0xFFFFFFFFu, flags, 8 * n + (lane >> 2));
+                    if ((f >> (lane & 3)) & 1u) add_to(sum[4 * r + n], from[4 * r + n]);
                 }
             }
         }
+    };
+    if (path0 < path1) load(v[0]);
+#pragma unroll 1
+    for (int i = path0; i < path1; i += 2) {
+        if (i + 1 < path1) load(v[1]);
+        add(i, v[0]);
+        if (i + 2 < path1) load(v[0]);
+        if (i + 1 < path1) add(i + 1, v[1]);
     }
-    if (P.n_groups > 1) {
+    if (n_groups > 1) {
 #pragma unroll
         for (int n = 0; n < E; ++n) s_part[warp][32 * n + lane] = sum[n];
         __syncthreads();
         if (group != 0) return;
-        for (int w = 1; w < P.n_groups; ++w)
+        for (int w = 1; w < n_groups; ++w)
 #pragma unroll
             for (int n = 0; n < E; ++n) sum[n] += s_part[warp + w][32 * n + lane];
     }
@@ -258,13 +259,14 @@ dropout_grad_kernel(const DropoutParams P) {
 #pragma unroll
     for (int n = 0; n < E; ++n) round_to(sum[n] * P.scale, &o[n]);
     T* out = static_cast<T*>(P.out) + row * P.ld_out;
-    if (whole) {
-        *reinterpret_cast<uint4*>(out + own) = *reinterpret_cast<const uint4*>(o);
-    } else {
 #pragma unroll
-        for (int n = 0; n < E; ++n) {
-            const int j = VEC ? own + n : first + 32 * n + lane;
-            if (j < P.d) out[j] = o[n];
+    for (int n = 0; n < E; n += V) {
+        if (VEC && at(n) + V <= P.d) {
+            *reinterpret_cast<uint4*>(out + at(n)) = *reinterpret_cast<const uint4*>(o + n);
+        } else {
+#pragma unroll
+            for (int k = n; k < n + V; ++k)
+                if (at(k) < P.d) out[at(k)] = o[k];
         }
     }
 }
@@ -273,44 +275,62 @@ bool aligned_rows(const void* p, long long ld, int elem) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * elem)) & 15u) == 0;
 }
 
-template <typename T>
+template <typename T, int NV>
 int launch(DropoutParams& P, bool grad, cudaStream_t stream) {
-    constexpr int kEntries = 32 * 4 * (sizeof(T) == 2 ? 2 : 1);      // of a warp's chunk
+    constexpr int kEntries = 32 * 4 * kQuads<T, NV>;      // of a warp's chunk
     const bool vec = aligned_rows(P.in, P.ld_in, sizeof(T)) && aligned_rows(P.out, P.ld_out, sizeof(T));
-    P.n_chunks = (P.d + kEntries - 1) / kEntries;
-    long long blocks;
+    const long long n_chunks = (P.d + kEntries - 1) / kEntries, chunks = P.rows * n_chunks;
+    int n_groups;
+    long long tasks, blocks;
     if (grad) {
         // runs of at least eight paths: what a warp adds up in one go
-        P.n_groups = P.K >= 64 ? 8 : P.K >= 32 ? 4 : P.K >= 16 ? 2 : 1;
-        P.group_paths = (P.K + P.n_groups - 1) / P.n_groups;
-        P.n_tasks = P.rows * P.n_chunks;
-        const int per_block = kWarps / P.n_groups;
-        blocks = (P.n_tasks + per_block - 1) / per_block;
+        n_groups = P.K >= 64 ? 8 : P.K >= 32 ? 4 : P.K >= 16 ? 2 : 1;
+        P.group_paths = (P.K + n_groups - 1) / n_groups;
+        tasks = chunks;
+        const int per_block = kWarps / n_groups;
+        blocks = (tasks + per_block - 1) / per_block;
     } else {
         // a warp takes all paths of its chunk unless that leaves the GPU short of warps (some 16 on each of its SMs)
-        const long long chunks = P.rows * P.n_chunks;
         P.group_paths = P.K;
         while (P.group_paths > 1 && chunks * ((P.K + P.group_paths - 1) / P.group_paths) < 2368) P.group_paths = (P.group_paths + 1) / 2;
-        P.n_groups = (P.K + P.group_paths - 1) / P.group_paths;
-        P.n_tasks = chunks * P.n_groups;
-        blocks = (P.n_tasks + kWarps - 1) / kWarps;
+        n_groups = (P.K + P.group_paths - 1) / P.group_paths;
+        tasks = chunks * n_groups;
+        blocks = (tasks + kWarps - 1) / kWarps;
     }
-    if (blocks > 0x7FFFFFFFll) return DM_EUNSUPPORTED;
+    if (tasks > 0x7FFFFFF0ll) return DM_EUNSUPPORTED;
+    P.n_tasks = (uint32_t)tasks;
+    P.by_chunks = Divisor((uint32_t)n_chunks);
+    P.by_groups = Divisor((uint32_t)n_groups);
+    P.by_T = Divisor((uint32_t)P.T);
     const unsigned grid = (unsigned)blocks;
     if (grad) {
-        if (vec) dropout_grad_kernel<T, true><<<grid, kThreads, 0, stream>>>(P);
-        else dropout_grad_kernel<T, false><<<grid, kThreads, 0, stream>>>(P);
+        if (vec) dropout_grad_kernel<T, true, NV><<<grid, kThreads, 0, stream>>>(P);
+        else dropout_grad_kernel<T, false, NV><<<grid, kThreads, 0, stream>>>(P);
     } else {
-        if (vec) dropout_kernel<T, true><<<grid, kThreads, 0, stream>>>(P);
-        else dropout_kernel<T, false><<<grid, kThreads, 0, stream>>>(P);
+        if (vec) dropout_kernel<T, true, NV><<<grid, kThreads, 0, stream>>>(P);
+        else dropout_kernel<T, false, NV><<<grid, kThreads, 0, stream>>>(P);
     }
     return cudaGetLastError() == cudaSuccess ? DM_OK : DM_ECUDA;
 }
 
+template <typename T>
+int launch_wide(DropoutParams& P, bool grad, cudaStream_t stream) {
+    // two vectors a lane share the paths' part of the generator and the keys; short rows would leave lanes idle, small calls warps
+    const long long chunks = P.rows * ((P.d + 64 * kVec<T> - 1) / (64 * kVec<T>));
+    const bool wide = P.d >= 64 * kVec<T> && chunks >= 2368;
+    return wide ? launch<T, 2>(P, grad, stream) : launch<T, 1>(P, grad, stream);
+}
+
 }  // namespace
 
-int launch_dropout(DropoutParams P, int dtype, bool grad, cudaStream_t stream) {
-    return dtype == DM_F32 ? launch<float>(P, grad, stream) : launch<__nv_bfloat16>(P, grad, stream);
+int launch_dropout(DropoutParams P, const MaskKey& mk, int dtype, bool grad, cudaStream_t stream) {
+    P.thr = mk.thr;
+    P.scale = mk.scale;
+    for (uint32_t r = 0; r < 10; ++r) {
+        P.key[r][0] = mk.key0 + r * 0x9E3779B9u;
+        P.key[r][1] = mk.key1 + r * 0xBB67AE85u;
+    }
+    return dtype == DM_F32 ? launch_wide<float>(P, grad, stream) : launch_wide<__nv_bfloat16>(P, grad, stream);
 }
 
 }  // namespace dm

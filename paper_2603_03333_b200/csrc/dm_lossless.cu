@@ -16,6 +16,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "dm_lossless.h"
 #include "dm_ptx.cuh"
 
@@ -630,6 +632,23 @@ next_kernel(const LosslessParams P, int cluster) {
     if (threadIdx.x == 0) P.out_next[b] = S.found != kNone ? S.found : S.last;
 }
 
+// Largest dynamic shared memory and cluster, once for each kernel and device.
+template <auto KERNEL>
+bool allow(int smem) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+    if ((smem > 0 && cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) ||
+        cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
 template <typename TP, typename TQ, bool HAS_Q>
 int launch(LosslessParams& P, cudaStream_t stream) {
     // CTAs that share a row: at most `most` on the GPU in all, with at least 2048 entries each; parts are whole 16-byte vectors
@@ -640,11 +659,6 @@ int launch(LosslessParams& P, cudaStream_t stream) {
         return cluster;
     };
     const auto run = [&](auto* kernel, int positions, int cluster, int threads, int smem, bool behind) {
-        if ((smem > 47 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) ||
-            (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) {
-            cudaGetLastError();
-            return DM_ECUDA;
-        }
         cudaLaunchAttribute attrs[2]{};
         attrs[0].id = cudaLaunchAttributeClusterDimension;
         attrs[0].val.clusterDim.x = (unsigned)cluster; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
@@ -666,12 +680,14 @@ int launch(LosslessParams& P, cudaStream_t stream) {
     if (P.T > 0) {
         // (96 x 7 rows of 151936: 2 or 4 CTAs each the same, 8: 8 % slower, 16: 40 %; 5 rows: 16 the fastest)
         const int cluster = cut((long long)P.B * P.T, 2800);
+        if (!allow<ratio_kernel<TP, TQ, HAS_Q>>(kRatioSmem)) return DM_ECUDA;
         const int st = run(ratio_kernel<TP, TQ, HAS_Q>, P.B * P.T, cluster, kRatioThreads, kRatioSmem, false);
         if (st != DM_OK) return st;
     }
     // (96 sequences of 151936: 8 CTAs each 168 us in all, 4: 175, 16: 190; one sequence: 16 the fastest)
     const int cluster = cut(P.B, 888);
     // (behind the ratios: the kernel waits for them before it reads anything)
+    if (!allow<next_kernel<TP, TQ, HAS_Q, 512>>(0) || !allow<next_kernel<TP, TQ, HAS_Q, 256>>(0)) return DM_ECUDA;
     return P.B * cluster <= 148 ? run(next_kernel<TP, TQ, HAS_Q, 512>, P.B, cluster, 512, 0, P.T > 0)
                                 : run(next_kernel<TP, TQ, HAS_Q, 256>, P.B, cluster, 256, 0, P.T > 0);
 }
