@@ -425,17 +425,24 @@ next_kernel(const LosslessParams P, int cluster) {
     // and part[set ^ 1].
     auto sums = [&](bool with_q, int skip) {
         double a[4] = {};
-        const auto add = [&](float x, float y) {
-            const double p = weight(x, at_p, P.e, S.table);
-            a[0] += p;
+        const auto add = [&](auto& x, auto& y) {      // (all the exponentials side by side, without a branch between them)
+            constexpr int N = sizeof(x) / sizeof(x[0]);
+            double p[N], q[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i] = weight(x[i], at_p, P.e, S.table);
             if (HAS_Q && with_q) {
-                const double q = weight(y, at_q, P.e_draft, S.table);
-                a[1] += q;
-                if (fma(-rho, q, p) > 0.0) {
-                    a[2] += p;
-                    a[3] += q;
+#pragma unroll
+                for (int i = 0; i < N; ++i) q[i] = weight(y[i], at_q, P.e_draft, S.table);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const bool more = fma(-rho, q[i], p[i]) > 0.0;
+                    a[1] += q[i];
+                    a[2] += more ? p[i] : 0.0;
+                    a[3] += more ? q[i] : 0.0;
                 }
             }
+#pragma unroll
+            for (int i = 0; i < N; ++i) a[0] += p[i];
         };
         constexpr int kAhead = 4;
         const TP* at_x = row_p + w_lo + lane;
@@ -460,14 +467,15 @@ next_kernel(const LosslessParams P, int cluster) {
         while (more) {       // two batches of loads on their way
             more = left > 32 * (kAhead - 1);
             if (more) load(x2, y2);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) add(x[i], y[i]);
+            add(x, y);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) { x[i] = x2[i]; y[i] = y2[i]; }
         }
 #pragma unroll 1
-        for (; left > 0; left -= 32, off -= 32, at_x += 32, at_y += 32)
-            add(off == 0 ? neg_inf() : entry(at_x, 0), HAS_Q && with_q ? entry(at_y, 0) : 0.0f);
+        for (; left > 0; left -= 32, off -= 32, at_x += 32, at_y += 32) {
+            const float x1[1] = {off == 0 ? neg_inf() : entry(at_x, 0)}, y1[1] = {HAS_Q && with_q ? entry(at_y, 0) : 0.0f};
+            add(x1, y1);
+        }
         __syncwarp();
         add_lanes(a);
         if (lane < 4) S.warp_part[warp][lane] = lane == 0 ? a[0] : lane == 1 ? a[1] : lane == 2 ? a[2] : a[3];
