@@ -657,28 +657,46 @@ bool allow(int smem) {
     return true;
 }
 
+cudaLaunchConfig_t launch_config(cudaLaunchAttribute (&attrs)[2], int clusters, int cluster, int threads, int smem, bool behind, cudaStream_t stream) {
+    attrs[0].id = cudaLaunchAttributeClusterDimension;
+    attrs[0].val.clusterDim.x = (unsigned)cluster; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
+    attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)clusters * (unsigned)cluster);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cfg.attrs = attrs;
+    cfg.numAttrs = behind ? 2 : 1;
+    return cfg;
+}
+
+// Clusters of this size that the device runs at a time (looked up once for each kernel, device and size).
+template <auto KERNEL>
+int clusters_at_once(int cluster, int threads) {
+    constexpr int kDevices = 16;
+    static std::atomic<int> known[kDevices][kMaxCluster + 1];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < kDevices && (n = known[dev][cluster].load(std::memory_order_relaxed)) > 0) return n;
+    cudaLaunchAttribute attrs[2]{};
+    const cudaLaunchConfig_t cfg = launch_config(attrs, 1, cluster, threads, 0, false, nullptr);
+    if (cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    if (dev < kDevices) known[dev][cluster].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 template <typename TP, typename TQ, bool HAS_Q>
 int launch(LosslessParams& P, cudaStream_t stream) {
-    // CTAs that share a row: at most `most` on the GPU in all, with at least 2048 entries each; parts are whole 16-byte vectors
-    const auto cut = [&](long long rows, long long most) {
-        int cluster = 1;
-        while (cluster < kMaxCluster && P.V / (2 * cluster) >= 2048 && 2 * rows * cluster <= most) cluster *= 2;
-        P.share = ((P.V + cluster - 1) / cluster + 7) & ~7;
-        return cluster;
-    };
-    const auto run = [&](auto* kernel, int positions, int cluster, int threads, int smem, bool behind) {
+    const auto enough = [&](int cluster) { return P.V / cluster >= 2048; };       // entries for a CTA
+    const auto run = [&](auto* kernel, int clusters, int cluster, int threads, int smem, bool behind) {
+        P.share = ((P.V + cluster - 1) / cluster + 7) & ~7;      // (whole 16-byte vectors)
         cudaLaunchAttribute attrs[2]{};
-        attrs[0].id = cudaLaunchAttributeClusterDimension;
-        attrs[0].val.clusterDim.x = (unsigned)cluster; attrs[0].val.clusterDim.y = 1; attrs[0].val.clusterDim.z = 1;
-        attrs[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attrs[1].val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)positions * (unsigned)cluster);
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.dynamicSmemBytes = (size_t)smem;
-        cfg.stream = stream;
-        cfg.attrs = attrs;
-        cfg.numAttrs = behind ? 2 : 1;
+        const cudaLaunchConfig_t cfg = launch_config(attrs, clusters, cluster, threads, smem, behind, stream);
         if (cudaLaunchKernelEx(&cfg, kernel, P, cluster) != cudaSuccess || cudaGetLastError() != cudaSuccess) {
             cudaGetLastError();
             return DM_ECUDA;
@@ -686,18 +704,31 @@ int launch(LosslessParams& P, cudaStream_t stream) {
         return DM_OK;
     };
     if (P.T > 0) {
-        // (96 x 7 rows of 151936: 2 or 4 CTAs each the same, 8: 8 % slower, 16: 40 %; 5 rows: 16 the fastest)
-        const int cluster = cut((long long)P.B * P.T, 2800);
+        // (96 x 7 rows of 151936 over 2 CTAs each: 73 us, 4: 79, 8: 96; the 5 of one sequence: 16 are the fastest)
+        int cluster = 1;
+        while (cluster < kMaxCluster && enough(2 * cluster) && 2ll * P.B * P.T * cluster <= 1400) cluster *= 2;
         if (!allow<ratio_kernel<TP, TQ, HAS_Q>>(kRatioSmem)) return DM_ECUDA;
         const int st = run(ratio_kernel<TP, TQ, HAS_Q>, P.B * P.T, cluster, kRatioThreads, kRatioSmem, false);
         if (st != DM_OK) return st;
     }
-    // (96 sequences of 151936: 8 CTAs each 168 us in all, 4: 175, 16: 190; one sequence: 16 the fastest)
-    const int cluster = cut(P.B, 888);
-    // (behind the ratios: the kernel waits for them before it reads anything)
+    // The largest clusters with which all sequences are drawn side by side: of 512 threads where that gives each sequence
+    // at least four CTAs, else of 256 (three on an SM); beyond that, in turns of six.  (Of 128256 entries, in all: 32
+    // sequences 53 us with 4 x 512, 61 with 3 x 512, 55 with 8 x 256; 64: 84 with 6 x 256, 88 with 2 x 512, 96 with
+    // 8 x 256; 128: 141 with 6 x 256, 147 with 3 x 256.)
     if (!allow<next_kernel<TP, TQ, HAS_Q, 512>>(0) || !allow<next_kernel<TP, TQ, HAS_Q, 256>>(0)) return DM_ECUDA;
-    return P.B * cluster <= 148 ? run(next_kernel<TP, TQ, HAS_Q, 512>, P.B, cluster, 512, 0, P.T > 0)
-                                : run(next_kernel<TP, TQ, HAS_Q, 256>, P.B, cluster, 256, 0, P.T > 0);
+    const auto largest = [&](auto at_once, int threads, int least) {
+        for (int cluster = kMaxCluster; cluster >= least; --cluster)
+            if (enough(cluster) && at_once(cluster, threads) >= P.B) return cluster;
+        return 0;
+    };
+    // (behind the ratios the kernel waits for them before it reads anything)
+    int most = 1;
+    while (most < kMaxCluster && enough(most + 1)) ++most;
+    int cluster = largest(clusters_at_once<next_kernel<TP, TQ, HAS_Q, 512>>, 512, (most < 4 ? most : 4));
+    if (cluster > 0) return run(next_kernel<TP, TQ, HAS_Q, 512>, P.B, cluster, 512, 0, P.T > 0);
+    cluster = largest(clusters_at_once<next_kernel<TP, TQ, HAS_Q, 256>>, 256, (most < 4 ? most : 4));
+    if (cluster == 0) cluster = (most < 6 ? most : 6);
+    return run(next_kernel<TP, TQ, HAS_Q, 256>, P.B, cluster, 256, 0, P.T > 0);
 }
 
 template <typename TP>
