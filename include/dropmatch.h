@@ -303,7 +303,8 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
  * the drafted token x is accepted iff u_accept[b,t] * q(x) < p(x); n is the length of the accepted prefix.  The
  * next token is drawn from r = max(p - q, 0) of row n (p, if r is 0 everywhere) where a token was rejected, and
  * from p of row n where all were accepted: the smallest v with  r(0) + ... + r(v) > u_next[b] * sum r.
- * Decisions and draws are those of 64-bit arithmetic on the given logits; out_accept_prob is fp32.
+ * Decisions and draws are those of 64-bit arithmetic on the given logits (exponentials to 2^-42; a difference p - q of
+ * less than 2^-40 p counts as 0); out_accept_prob is fp32.
  *   target[B][T + bonus_row][ld_target]   dtype DM_F32 or DM_BF16; row stride ld_target >= V entries, aligned to one
  *                                entry (16-byte aligned rows are the fastest).  bonus_row = 1: one more row per
  *                                sequence, behind the last drafted token
@@ -312,7 +313,7 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
  *   draft[B,T]                   ids outside [0,V) have p = 0
  *   draft_len[B]                 drafted tokens of each sequence, in [0,T] (clamped), or NULL: T.  Rows and tokens behind
  *                                them are not read, but for row draft_len[b] of the target, which the next token is drawn from
- *   u_accept[B,T], u_next[B]     float32 in [0,1)
+ *   u_accept[B,T], u_next[B]     float32 in [0,1).  Outputs must not overlap inputs
  *   out_accept_len[B], out_next_token[B]   -1 if every one of T tokens was accepted and there is no bonus row
  *   out_accept_prob[B,T]         float32, min(1, p(x) / q(x)); 0 behind draft_len.  Read by the call's second kernel
  * Masked entries: -inf has probability 0; a row of nothing but -inf has probability 0 everywhere.  A row that holds a

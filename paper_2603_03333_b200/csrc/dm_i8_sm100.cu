@@ -8,6 +8,8 @@
 // epilogue thread owns a vocabulary entry and a warp's store of one token's outputs is contiguous as it comes out of
 // TMEM.  CTAs (pairs) walk over tiles, the token tiles of one piece of W next to each other, with the accumulator of the
 // next tile filling while one is read out.  Bounds: HBM's stream of W for up to some 200 tokens, the tensor pipe above.
+#include <atomic>
+
 #include "dm_i8.h"
 #include "dm_ptx.cuh"
 
@@ -404,9 +406,15 @@ int launch(const I8Args& A, I8Params& P, int sms, cudaStream_t stream) {
     CUtensorMap tmap_w, tmap_a;
     if (!tensor_map_u8(&tmap_w, A.w, A.V, A.d, A.ld_w, P.tile_m) || !tensor_map_u8(&tmap_a, A.a, A.n_rows, A.d, A.ld_a, P.tile_n / kCtas))
         return DM_ECUDA;
-    if (cudaFuncSetAttribute(matmul_i8_kernel<kPair, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) {
-        cudaGetLastError();
-        return DM_ECUDA;
+    static std::atomic<uint64_t> allowed{0};      // devices on which this kernel may have that much shared memory
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return DM_ECUDA;
+    if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (cudaFuncSetAttribute(matmul_i8_kernel<kPair, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit) != cudaSuccess) {
+            cudaGetLastError();
+            return DM_ECUDA;
+        }
+        if (dev < 64) allowed.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     const int units = P.n_tiles < all ? P.n_tiles : all;
     cudaLaunchConfig_t cfg{};

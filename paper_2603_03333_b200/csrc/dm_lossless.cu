@@ -11,7 +11,7 @@
 // next_kernel: a cluster per sequence finds n and draws from row n.  Bounds: fp64 instructions.  Decisions and the place in the cumulative sum
 // are those of 64-bit arithmetic: a position whose u_t lies within 2^-16 of the fp32 ratio (far more than that
 // is off, see kBand) is decided again from fp64 sums, and all sums over row n are fp64 with exponentials good to
-// some 2^-50 (see exp_neg).  In fp32 a token of the flat tail of 100 thousand would come out one place off in about a
+// 2^-42 (see weight).  In fp32 a token of the flat tail of 100 thousand would come out one place off in about a
 // draw of ten, and two engines with equal random numbers would drift apart.
 #include <math.h>
 #include <string.h>
@@ -315,8 +315,9 @@ struct Row64 {
         base = (double)ref + (double)k0 * E.step;
     }
 };
-__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table) {
+__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table, float& top) {
     const float d = x - R.ref, kf = fmaf(d, E.c16, R.bias);      // 1.5 2^23 + (k - k0): rounded to whole numbers, in the low bits
+    top = fmaxf(top, kf);
     const int bits = __float_as_int(fmaxf(kf, 12582912.0f - 16300.0f));
     const double k = __hiloint2double(0x43300000, bits) - R.offset;
     const double r = fma(-k, E.step, (double)d);
@@ -329,6 +330,15 @@ __device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E
     e *= __hiloint2double((int)((uint32_t)__double2hiint(t) + ((uint32_t)bits << 16)), __double2loint(t));
     return kf < 12582912.0f - 16160.0f ? 0.0 : e;
 }
+
+__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table) {
+    float top = 0.0f;
+    return weight(x, R, E, table, top);
+}
+// Is the largest weight of a row (by its `top`) far from fp64's ends, so that nothing of it can have been lost?
+__device__ __forceinline__ bool in_reach(float top) { return top > 12582912.0f - 8000.0f && top < 12582912.0f + 15000.0f; }
+// A reference for a row's weights that need not be its maximum.
+__device__ __forceinline__ bool near_zero(float x, const Exp64& E) { return fabsf(x) * E.c16 < 131072.0f; }
 
 // Which of the lanes' parts (of a CTA, of a warp) holds the place `at` of their cumulative weight; `at` becomes the place
 // within it.  Where rounding (or a random number of 1) leaves none, the last part with any weight, and no place in it is reached.
@@ -354,21 +364,26 @@ __device__ __forceinline__ int part_of(double& at, double w) {
 }
 
 constexpr int kNone = 0x7FFFFFFF;
+constexpr double kAbove = 1.0 + 9.094947017729282e-13;     // 1 + 2^-40: what p has to exceed q by for the difference to count
 
 template <int kNextWarps>
 struct NextShared {
     double table[16];
     float2 warp_sum[kNextWarps][2];
     double warp_part[kNextWarps][4];
+    float2 warp_top[kNextWarps], top[2][kMaxCluster];
     double part[2][kMaxCluster][4];     // of every CTA, written by it; two sets in turn, so that one barrier per exchange does
     double scan[kNextWarps];
     int found, last;
 };
 
-// Lane i of warp 0 hands v to CTA i of the cluster: everybody's four numbers for everybody.
+// Lane i of warp 0 hands v and top to CTA i of the cluster: everybody's numbers for everybody.
 template <typename S_>
-__device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, const double (&v)[4]) {
+__device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, const double (&v)[4], float2 top) {
     if (threadIdx.x < (unsigned)cluster) {
+        const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&S.top[set][rank]), threadIdx.x);
+        ptx::st_cluster_u32(at, __float_as_uint(top.x));
+        ptx::st_cluster_u32(at + 4, __float_as_uint(top.y));
         const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&S.part[set][rank][0]), threadIdx.x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) st_cluster_f64(to + 8 * i, v[i]);
@@ -387,10 +402,12 @@ __device__ __forceinline__ void add_lanes(double (&a)[4]) {
 // The row that a token is drawn from.  Weights of entry v, in units of 1 / sum p:
 //   p(v) = exp(x / T) up to a factor (see Row64),  q(v) likewise,  r(v) = max(p(v) - rho q(v), 0)  with rho = sum p / sum q.
 // Sums over r need rho, which needs the sums over p and q: one pass takes all of them, with the entries that count
-// decided by an fp32 rho (off by some 2^-20) that a quick pass over the row has left behind.  Sums A of p and D of q over
+// decided by an fp32 rho (off by some 2^-20) that the first kernel, or a quick pass over the row, has left behind.  Sums A of p and D of q over
 // those entries then give sum r = A - rho D for the rho that came out: an entry on the wrong side of the
 // border is off by less than |rho - rho~| q(v), and only entries that close to the border are, so that the sum
-// is off by the square of that, unless there is little but such entries: then the pass is done once more.
+// is off by the square of that, unless there is little but such entries: then the pass is done once more.  A difference
+// of less than 2^-40 p counts as 0: next to a token that both are certain of it would be rounding (the exponentials are good
+// to 2^-42), and outweigh a rest of 1e-90 that is not.
 // (Two passes, the first for rho, are as exact and took 40 % longer.)
 
 // THREADS: 256, three CTAs per SM, or 512 where there are fewer CTAs than SMs.
@@ -422,20 +439,22 @@ next_kernel(const LosslessParams P, int cluster) {
     const TQ* row_q = draft_rows;
 
     // fp64 sums over the row; entry `skip` of p counts as masked.  The warps' and CTAs' sums of p, q, A, D stay in warp_part
-    // and part[set ^ 1].
+    // and part[set ^ 1].  Are the weights in reach of their reference?
     auto sums = [&](bool with_q, int skip) {
         double a[4] = {};
+        const double rho_up = rho * kAbove;
+        float2 top = make_float2(neg_inf(), neg_inf());
         const auto add = [&](auto& x, auto& y) {      // (all the exponentials side by side, without a branch between them)
             constexpr int N = sizeof(x) / sizeof(x[0]);
             double p[N], q[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[i] = weight(x[i], at_p, P.e, S.table);
+            for (int i = 0; i < N; ++i) p[i] = weight(x[i], at_p, P.e, S.table, top.x);
             if (HAS_Q && with_q) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) q[i] = weight(y[i], at_q, P.e_draft, S.table);
+                for (int i = 0; i < N; ++i) q[i] = weight(y[i], at_q, P.e_draft, S.table, top.y);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const bool more = fma(-rho, q[i], p[i]) > 0.0;
+                    const bool more = p[i] > rho_up * q[i];
                     a[1] += q[i];
                     a[2] += more ? p[i] : 0.0;
                     a[3] += more ? q[i] : 0.0;
@@ -478,25 +497,41 @@ next_kernel(const LosslessParams P, int cluster) {
         }
         __syncwarp();
         add_lanes(a);
+        top = make_float2(warp_max(top.x), warp_max(top.y));
         if (lane < 4) S.warp_part[warp][lane] = lane == 0 ? a[0] : lane == 1 ? a[1] : lane == 2 ? a[2] : a[3];
+        if (lane == 0) S.warp_top[warp] = top;
         __syncthreads();
         if (warp == 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) a[i] = lane < kNextWarps ? S.warp_part[lane][i] : 0.0;
             add_lanes(a);
+            top = S.warp_top[lane < kNextWarps ? lane : 0];
+            top = make_float2(warp_max(top.x), warp_max(top.y));
         }
-        exchange(S, set, rank, cluster, a);
+        exchange(S, set, rank, cluster, a, top);
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = lane < cluster ? S.part[set][lane][i] : 0.0;
         add_lanes(a);
         sum_p = a[0]; sum_q = a[1]; sum_a = a[2]; sum_d = a[3];
+        top = S.top[set][lane < cluster ? lane : 0];
+        top = make_float2(warp_max(top.x), warp_max(top.y));
         set ^= 1;
+        return in_reach(top.x) && (!(HAS_Q && with_q) || in_reach(top.y));
     };
-    // Row t: the maxima and an fp32 rho, then the sums.
-    auto look_at = [&](int t, bool with_q, int skip) {
+    // Row t.  The drafted token's logits are a reference as good as the rows' maxima, as a rule, and with them its ratio (from
+    // the first kernel) says what rho is; without a token some entry of the row is.  Where they are not (no such token, a
+    // ratio of nothing, logits too far apart for fp64), a quick pass over the rows finds maxima and rho first.
+    auto look_at = [&](int t, bool with_q, int skip, int tok, float ratio) {
         row_p = target + (long long)t * P.ld_target;
         row_q = draft_rows + (long long)t * P.ld_draft;
-        const bool two = HAS_Q && with_q;
+        const bool two = HAS_Q && with_q, token = (unsigned)tok < (unsigned)P.V;
+        const float x = token ? entry(row_p, tok) : warp_max(entry(row_p, (long long)lane * P.V / 32)), y = two && token ? entry(row_q, tok) : 0.0f;
+        if (near_zero(x, P.e) && (!two || (token && near_zero(y, P.e_draft) && ratio > 1e-30f))) {      // (false for a NaN)
+            at_p = Row64(x, P.e);
+            at_q = Row64(y, P.e_draft);
+            rho = two ? weight(x, at_p, P.e, S.table) / (weight(y, at_q, P.e_draft, S.table) * (double)ratio) : 0.0;
+            if (sums(with_q, skip)) return;
+        }
         Sum p, q;
         const Share<TP> sp(row_p, lo, hi);
         const Share<TQ> sq(row_q, lo, two ? hi : lo);
@@ -511,6 +546,7 @@ next_kernel(const LosslessParams P, int cluster) {
         }
         sp.add_ends(p, P.c);
         if (two) sq.add_ends(q, P.c_draft);
+        __syncwarp();
         const float2 wp = join_lanes(p.m, p.s, P.c), wq = join_lanes(q.m, q.s, P.c_draft);
         if (lane == 0) { S.warp_sum[warp][0] = wp; S.warp_sum[warp][1] = wq; }
         __syncthreads();
@@ -519,7 +555,7 @@ next_kernel(const LosslessParams P, int cluster) {
             const float2 cp = join_parts(&S.warp_sum[0][0], kNextWarps, 2, P.c), cq = join_parts(&S.warp_sum[0][1], kNextWarps, 2, P.c_draft);
             v[0] = cp.x; v[1] = cp.y; v[2] = cq.x; v[3] = cq.y;
         }
-        exchange(S, set, rank, cluster, v);
+        exchange(S, set, rank, cluster, v, make_float2(0.0f, 0.0f));
         const double* part = S.part[set][lane < cluster ? lane : 0];
         const float2 ap = join_lanes((float)part[0], lane < cluster ? (float)part[1] : 0.0f, P.c);
         const float2 aq = join_lanes((float)part[2], lane < cluster ? (float)part[3] : 0.0f, P.c_draft);
@@ -545,7 +581,7 @@ next_kernel(const LosslessParams P, int cluster) {
         if (u > a * (1.0f + kBand)) break;
         const int tok = P.draft[(long long)b * P.T + n];
         if ((unsigned)tok >= (unsigned)P.V) break;
-        look_at(n, true, -1);
+        look_at(n, true, -1, tok, a);
         known = n;
         const float xp = entry(row_p, tok), xq = HAS_Q ? entry(row_q, tok) : 0.0f;
         if (!(xp > neg_inf()) || !(sum_p > 0.0) || (HAS_Q && !(sum_q >= 0.0))) break;     // p(x) = 0, or a NaN or +inf in a row
@@ -566,9 +602,9 @@ next_kernel(const LosslessParams P, int cluster) {
     // Row n: weights r where a token was rejected against a distribution; p without the token where it was rejected by a
     // drafter that has none; else p.
     const bool rejected = n < len;
-    const int skip = rejected && !HAS_Q ? P.draft[(long long)b * P.T + n] : -1;
+    const int token = rejected ? P.draft[(long long)b * P.T + n] : -1, skip = HAS_Q ? -1 : token;
     bool against_q = HAS_Q && rejected;
-    if (known != n || skip >= 0) look_at(n, against_q, skip);
+    if (known != n || skip >= 0) look_at(n, against_q, skip, token, rejected ? P.out_accept_prob[(long long)b * P.T + n] : 0.0f);
     double total = sum_p;
     if (against_q) {
         const double guess = rho;
@@ -590,7 +626,9 @@ next_kernel(const LosslessParams P, int cluster) {
     }
     const auto entry_weight = [&](int j) {
         const double p = j == skip ? 0.0 : weight(entry(row_p, j), at_p, P.e, S.table);
-        return HAS_Q && against_q ? fmax(fma(-rho, weight(entry(row_q, j), at_q, P.e_draft, S.table), p), 0.0) : p;
+        if (!HAS_Q || !against_q) return p;
+        const double q = weight(entry(row_q, j), at_q, P.e_draft, S.table);
+        return p > rho * kAbove * q ? fma(-rho, q, p) : 0.0;
     };
     const auto part_weight = [&](const double* part) { return against_q ? part[2] - rho * part[3] : part[0]; };
     // the part that holds the place u_next * total: a CTA's, then a warp's

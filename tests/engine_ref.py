@@ -91,7 +91,7 @@ def lossless(target, draft, u_accept, u_next, draft_logits=None, draft_len=None,
             x = int(draft[b, n])
             if draft_logits is not None:
                 r = p - softmax64(draft_logits[b, n], Td)
-                r = torch.where(r < 0, torch.zeros_like(r), r)     # (a NaN stays)
+                r = torch.where(r < 2.0 ** -40 * p, torch.zeros_like(r), r)     # (a NaN stays)
             else:
                 r = p.clone()
                 if 0 <= x < V:

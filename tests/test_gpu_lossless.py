@@ -194,6 +194,19 @@ def test_large_logits_and_small_temperatures(ctx):
         check(ctx, a, T=T, Td=T)
 
 
+@pytest.mark.parametrize("draft", ["f32", None])
+def test_logits_spread_wider_than_fp64_reaches(ctx, draft):
+    """The drafted token, or the entries that are looked at first, lie e^700 and more below the row's maximum."""
+    for scale in (100.0, 400.0, 1000.0):
+        a = make(8, 3, 2001, "f32", draft, seed=int(scale), scale=scale)
+        a["u_accept"][::2] = 0.5
+        check(ctx, a)
+        a["draft"] = torch.randint(0, 2001, (8, 3), generator=torch.Generator(device=DEV).manual_seed(5), device=DEV, dtype=torch.int32)
+        check(ctx, a)
+        a["target"][:, :, ::3] = NINF
+        check(ctx, a)
+
+
 def test_lengths_outside_the_draft_are_clamped(ctx):
     a = make(4, 3, 500, seed=8)
     a["draft_len"] = torch.tensor([-3, 9, 2 ** 31 - 1, 1], dtype=torch.int32, device=DEV)
