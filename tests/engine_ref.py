@@ -2,14 +2,12 @@
 integers, and the error bounds of the CUDA path.
 
 Lossless verification.  Accepted lengths and next tokens are those of 64-bit arithmetic: they are equal.
-out_accept_prob is fp32: a term of a row's sum is 2^w, w = (x - m) log2(e)/T, with three roundings in w (the
-difference, the rounded factor, the product: 3 |w| ln 2 u for u = 2^-24), one instruction of 2^-22 = 4u, and some 7
-additions in fp32 per batch; sums of batches are joined in fp64, with one more exponential of the same kind per
-join (at most 8 warps + 5 shuffles + 8 CTAs, and the batches that raised the maximum; a factor that is
-not 1 has its own |w|, and telescopes: the exponents of one entry's factors add up to its own |w|, each factor
-adds 4u).  With Z = |w| ln 2 <= 110 (what lies below 2^-150 adds nothing) averaged under the row's own
-distribution, whose mean is at most ln V, a sum is off by at most (3 ln V + 4 + 7 + 4 * 40) u relative; p / q has two
-of them and one rounding.
+out_accept_prob is fp32: a term of a row's sum is 2^w, w = (x - m) log2(e)/T for a reference m of which the maximum is at
+most the 2^20-fold, with three roundings in w (the difference, the rounded factor, the product: 3 |w| ln 2 u for
+u = 2^-24) and one instruction of 2^-22 = 4u; |w| ln 2 averaged under the row's own distribution is at most ln V + 20 ln 2.
+Seven additions per batch, batches joined with compensation; three joins (lanes, warps, CTAs) of one
+exponential (4u and its own part of |w|) and at most 5 additions each.  A sum is off by at most
+(3 (ln V + 14) + 4 + 7 + 30) u relative; p / q has two of them, two logarithms' worth of u, and one rounding.
 
 Dropout.  x * s is one product and one rounding to the storage type; s = 1 / (1 - p) is rounded to fp32.  The gradient
 adds up to K fp32 values (K u sum |g|), times s, rounded once.
@@ -31,8 +29,8 @@ def single(x):
 
 
 def accept_tol(V, with_q):
-    one = (3 * math.log(max(V, 2)) + 11 + 160) * U
-    return one * (2 if with_q else 1) + 2 * U
+    one = (3 * (math.log(max(V, 2)) + 14) + 41) * U
+    return one * (2 if with_q else 1) + 4 * U
 
 
 def softmax64(x, T):

@@ -229,6 +229,24 @@ def test_many_sequences(ctx):
     check(ctx, a)
 
 
+@pytest.mark.parametrize("descending", [False, True])
+def test_rows_in_order(ctx, descending):
+    """Every batch of a row above (below) all before it: sums must not be rounded anew with each."""
+    for V, B, scale in ((300000, 8, 0.5), (300000, 8, 8.0), (40001, 30, 0.01)):
+        a = make(B, 1, V, "f32", "f32", seed=V, scale=scale)
+        for k in ("target", "draft_logits"):
+            a[k].copy_(torch.sort(a[k], dim=2, descending=descending).values)
+        check(ctx, a)
+    # many positions, each read by one CTA alone
+    a = make(300, 5, 20001, "bf16", "bf16", seed=3, scale=0.5)
+    for k in ("target", "draft_logits"):
+        a[k].copy_(torch.sort(a[k], dim=2, descending=descending).values)
+    got = ctx.verify_lossless(**a)
+    lp = torch.log_softmax(a["target"][:, :5].double(), 2) - torch.log_softmax(a["draft_logits"].double(), 2)
+    want = lp.gather(2, a["draft"].long()[:, :, None])[:, :, 0].exp().clamp(max=1.0)
+    assert bool(((got["accept_prob"].double() - want).abs() <= ref.accept_tol(20001, True) * want).all())
+
+
 def test_streams_graph_and_two_calls_at_once(ctx):
     a, o = make(5, 4, 20001, seed=21), make(6, 3, 30011, "f32", "f32", seed=22)
     want_a, want_o = check(ctx, a), check(ctx, o)
