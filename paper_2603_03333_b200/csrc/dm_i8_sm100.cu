@@ -7,7 +7,14 @@
 // matmul_i8_kernel.  Rows of W are the M operand (128 of a CTA, 256 of a CTA pair), up to 256 tokens the N operand, so that an
 // epilogue thread owns a vocabulary entry and a warp's store of one token's outputs is contiguous as it comes out of
 // TMEM.  CTAs (pairs) walk over tiles, the token tiles of one piece of W next to each other, with the accumulator of the
-// next tile filling while one is read out.  Bounds: HBM's stream of W for up to some 200 tokens, the tensor pipe above.
+// next tile filling while one is read out.  Bounds: HBM's stream of W for up to some 200 tokens, the tensor pipe above, and
+// under sustained load the power cap in either case (integers of full range toggle every bit of what is streamed).
+// Measured, quantisation included: one token against 128256 x 4096 90-96 us (525 MB, a bare read of which takes 78-86), 61
+// tokens against 151936 x 4096 117-120 us (622 MB; 130-135 back to back), 2047 against 128256 x 8192 1.54-1.6 ms
+// (2.7-2.8 PFLOP/s; back to back 1.78-1.84 ms, 2.35-2.4 PFLOP/s, 0.85 of twice what a bf16 GEMM sustains).
+// Tried: two blocks of 256 tokens per piece of W, filling TMEM (a quarter less traffic into shared memory, but read-out that
+// the next tile does not hide: 978 against 826 us at d = 4096, the same at 8192); pairs for few tokens, steps that start at
+// another depth in every CTA (no difference).
 #include <atomic>
 
 #include "dm_i8.h"
@@ -391,7 +398,7 @@ int launch(const I8Args& A, I8Params& P, int sms, cudaStream_t stream) {
     P.once = P.n_tiles_n == 1;
     if (P.once && tiles_m > all) {
         // W is read once and bounds the call: the same number of rows for everybody, in equal tiles (one token against
-        // 128256 x 4096, 6.8 tiles of 128 rows for each CTA: FIG us in 7 tiles of 124, FIG in up to 7 of 128)
+        // 128256 x 4096, 6.8 tiles of 128 rows for each CTA: 90 us in 7 tiles of 124, 92 in up to 7 of 128)
         const int rounds = (tiles_m + all - 1) / all;
         const long long share = (long long)all * kCtas * rounds;
         P.tile_m = (int)((((long long)A.V + share - 1) / share + 3) & ~3ll);

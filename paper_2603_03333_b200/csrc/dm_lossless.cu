@@ -608,10 +608,16 @@ next_kernel(const LosslessParams P, int cluster) {
     // Row n: weights r where a token was rejected against a distribution; p without the token where it was rejected by a
     // drafter that has none; else p.
     const bool rejected = n < len;
-    const int token = rejected ? P.draft[(long long)b * P.T + n] : -1, skip = HAS_Q ? -1 : token;
+    const int token = rejected ? P.draft[(long long)b * P.T + n] : -1;
+    int skip = !HAS_Q && (unsigned)token < (unsigned)P.V ? token : -1;
     bool against_q = HAS_Q && rejected;
     if (known != n || skip >= 0) look_at(n, against_q, skip, token, rejected ? P.out_accept_prob[(long long)b * P.T + n] : 0.0f);
     double total = sum_p;
+    if (skip >= 0 && total == 0.0) {      // (nothing but the token)
+        skip = -1;
+        look_at(n, false, -1, token, 0.0f);
+        total = sum_p;
+    }
     if (against_q) {
         const double guess = rho;
         rho = sum_q > 0.0 ? sum_p / sum_q : 0.0;
