@@ -13,8 +13,8 @@
 // can be off, see kBand) is decided again from fp64 sums, and all sums over row n are fp64 with exponentials good to
 // 2^-42 (see weight).  In fp32 a token of the flat tail of 100 thousand would come out one place off in about a
 // draw of ten, and two engines with equal random numbers would drift apart.
-// Measured: 96 sequences of 7 tokens, 151936 bf16 entries, both models (408 MB) 150 us (138 back to back): 73 + 74, where HBM
-// takes 62; one sequence of 5 tokens of 128256 18 us.  Rows through registers instead of the ring, per-thread joins and
+// Measured: 96 sequences of 7 tokens, 151936 bf16 entries, both models (408 MB) 150 us (134 back to back in a graph): 73 + 74,
+// where HBM takes 62; one sequence of 5 tokens of 128256 18-20 us (14 in a graph), 4 tokens of 4096 fp32 14 (9).  Rows through registers instead of the ring, per-thread joins and
 // two fp64 passes took 396 and 89; ratios and draws in one kernel, a cluster going through its sequence's rows, 160 and 22.
 #include <math.h>
 #include <string.h>
@@ -181,7 +181,7 @@ constexpr int kRatioSmem = kStages * 4 * kRatioThreads * 16;
 
 template <typename TP, typename TQ, bool HAS_Q>
 __global__ void __launch_bounds__(kRatioThreads)
-ratio_kernel(const LosslessParams P, int cluster) {
+ratio_kernel(const __grid_constant__ LosslessParams P, int cluster) {
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ __align__(16) float2 s_warp[kRatioWarps][2];     // maximum and sum of the target's row, of the draft's
     __shared__ __align__(16) float2 s_part[kMaxCluster][2];     // of every CTA, written by it into the first
@@ -306,7 +306,7 @@ ratio_kernel(const LosslessParams P, int cluster) {
 // what the polynomial leaves out is below 2^-42 of the value.  Twenty instructions, eight of them fp64; with a
 // polynomial for |r/T| <= ln2/2 that needs no table, three fp64 instructions more.  Sixteen doubles lie in as many pairs of banks: lanes never
 // conflict.  Where k would be beyond 2^17, x - m takes x's place: fp32 holds it exactly for every entry that counts.
-// x = -inf: 0.  A NaN, or +inf (then m is +inf too): NaN.  Below e^-700 of the maximum: 0.
+// x = -inf, and what lies below e^-700 of the reference: 0.  A NaN, or +inf (then m is +inf too): NaN.
 struct Row64 {
     float ref, bias;      // m or 0; 1.5 2^23 - k0
     double offset;        // 2^52 + (bits of 1.5 2^23) - k0
@@ -321,9 +321,8 @@ struct Row64 {
         base = (double)ref + (double)k0 * E.step;
     }
 };
-__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table, float& top) {
+__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table) {
     const float d = x - R.ref, kf = fmaf(d, E.c16, R.bias);      // 1.5 2^23 + (k - k0): rounded to whole numbers, in the low bits
-    top = fmaxf(top, kf);
     const int bits = __float_as_int(fmaxf(kf, 12582912.0f - 16300.0f));
     const double k = __hiloint2double(0x43300000, bits) - R.offset;
     const double r = fma(-k, E.step, (double)d);
@@ -336,13 +335,11 @@ __device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E
     e *= __hiloint2double((int)((uint32_t)__double2hiint(t) + ((uint32_t)bits << 16)), __double2loint(t));
     return kf < 12582912.0f - 16160.0f ? 0.0 : e;
 }
-
-__device__ __forceinline__ double weight(float x, const Row64& R, const Exp64& E, const double* table) {
-    float top = 0.0f;
-    return weight(x, R, E, table, top);
+// Is a row's largest entry far from fp64's ends, measured from the row's reference, so that nothing of it can have been lost?
+__device__ __forceinline__ bool in_reach(float top, const Row64& R, const Exp64& E) {
+    const float kf = fmaf(top - R.ref, E.c16, R.bias);
+    return kf > 12582912.0f - 500.0f && kf < 12582912.0f + 15000.0f;
 }
-// Is the largest weight of a row (by its `top`) far from fp64's ends, so that nothing of it can have been lost?
-__device__ __forceinline__ bool in_reach(float top) { return top > 12582912.0f - 8000.0f && top < 12582912.0f + 15000.0f; }
 // A reference for a row's weights that need not be its maximum.
 __device__ __forceinline__ bool near_zero(float x, const Exp64& E) { return fabsf(x) * E.c16 < 131072.0f; }
 
@@ -381,6 +378,9 @@ struct NextShared {
     double part[2][kMaxCluster][4];     // of every CTA, written by it; two sets in turn, so that one barrier per exchange does
     double scan[kNextWarps];
     int found, last;
+    int tok[32];                        // of 32 positions: drafted token, random number, logits
+    float u[32], x[32], y[32], ratio[32];
+    float behind, u_next;
 };
 
 // Lane i of warp 0 hands v and top to CTA i of the cluster: everybody's numbers for everybody.
@@ -396,6 +396,14 @@ __device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, 
     }
     __syncwarp();
     ptx::cluster_sync_all();
+}
+// a += p and d += q where p > border, by predicate: a branch would part the exponentials, a selection costs four instructions.
+__device__ __forceinline__ void add_if_more(double p, double border, double q, double& a, double& d) {
+    asm("{\n\t.reg .pred more;\n\t"
+        "setp.gt.f64 more, %2, %3;\n\t"
+        "@more add.rn.f64 %0, %0, %2;\n\t"
+        "@more add.rn.f64 %1, %1, %4;\n\t}"
+        : "+d"(a), "+d"(d) : "d"(p), "d"(border), "d"(q));
 }
 // Sums over the lanes, the same bits in every lane.
 __device__ __forceinline__ void add_lanes(double (&a)[4]) {
@@ -419,16 +427,13 @@ __device__ __forceinline__ void add_lanes(double (&a)[4]) {
 // THREADS: 256, three CTAs per SM, or 512 where there are fewer CTAs than SMs.
 template <typename TP, typename TQ, bool HAS_Q, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1)
-next_kernel(const LosslessParams P, int cluster) {
+next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
     constexpr int kNextThreads = THREADS, kNextWarps = THREADS / 32;
     __shared__ NextShared<kNextWarps> S;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = (int)(blockIdx.x / (unsigned)cluster), rank = (int)(blockIdx.x % (unsigned)cluster);
     if (threadIdx.x < 16) S.table[threadIdx.x] = P.table[threadIdx.x];
     if (threadIdx.x == 0) { S.found = kNone; S.last = -1; }
-    ptx::cluster_sync_all();      // (the other CTAs have started: their shared memory may be written)
-    ptx::griddep_wait();
-
     const int len = P.draft_len == nullptr ? P.T : min(P.T, max(0, P.draft_len[b]));
     // the CTA's part of a row, and the warp's part of that, both in token order
     const int lo = (int)min((long long)P.V, (long long)rank * P.share), hi = (int)min((long long)P.V, (long long)lo + P.share);
@@ -454,22 +459,24 @@ next_kernel(const LosslessParams P, int cluster) {
             constexpr int N = sizeof(x) / sizeof(x[0]);
             double p[N], q[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[i] = weight(x[i], at_p, P.e, S.table, top.x);
+            for (int i = 0; i < N; ++i) p[i] = weight(x[i], at_p, P.e, S.table);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) top.x = fmaxf(top.x, fmaxf(x[i], x[i + 1 < N ? i + 1 : i]));
             if (HAS_Q && with_q) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) q[i] = weight(y[i], at_q, P.e_draft, S.table, top.y);
+                for (int i = 0; i < N; ++i) q[i] = weight(y[i], at_q, P.e_draft, S.table);
+#pragma unroll
+                for (int i = 0; i < N; i += 2) top.y = fmaxf(top.y, fmaxf(y[i], y[i + 1 < N ? i + 1 : i]));
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const bool more = p[i] > rho_up * q[i];
                     a[1] += q[i];
-                    a[2] += more ? p[i] : 0.0;
-                    a[3] += more ? q[i] : 0.0;
+                    add_if_more(p[i], rho_up * q[i], q[i], a[2], a[3]);
                 }
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) a[0] += p[i];
         };
-        constexpr int kAhead = 4;
+        constexpr int kAhead = 8;
         const TP* at_x = row_p + w_lo + lane;
         const TQ* at_y = row_q + w_lo + lane;
         int left = w_hi - w_lo - lane, off = skip - w_lo - lane;      // entries from the lane's on; where the one to skip is
@@ -485,16 +492,11 @@ next_kernel(const LosslessParams P, int cluster) {
             left -= 32 * kAhead;
             off -= 32 * kAhead;
         };
-        float x[kAhead], y[kAhead] = {}, x2[kAhead], y2[kAhead] = {};
-        bool more = left > 32 * (kAhead - 1);
-        if (more) load(x, y);
 #pragma unroll 1
-        while (more) {       // two batches of loads on their way
-            more = left > 32 * (kAhead - 1);
-            if (more) load(x2, y2);
+        while (left > 32 * (kAhead - 1)) {
+            float x[kAhead], y[kAhead] = {};
+            load(x, y);
             add(x, y);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) { x[i] = x2[i]; y[i] = y2[i]; }
         }
 #pragma unroll 1
         for (; left > 0; left -= 32, off -= 32, at_x += 32, at_y += 32) {
@@ -522,117 +524,159 @@ next_kernel(const LosslessParams P, int cluster) {
         top = S.top[set][lane < cluster ? lane : 0];
         top = make_float2(warp_max(top.x), warp_max(top.y));
         set ^= 1;
-        return in_reach(top.x) && (!(HAS_Q && with_q) || in_reach(top.y));
+        return in_reach(top.x, at_p, P.e) && (!(HAS_Q && with_q) || in_reach(top.y, at_q, P.e_draft));
     };
-    // Row t.  The drafted token's logits are a reference as good as the rows' maxima, as a rule, and with them its ratio (from
-    // the first kernel) says what rho is; without a token some entry of the row is.  Where they are not (no such token, a
-    // ratio of nothing, logits too far apart for fp64), a quick pass over the rows finds maxima and rho first.
-    auto look_at = [&](int t, bool with_q, int skip, int tok, float ratio) {
-        row_p = target + (long long)t * P.ld_target;
-        row_q = draft_rows + (long long)t * P.ld_draft;
-        const bool two = HAS_Q && with_q, token = (unsigned)tok < (unsigned)P.V;
-        const float x = token ? entry(row_p, tok) : warp_max(entry(row_p, (long long)lane * P.V / 32)), y = two && token ? entry(row_q, tok) : 0.0f;
-        if (near_zero(x, P.e) && (!two || (token && near_zero(y, P.e_draft) && ratio > 1e-30f))) {      // (false for a NaN)
+    // 32 positions' drafted tokens, random numbers and logits (by warp 0), of the first 32, and of what follows the draft,
+    // ahead of the ratios.
+    int window = 0;
+    const auto open_window = [&]() {
+        const int t = window + lane;
+        if (warp != 0 || t >= len) return;
+        const int tok = P.draft[(long long)b * P.T + t];
+        S.tok[lane] = tok;
+        S.u[lane] = P.u_accept[(long long)b * P.T + t];
+        if ((unsigned)tok < (unsigned)P.V) {
+            S.x[lane] = entry(target + (long long)t * P.ld_target, tok);
+            if (HAS_Q) S.y[lane] = entry(draft_rows + (long long)t * P.ld_draft, tok);
+        }
+    };
+    open_window();
+    if (warp == 1) {
+        const float behind = len < P.T + P.bonus ? warp_max(entry(target + (long long)len * P.ld_target, (long long)lane * P.V / 32)) : 0.0f;
+        if (lane == 0) { S.behind = behind; S.u_next = P.u_next[b]; }
+    }
+    __syncwarp();
+    ptx::cluster_sync_all();      // (the other CTAs have started: their shared memory may be written)
+    ptx::griddep_wait();
+    const auto ratios = [&]() {
+        if (warp == 0 && window + lane < len) S.ratio[lane] = P.out_accept_prob[(long long)b * P.T + window + lane];
+        __syncthreads();
+    };
+    ratios();
+
+    // Row n, and whether a token was rejected there: known at once, or after a look at the row in 64 bits.
+    int n = 0, skip = -1;
+    bool decided = false, against_q = false;
+    double total = 0.0;
+    // (one loop, so that there is one copy of the sums in the code: a single sequence's draw waits for instructions, too)
+#pragma unroll 1
+    for (;;) {
+        // the accepted prefix: up to the first position that is not surely accepted
+        while (!decided) {
+            if (n >= len) { decided = true; break; }
+            if (n >= window + 32) {
+                __syncthreads();
+                window += 32;
+                open_window();
+                ratios();
+            }
+            const int t = window + lane;
+            const uint32_t open = __ballot_sync(0xFFFFFFFFu, t >= n && t < len && !(S.u[lane] < S.ratio[lane] * (1.0f - kBand)));
+            if (open == 0) { n = min(len, window + 32); continue; }
+            const int first = __ffs(open) - 1;
+            n = window + first;
+            decided = S.u[first] > S.ratio[first] * (1.0f + kBand) || (unsigned)S.tok[first] >= (unsigned)P.V;
+            break;
+        }
+        if (n >= P.T + P.bonus) {      // every drafted token accepted and no row behind them
+            if (rank == 0 && threadIdx.x == 0) { P.out_accept_len[b] = n; P.out_next[b] = -1; }
+            return;
+        }
+        const bool drafted = n < len;
+        const int tok = drafted ? S.tok[n - window] : -1;
+        const float ratio = drafted ? S.ratio[n - window] : 0.0f;
+        const bool token = (unsigned)tok < (unsigned)P.V;
+        against_q = HAS_Q && drafted;
+        skip = !HAS_Q && decided && token ? tok : -1;
+
+        // The drafted token's logits are a reference as good as the rows' maxima, as a rule, and with them its ratio (from the
+        // first kernel) says what rho is; without a token some entry of the row is.  Where they are not (no such token, a
+        // ratio of nothing, logits too far apart for fp64), a quick pass over the rows finds maxima and rho first.
+        row_p = target + (long long)n * P.ld_target;
+        row_q = draft_rows + (long long)n * P.ld_draft;
+        const float x = drafted ? S.x[n - window] : S.behind, y = HAS_Q && drafted ? S.y[n - window] : 0.0f;      // (of a token that does not exist: not used)
+        enum { kQuick, kCareful, kExact } how = kCareful;
+        if (drafted == token && near_zero(x, P.e) && (!against_q || (near_zero(y, P.e_draft) && ratio > 1e-30f))) {      // (false for a NaN)
+            how = kQuick;
             at_p = Row64(x, P.e);
             at_q = Row64(y, P.e_draft);
-            rho = two ? weight(x, at_p, P.e, S.table) / (weight(y, at_q, P.e_draft, S.table) * (double)ratio) : 0.0;
-            if (sums(with_q, skip)) return;
+            rho = against_q ? weight(x, at_p, P.e, S.table) / (weight(y, at_q, P.e_draft, S.table) * (double)ratio) : 0.0;
         }
-        Sum p, q;
-        const Share<TP> sp(row_p, lo, hi);
-        const Share<TQ> sq(row_q, lo, two ? hi : lo);
 #pragma unroll 1
-        for (int v0 = threadIdx.x; v0 < max(sp.vecs, sq.vecs); v0 += kNextThreads) {
-            uint4 v[1] = {make_uint4(Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone)};
-            uint4 w[1] = {make_uint4(Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone)};
-            if (v0 < sp.vecs) v[0] = sp.body[v0];
-            if (v0 < sq.vecs) w[0] = sq.body[v0];
-            sp.add(p, v, P.c);
-            if (two) sq.add(q, w, P.c_draft);
+        for (;;) {
+            if (how == kCareful) {
+                const bool two = against_q;
+                Sum p, q;
+                const Share<TP> sp(row_p, lo, hi);
+                const Share<TQ> sq(row_q, lo, two ? hi : lo);
+#pragma unroll 1
+                for (int v0 = threadIdx.x; v0 < max(sp.vecs, sq.vecs); v0 += kNextThreads) {
+                    uint4 v[1] = {make_uint4(Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone, Vec<TP>::kNone)};
+                    uint4 w[1] = {make_uint4(Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone, Vec<TQ>::kNone)};
+                    if (v0 < sp.vecs) v[0] = sp.body[v0];
+                    if (v0 < sq.vecs) w[0] = sq.body[v0];
+                    sp.add(p, v, P.c);
+                    if (two) sq.add(q, w, P.c_draft);
+                }
+                sp.add_ends(p, P.c);
+                if (two) sq.add_ends(q, P.c_draft);
+                __syncwarp();
+                const float2 wp = join_lanes(p.m, p.s, P.c), wq = join_lanes(q.m, q.s, P.c_draft);
+                if (lane == 0) { S.warp_sum[warp][0] = wp; S.warp_sum[warp][1] = wq; }
+                __syncthreads();
+                double v[4] = {};
+                if (warp == 0) {
+                    const float2 cp = join_parts(&S.warp_sum[0][0], kNextWarps, 2, P.c), cq = join_parts(&S.warp_sum[0][1], kNextWarps, 2, P.c_draft);
+                    v[0] = cp.x; v[1] = cp.y; v[2] = cq.x; v[3] = cq.y;
+                }
+                exchange(S, set, rank, cluster, v, make_float2(0.0f, 0.0f));
+                const double* part = S.part[set][lane < cluster ? lane : 0];
+                const float2 ap = join_lanes((float)part[0], lane < cluster ? (float)part[1] : 0.0f, P.c);
+                const float2 aq = join_lanes((float)part[2], lane < cluster ? (float)part[3] : 0.0f, P.c_draft);
+                at_p = Row64(ap.x, P.e);
+                at_q = Row64(aq.x, P.e_draft);
+                rho = aq.y > 0.0f ? (double)ap.y * weight(ap.x, at_p, P.e, S.table) / ((double)aq.y * weight(aq.x, at_q, P.e_draft, S.table)) : 0.0;
+                set ^= 1;
+            }
+            if (!sums(against_q, skip) && how == kQuick) { how = kCareful; continue; }
+            total = sum_p;
+            if (against_q) {
+                const double guess = rho;
+                rho = sum_q > 0.0 ? sum_p / sum_q : 0.0;
+                total = sum_a - rho * sum_d;
+                if (how != kExact && rho != guess && !(total > sum_p * 0.0009765625)) {      // p and q nearly equal (or not numbers): with the rho that came out
+                    how = kExact;
+                    continue;
+                }
+            }
+            break;
         }
-        sp.add_ends(p, P.c);
-        if (two) sq.add_ends(q, P.c_draft);
-        __syncwarp();
-        const float2 wp = join_lanes(p.m, p.s, P.c), wq = join_lanes(q.m, q.s, P.c_draft);
-        if (lane == 0) { S.warp_sum[warp][0] = wp; S.warp_sum[warp][1] = wq; }
-        __syncthreads();
-        double v[4] = {};
-        if (warp == 0) {
-            const float2 cp = join_parts(&S.warp_sum[0][0], kNextWarps, 2, P.c), cq = join_parts(&S.warp_sum[0][1], kNextWarps, 2, P.c_draft);
-            v[0] = cp.x; v[1] = cp.y; v[2] = cq.x; v[3] = cq.y;
-        }
-        exchange(S, set, rank, cluster, v, make_float2(0.0f, 0.0f));
-        const double* part = S.part[set][lane < cluster ? lane : 0];
-        const float2 ap = join_lanes((float)part[0], lane < cluster ? (float)part[1] : 0.0f, P.c);
-        const float2 aq = join_lanes((float)part[2], lane < cluster ? (float)part[3] : 0.0f, P.c_draft);
-        at_p = Row64(ap.x, P.e);
-        at_q = Row64(aq.x, P.e_draft);
-        rho = aq.y > 0.0f ? (double)ap.y * weight(ap.x, at_p, P.e, S.table) / ((double)aq.y * weight(aq.x, at_q, P.e_draft, S.table)) : 0.0;
-        set ^= 1;
-        sums(with_q, skip);
-    };
-
-    // the accepted prefix: the first position that is not surely accepted, decided in 64 bits if it may be
-    int n = 0, known = -1;       // known: the row whose sums these are
-    while (n < len) {
-        const int t = n + lane;
-        float a = 1.0f, u = 0.0f;
-        if (t < len) { a = P.out_accept_prob[(long long)b * P.T + t]; u = P.u_accept[(long long)b * P.T + t]; }
-        const uint32_t open = __ballot_sync(0xFFFFFFFFu, !(u < a * (1.0f - kBand)));
-        if (open == 0) { n = min(len, n + 32); continue; }
-        const int first = __ffs(open) - 1;
-        n += first;
-        a = __shfl_sync(0xFFFFFFFFu, a, first);
-        u = __shfl_sync(0xFFFFFFFFu, u, first);
-        if (u > a * (1.0f + kBand)) break;
-        const int tok = P.draft[(long long)b * P.T + n];
-        if ((unsigned)tok >= (unsigned)P.V) break;
-        look_at(n, true, -1, tok, a);
-        known = n;
-        const float xp = entry(row_p, tok), xq = HAS_Q ? entry(row_q, tok) : 0.0f;
-        if (!(xp > neg_inf()) || !(sum_p > 0.0) || (HAS_Q && !(sum_q >= 0.0))) break;     // p(x) = 0, or a NaN or +inf in a row
-        if (!HAS_Q || xq > neg_inf()) {      // (q(x) = 0 otherwise)
+        if (decided) break;
+        // is this position's token accepted?  (p(x) = 0, or a NaN or +inf in a row: no)
+        bool ok = x > neg_inf() && sum_p > 0.0 && (!HAS_Q || sum_q >= 0.0);
+        if (ok && (!HAS_Q || y > neg_inf())) {      // (q(x) = 0 otherwise: yes)
             // by logarithms: p(x) and q(x) may both lie below fp64's range
-            double l = ((double)xp - at_p.base) * P.inv_temp - log(sum_p);
-            if (HAS_Q) l -= ((double)xq - at_q.base) * P.inv_draft_temp - log(sum_q);
-            if (!(u <= 0.0f || (double)u < exp(l))) break;
+            double l = ((double)x - at_p.base) * P.inv_temp - log(sum_p);
+            if (HAS_Q) l -= ((double)y - at_q.base) * P.inv_draft_temp - log(sum_q);
+            const float u = S.u[n - window];
+            ok = u <= 0.0f || (double)u < exp(l);
         }
-        ++n;
+        if (ok) { ++n; continue; }
+        decided = true;
+        if (HAS_Q) break;       // (without a draft's distribution the sums have to leave the token out)
     }
     if (rank == 0 && threadIdx.x == 0) P.out_accept_len[b] = n;
-    if (n >= P.T + P.bonus) {      // every drafted token accepted and no row behind them
-        if (rank == 0 && threadIdx.x == 0) P.out_next[b] = -1;
+    if (skip >= 0 && total == 0.0) {      // nothing but the rejected token
+        if (rank == 0 && threadIdx.x == 0) P.out_next[b] = entry(row_p, skip) > neg_inf() ? skip : -1;
         return;
     }
-
-    // Row n: weights r where a token was rejected against a distribution; p without the token where it was rejected by a
-    // drafter that has none; else p.
-    const bool rejected = n < len;
-    const int token = rejected ? P.draft[(long long)b * P.T + n] : -1;
-    int skip = !HAS_Q && (unsigned)token < (unsigned)P.V ? token : -1;
-    bool against_q = HAS_Q && rejected;
-    if (known != n || skip >= 0) look_at(n, against_q, skip, token, rejected ? P.out_accept_prob[(long long)b * P.T + n] : 0.0f);
-    double total = sum_p;
-    if (skip >= 0 && total == 0.0) {      // (nothing but the token)
-        skip = -1;
-        look_at(n, false, -1, token, 0.0f);
+    const bool from_q = against_q;
+    if (against_q && total == 0.0) {       // p - q leaves nothing: p
+        against_q = false;
         total = sum_p;
     }
-    if (against_q) {
-        const double guess = rho;
-        rho = sum_q > 0.0 ? sum_p / sum_q : 0.0;
-        total = sum_a - rho * sum_d;
-        if (rho != guess && !(total > sum_p * 0.0009765625)) {      // p and q nearly equal (or not numbers): with the rho that came out
-            sums(true, -1);
-            total = sum_a - rho * sum_d;
-        }
-        if (total == 0.0) {       // p - q leaves nothing: p
-            against_q = false;
-            total = sum_p;
-        }
-    }
     // (no CTA writes to another from here on: each may leave when it is done)
-    if (!(total > 0.0) || (HAS_Q && rejected && !(sum_q >= 0.0))) {      // nothing to draw from, or a NaN or +inf in a row
+    if (!(sum_p > 0.0) || !(total > 0.0) || (from_q && !(sum_q >= 0.0))) {      // nothing to draw from, or a NaN or +inf in a row
         if (rank == 0 && threadIdx.x == 0) P.out_next[b] = -1;
         return;
     }
@@ -644,7 +688,7 @@ next_kernel(const LosslessParams P, int cluster) {
     };
     const auto part_weight = [&](const double* part) { return against_q ? part[2] - rho * part[3] : part[0]; };
     // the part that holds the place u_next * total: a CTA's, then a warp's
-    double place = (double)P.u_next[b] * total;
+    double place = (double)S.u_next * total;
     if (part_of(place, lane < cluster ? part_weight(S.part[set ^ 1][lane]) : 0.0) != rank) return;
     const int pick = part_of(place, lane < kNextWarps ? part_weight(S.warp_part[lane]) : 0.0);
     // the entry within that: the whole block, a run of four entries per thread
