@@ -13,7 +13,10 @@
 // otherwise be generated twice).
 //
 // What bounds it: the generator, then HBM.  Ten rounds are 20 widening multiplies per quad, at a quarter of the issue rate; in a
-// loop over paths a quarter of them stays the same (see PhiloxQuad).  What is left keeps that pipe 72 % and the ALU 57 % busy.
+// loop over paths a quarter of them stays the same (see PhiloxQuad).  What is left keeps that pipe 72 % and the ALU 57 % busy,
+// and takes more: timed alone, the seven rounds are 58 cycles per quad, warp and quarter of an SM, and each integer
+// instruction beside them (comparison, selection, address) 2, as if multiplier and ALU were fed through one port.  A quad here has
+// some 49 of both: 97 cycles, as many as measured.
 // Measured: 4096 rows of 4096 bf16 under 8 paths (302 MB) 92-94 us, where the multiplies alone take 58 and HBM 46;
 // the gradient of 976 x 16 rows of 8192 bf16 (272 MB) 98 us; 4084 rows of 5003 fp32 (163 MB, rows off 16-byte boundaries) 39-41 us.
 // Round keys as constants, two vectors a lane, divisions by multiplication: 103, 107 and 56 us before.

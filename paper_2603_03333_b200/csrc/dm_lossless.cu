@@ -768,14 +768,14 @@ cudaLaunchConfig_t launch_config(cudaLaunchAttribute (&attrs)[2], int clusters, 
 
 // Clusters of this size that the device runs at a time (looked up once for each kernel, device and size).
 template <auto KERNEL>
-int clusters_at_once(int cluster, int threads) {
+int clusters_at_once(int cluster, int threads, int smem) {
     constexpr int kDevices = 16;
     static std::atomic<int> known[kDevices][kMaxCluster + 1];
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
     if (dev < kDevices && (n = known[dev][cluster].load(std::memory_order_relaxed)) > 0) return n;
     cudaLaunchAttribute attrs[2]{};
-    const cudaLaunchConfig_t cfg = launch_config(attrs, 1, cluster, threads, 0, false, nullptr);
+    const cudaLaunchConfig_t cfg = launch_config(attrs, 1, cluster, threads, smem, false, nullptr);
     if (cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) != cudaSuccess) {
         cudaGetLastError();
         return 0;
@@ -802,6 +802,8 @@ int launch(LosslessParams& P, cudaStream_t stream) {
         int cluster = 1;
         while (cluster < kMaxCluster && enough(2 * cluster) && 2ll * P.B * P.T * cluster <= 1400) cluster *= 2;
         if (!allow<ratio_kernel<TP, TQ, HAS_Q>>(kRatioSmem)) return DM_ECUDA;
+        // (a part of a GPU may have no room for the largest clusters)
+        while (cluster > 1 && clusters_at_once<ratio_kernel<TP, TQ, HAS_Q>>(cluster, kRatioThreads, kRatioSmem) == 0) cluster /= 2;
         const int st = run(ratio_kernel<TP, TQ, HAS_Q>, P.B * P.T, cluster, kRatioThreads, kRatioSmem, false);
         if (st != DM_OK) return st;
     }
@@ -812,7 +814,7 @@ int launch(LosslessParams& P, cudaStream_t stream) {
     if (!allow<next_kernel<TP, TQ, HAS_Q, 512>>(0) || !allow<next_kernel<TP, TQ, HAS_Q, 256>>(0)) return DM_ECUDA;
     const auto largest = [&](auto at_once, int threads, int least) {
         for (int cluster = kMaxCluster; cluster >= least; --cluster)
-            if (enough(cluster) && at_once(cluster, threads) >= P.B) return cluster;
+            if (enough(cluster) && at_once(cluster, threads, 0) >= P.B) return cluster;
         return 0;
     };
     // (behind the ratios the kernel waits for them before it reads anything)
@@ -821,7 +823,10 @@ int launch(LosslessParams& P, cudaStream_t stream) {
     int cluster = largest(clusters_at_once<next_kernel<TP, TQ, HAS_Q, 512>>, 512, (most < 4 ? most : 4));
     if (cluster > 0) return run(next_kernel<TP, TQ, HAS_Q, 512>, P.B, cluster, 512, 0, P.T > 0);
     cluster = largest(clusters_at_once<next_kernel<TP, TQ, HAS_Q, 256>>, 256, (most < 4 ? most : 4));
-    if (cluster == 0) cluster = (most < 6 ? most : 6);
+    if (cluster == 0) {
+        cluster = (most < 6 ? most : 6);
+        while (cluster > 1 && clusters_at_once<next_kernel<TP, TQ, HAS_Q, 256>>(cluster, 256, 0) == 0) --cluster;
+    }
     return run(next_kernel<TP, TQ, HAS_Q, 256>, P.B, cluster, 256, 0, P.T > 0);
 }
 
