@@ -375,6 +375,7 @@ struct NextShared {
     float2 warp_sum[kNextWarps][2];
     double warp_part[kNextWarps][4];
     float2 warp_top[kNextWarps], top[2][kMaxCluster];
+    int warp_closest[kNextWarps], closest[2][kMaxCluster];
     double part[2][kMaxCluster][4];     // of every CTA, written by it; two sets in turn, so that one barrier per exchange does
     double scan[kNextWarps];
     int found, last;
@@ -383,13 +384,14 @@ struct NextShared {
     float behind, u_next;
 };
 
-// Lane i of warp 0 hands v and top to CTA i of the cluster: everybody's numbers for everybody.
+// Lane i of warp 0 hands v, top and closest to CTA i of the cluster: everybody's numbers for everybody.
 template <typename S_>
-__device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, const double (&v)[4], float2 top) {
+__device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, const double (&v)[4], float2 top, int closest) {
     if (threadIdx.x < (unsigned)cluster) {
         const uint32_t at = ptx::map_to_cta(ptx::smem_u32(&S.top[set][rank]), threadIdx.x);
         ptx::st_cluster_u32(at, __float_as_uint(top.x));
         ptx::st_cluster_u32(at + 4, __float_as_uint(top.y));
+        ptx::st_cluster_u32(ptx::map_to_cta(ptx::smem_u32(&S.closest[set][rank]), threadIdx.x), (uint32_t)closest);
         const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&S.part[set][rank][0]), threadIdx.x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) st_cluster_f64(to + 8 * i, v[i]);
@@ -397,13 +399,13 @@ __device__ __forceinline__ void exchange(S_& S, int set, int rank, int cluster, 
     __syncwarp();
     ptx::cluster_sync_all();
 }
-// a += p and d += q where p > border, by predicate: a branch would part the exponentials, a selection costs four instructions.
-__device__ __forceinline__ void add_if_more(double p, double border, double q, double& a, double& d) {
+// a += t and d += q where t > 0, by predicate: a branch would part the exponentials, a selection costs four instructions.
+__device__ __forceinline__ void add_if_above(double t, double q, double& a, double& d) {
     asm("{\n\t.reg .pred more;\n\t"
-        "setp.gt.f64 more, %2, %3;\n\t"
+        "setp.gt.f64 more, %2, 0d0000000000000000;\n\t"
         "@more add.rn.f64 %0, %0, %2;\n\t"
-        "@more add.rn.f64 %1, %1, %4;\n\t}"
-        : "+d"(a), "+d"(d) : "d"(p), "d"(border), "d"(q));
+        "@more add.rn.f64 %1, %1, %3;\n\t}"
+        : "+d"(a), "+d"(d) : "d"(t), "d"(q));
 }
 // Sums over the lanes, the same bits in every lane.
 __device__ __forceinline__ void add_lanes(double (&a)[4]) {
@@ -415,14 +417,26 @@ __device__ __forceinline__ void add_lanes(double (&a)[4]) {
 
 // The row that a token is drawn from.  Weights of entry v, in units of 1 / sum p:
 //   p(v) = exp(x / T) up to a factor (see Row64),  q(v) likewise,  r(v) = max(p(v) - rho q(v), 0)  with rho = sum p / sum q.
-// Sums over r need rho, which needs the sums over p and q: one pass takes all of them, with the entries that count
-// decided by an fp32 rho (off by some 2^-20) that the first kernel, or a quick pass over the row, has left behind.  Sums A of p and D of q over
-// those entries then give sum r = A - rho D for the rho that came out: an entry on the wrong side of the
-// border is off by less than |rho - rho~| q(v), and only entries that close to the border are, so that the sum
-// is off by the square of that, unless there is little but such entries: then the pass is done once more.  A difference
-// of less than 2^-40 p counts as 0: next to a token that both are certain of it would be rounding (the exponentials are good
-// to 2^-42), and outweigh a rest of 1e-90 that is not.
-// (Two passes, the first for rho, are as exact and took 40 % longer.)
+// A difference of less than 2^-40 p counts as 0: next to a token that both are certain of it would be rounding (the
+// exponentials are good to 2^-42), and outweigh a rest of 1e-90 that is not.  So entry v counts where
+// t(v) = p(v) - border q(v) > 0, border = rho (1 + 2^-40).
+// Sums over r need rho, which needs the sums over p and q: one pass takes all of them, with a border from an fp32
+// rho (off by some 2^-22) that the first kernel, or a quick pass over the row, has left behind.  With sums A of t and D of q over
+// the entries that counted, sum r = A + (border - rho) D for the rho that came out, if the same entries count against
+// the right border.  An entry changes sides only if the border is off by |t| / q or more, so the pass also notes the entry
+// that comes closest to it: the largest difference of the high words of p and |t|, taken as whole numbers, which are logarithms to
+// within 0.0861 + 2^-19, in 2^-20 of a power of two (see nearest).  Where the border was off by as much as that, an entry of any weight
+// may have been on the wrong side - most of the row, if the draft agrees with the target on most of the vocabulary - and
+// the pass is done once more, with the right border: a few draws in a hundred over 150 thousand tokens.
+// (Two passes in any case, the first for rho, took 40 % longer.)
+
+// How far, at least, every entry of a row is from `border`, as a difference of borders: |t| >= g p, and p = t + border q, give
+// |t| / q >= border g / (1 + g).
+__device__ __forceinline__ double nearest(double border, int closest) {
+    const float g = exp2f(-9.5367431640625e-7f * (float)closest - 0.0875f);
+    return border * (double)g / (1.0 + (double)g);
+}
+__device__ __forceinline__ int closeness(double p, double t) { return __double2hiint(p) + ~(__double2hiint(t) & 0x7FFFFFFF); }
 
 // THREADS: 256, three CTAs per SM, or 512 where there are fewer CTAs than SMs.
 template <typename TP, typename TQ, bool HAS_Q, int THREADS>
@@ -445,15 +459,16 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
 
     // What every thread of the cluster knows about a row.
     Row64 at_p, at_q;
-    double rho = 0.0, sum_p = 0.0, sum_q = 0.0, sum_a = 0.0, sum_d = 0.0;
+    double border = 0.0, rho = 0.0, sum_p = 0.0, sum_q = 0.0, sum_t = 0.0, sum_d = 0.0;
+    int closest = 0;
     const TP* row_p = target;
     const TQ* row_q = draft_rows;
 
-    // fp64 sums over the row; entry `skip` of p counts as masked.  The warps' and CTAs' sums of p, q, A, D stay in warp_part
+    // fp64 sums over the row; entry `skip` of p counts as masked.  The warps' and CTAs' sums of p, q, t, D stay in warp_part
     // and part[set ^ 1].  Are the weights in reach of their reference?
     auto sums = [&](bool with_q, int skip) {
         double a[4] = {};
-        const double rho_up = rho * kAbove;
+        closest = 0;
         float2 top = make_float2(neg_inf(), neg_inf());
         const auto add = [&](auto& x, auto& y) {      // (all the exponentials side by side, without a branch between them)
             constexpr int N = sizeof(x) / sizeof(x[0]);
@@ -469,8 +484,10 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
                 for (int i = 0; i < N; i += 2) top.y = fmaxf(top.y, fmaxf(y[i], y[i + 1 < N ? i + 1 : i]));
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
+                    const double t = fma(-border, q[i], p[i]);
                     a[1] += q[i];
-                    add_if_more(p[i], rho_up * q[i], q[i], a[2], a[3]);
+                    add_if_above(t, q[i], a[2], a[3]);
+                    closest = max(closest, closeness(p[i], t));
                 }
             }
 #pragma unroll
@@ -506,8 +523,9 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
         __syncwarp();
         add_lanes(a);
         top = make_float2(warp_max(top.x), warp_max(top.y));
+        closest = __reduce_max_sync(0xFFFFFFFFu, closest);
         if (lane < 4) S.warp_part[warp][lane] = lane == 0 ? a[0] : lane == 1 ? a[1] : lane == 2 ? a[2] : a[3];
-        if (lane == 0) S.warp_top[warp] = top;
+        if (lane == 0) { S.warp_top[warp] = top; S.warp_closest[warp] = closest; }
         __syncthreads();
         if (warp == 0) {
 #pragma unroll
@@ -515,14 +533,16 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
             add_lanes(a);
             top = S.warp_top[lane < kNextWarps ? lane : 0];
             top = make_float2(warp_max(top.x), warp_max(top.y));
+            closest = __reduce_max_sync(0xFFFFFFFFu, S.warp_closest[lane < kNextWarps ? lane : 0]);
         }
-        exchange(S, set, rank, cluster, a, top);
+        exchange(S, set, rank, cluster, a, top, closest);
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = lane < cluster ? S.part[set][lane][i] : 0.0;
         add_lanes(a);
-        sum_p = a[0]; sum_q = a[1]; sum_a = a[2]; sum_d = a[3];
+        sum_p = a[0]; sum_q = a[1]; sum_t = a[2]; sum_d = a[3];
         top = S.top[set][lane < cluster ? lane : 0];
         top = make_float2(warp_max(top.x), warp_max(top.y));
+        closest = __reduce_max_sync(0xFFFFFFFFu, S.closest[set][lane < cluster ? lane : 0]);
         set ^= 1;
         return in_reach(top.x, at_p, P.e) && (!(HAS_Q && with_q) || in_reach(top.y, at_q, P.e_draft));
     };
@@ -590,17 +610,18 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
         skip = !HAS_Q && decided && token ? tok : -1;
 
         // The drafted token's logits are a reference as good as the rows' maxima, as a rule, and with them its ratio (from the
-        // first kernel) says what rho is; without a token some entry of the row is.  Where they are not (no such token, a
+        // first kernel) says what rho is, but for the rounding; without a token some entry of the row is.  Where they are not (no such token, a
         // ratio of nothing, logits too far apart for fp64), a quick pass over the rows finds maxima and rho first.
         row_p = target + (long long)n * P.ld_target;
         row_q = draft_rows + (long long)n * P.ld_draft;
         const float x = drafted ? S.x[n - window] : S.behind, y = HAS_Q && drafted ? S.y[n - window] : 0.0f;      // (of a token that does not exist: not used)
         enum { kQuick, kCareful, kExact } how = kCareful;
+        bool accepted = false, again = false;
         if (drafted == token && near_zero(x, P.e) && (!against_q || (near_zero(y, P.e_draft) && ratio > 1e-30f))) {      // (false for a NaN)
             how = kQuick;
             at_p = Row64(x, P.e);
             at_q = Row64(y, P.e_draft);
-            rho = against_q ? weight(x, at_p, P.e, S.table) / (weight(y, at_q, P.e_draft, S.table) * (double)ratio) : 0.0;
+            border = against_q ? kAbove * weight(x, at_p, P.e, S.table) / (weight(y, at_q, P.e_draft, S.table) * (double)ratio) : 0.0;
         }
 #pragma unroll 1
         for (;;) {
@@ -629,41 +650,46 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
                     const float2 cp = join_parts(&S.warp_sum[0][0], kNextWarps, 2, P.c), cq = join_parts(&S.warp_sum[0][1], kNextWarps, 2, P.c_draft);
                     v[0] = cp.x; v[1] = cp.y; v[2] = cq.x; v[3] = cq.y;
                 }
-                exchange(S, set, rank, cluster, v, make_float2(0.0f, 0.0f));
+                exchange(S, set, rank, cluster, v, make_float2(0.0f, 0.0f), 0);
                 const double* part = S.part[set][lane < cluster ? lane : 0];
                 const float2 ap = join_lanes((float)part[0], lane < cluster ? (float)part[1] : 0.0f, P.c);
                 const float2 aq = join_lanes((float)part[2], lane < cluster ? (float)part[3] : 0.0f, P.c_draft);
                 at_p = Row64(ap.x, P.e);
                 at_q = Row64(aq.x, P.e_draft);
-                rho = aq.y > 0.0f ? (double)ap.y * weight(ap.x, at_p, P.e, S.table) / ((double)aq.y * weight(aq.x, at_q, P.e_draft, S.table)) : 0.0;
+                border = aq.y > 0.0f ? kAbove * (double)ap.y * weight(ap.x, at_p, P.e, S.table) / ((double)aq.y * weight(aq.x, at_q, P.e_draft, S.table)) : 0.0;
                 set ^= 1;
             }
             if (!sums(against_q, skip) && how == kQuick) { how = kCareful; continue; }
             total = sum_p;
+            if (!decided) {
+                // is this position's token accepted?  (p(x) = 0, or a NaN or +inf in a row: no)
+                accepted = x > neg_inf() && sum_p > 0.0 && (!HAS_Q || sum_q >= 0.0);
+                if (accepted && (!HAS_Q || y > neg_inf())) {      // (q(x) = 0 otherwise: yes)
+                    // by logarithms: p(x) and q(x) may both lie below fp64's range
+                    double l = ((double)x - at_p.base) * P.inv_temp - log(sum_p);
+                    if (HAS_Q) l -= ((double)y - at_q.base) * P.inv_draft_temp - log(sum_q);
+                    const float u = S.u[n - window];
+                    accepted = u <= 0.0f || (double)u < exp(l);
+                }
+                if (accepted) break;
+                decided = true;
+                again = !HAS_Q;       // (without a draft's distribution the sums have to leave the token out)
+            }
             if (against_q) {
-                const double guess = rho;
                 rho = sum_q > 0.0 ? sum_p / sum_q : 0.0;
-                total = sum_a - rho * sum_d;
-                if (how != kExact && rho != guess && !(total > sum_p * 0.0009765625)) {      // p and q nearly equal (or not numbers): with the rho that came out
+                total = fma(border - rho, sum_d, sum_t);
+                const double right = rho * kAbove;
+                // (a NaN comes here once; of weights near fp64's lower end the high words are no logarithms)
+                if (how != kExact && right != border && !(fabs(right - border) < nearest(border, closest) && total > 1e-270)) {
                     how = kExact;
+                    border = right;
                     continue;
                 }
             }
             break;
         }
-        if (decided) break;
-        // is this position's token accepted?  (p(x) = 0, or a NaN or +inf in a row: no)
-        bool ok = x > neg_inf() && sum_p > 0.0 && (!HAS_Q || sum_q >= 0.0);
-        if (ok && (!HAS_Q || y > neg_inf())) {      // (q(x) = 0 otherwise: yes)
-            // by logarithms: p(x) and q(x) may both lie below fp64's range
-            double l = ((double)x - at_p.base) * P.inv_temp - log(sum_p);
-            if (HAS_Q) l -= ((double)y - at_q.base) * P.inv_draft_temp - log(sum_q);
-            const float u = S.u[n - window];
-            ok = u <= 0.0f || (double)u < exp(l);
-        }
-        if (ok) { ++n; continue; }
-        decided = true;
-        if (HAS_Q) break;       // (without a draft's distribution the sums have to leave the token out)
+        if (accepted) { ++n; continue; }
+        if (!again) break;
     }
     if (rank == 0 && threadIdx.x == 0) P.out_accept_len[b] = n;
     if (skip >= 0 && total == 0.0) {      // nothing but the rejected token
@@ -683,10 +709,10 @@ next_kernel(const __grid_constant__ LosslessParams P, int cluster) {
     const auto entry_weight = [&](int j) {
         const double p = j == skip ? 0.0 : weight(entry(row_p, j), at_p, P.e, S.table);
         if (!HAS_Q || !against_q) return p;
-        const double q = weight(entry(row_q, j), at_q, P.e_draft, S.table);
-        return p > rho * kAbove * q ? fma(-rho, q, p) : 0.0;
+        const double q = weight(entry(row_q, j), at_q, P.e_draft, S.table), t = fma(-border, q, p);
+        return t > 0.0 ? fma(border - rho, q, t) : 0.0;
     };
-    const auto part_weight = [&](const double* part) { return against_q ? part[2] - rho * part[3] : part[0]; };
+    const auto part_weight = [&](const double* part) { return against_q ? fma(border - rho, part[3], part[2]) : part[0]; };
     // the part that holds the place u_next * total: a CTA's, then a warp's
     double place = (double)S.u_next * total;
     if (part_of(place, lane < cluster ? part_weight(S.part[set ^ 1][lane]) : 0.0) != rank) return;
