@@ -315,7 +315,9 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
  *                                them are not read, but for row draft_len[b] of the target, which the next token is drawn from
  *   u_accept[B,T], u_next[B]     float32 in [0,1).  Outputs must not overlap inputs
  *   out_accept_len[B], out_next_token[B]   -1 if every one of T tokens was accepted and there is no bonus row
- *   out_accept_prob[B,T]         float32, min(1, p(x) / q(x)); 0 behind draft_len.  Read by the call's second kernel
+ *   out_accept_prob[B,T]         float32, min(1, p(x) / q(x)); 0 behind draft_len.  Read by the call's second kernel.  Its
+ *                                sums are split by B, T and V: a position's last bits may differ with the B and T of the
+ *                                call, decisions and tokens only where 64-bit sums round apart
  * Masked entries: -inf has probability 0; a row of nothing but -inf has probability 0 everywhere.  A row that holds a
  * NaN or +inf: accept_prob NaN, the token is not accepted, next token -1; next token -1 too where there is nothing to draw from.
  * T = 0 with a bonus row draws one token per sequence (draft, u_accept and out_accept_prob may be NULL).  B = 0 is
