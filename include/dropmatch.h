@@ -362,7 +362,8 @@ int dropmatch_dropout_grad(dm_ctx* ctx, const void* grad, int dtype, int64_t ld,
  *                          earlier work of the same stream.
  * 8-bit matrices: any value in [-128, 127], 16-byte aligned, row strides (bytes) a multiple of 16; bytes d..ld of a row are
  * neither read nor written.  x, scales and out are aligned to one entry, strides at least the row's length; columns V..ld_out
- * are left as they are.  d <= 131071 (matrix products), V <= 2^30, else DM_EUNSUPPORTED.  Outputs must not overlap inputs.
+ * are left as they are.  Products: d <= 131071, V and n_rows <= 2^30; quantisation: n <= 2^30; else DM_EUNSUPPORTED.  Outputs
+ * must not overlap inputs.
  * n_rows = 0 is allowed and does nothing.  Need no head and no workspace: calls of one context may overlap (linear's with
  * their own out_q and out_scale).  If a kernel gives up on a wait (dm_device_error), outputs that it did not reach are NaN. */
 int dropmatch_quantize_i8(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int n_rows, int n, int8_t* out_q,

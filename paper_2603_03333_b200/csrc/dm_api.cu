@@ -296,7 +296,7 @@ int check_quantize(const void* x, int dtype, int64_t ld, int n_rows, int n, cons
 int check_matmul_i8(const int8_t* w, int64_t ld_w, const float* w_scale, int n_rows, int V, int d, const void* out, int out_dtype,
                     int64_t ld_out) {
     if (n_rows < 0 || V < 1 || d < 1 || (out_dtype != DM_F32 && out_dtype != DM_BF16) || ld_out < V) return DM_EINVAL;
-    if (V > kRowsMaxV || d > kI8MaxDepth) return DM_EUNSUPPORTED;
+    if (V > kRowsMaxV || d > kI8MaxDepth || n_rows > kRowsMaxV) return DM_EUNSUPPORTED;
     if (n_rows == 0) return DM_OK;
     if (!i8_rows_ok(w, ld_w, d) || !aligned_to_entry(w_scale, DM_F32) || !aligned_to_entry(out, out_dtype)) return DM_EINVAL;
     const int64_t elem = out_dtype == DM_F32 ? 4 : 2;
