@@ -321,7 +321,8 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
  * Masked entries: -inf has probability 0; a row of nothing but -inf has probability 0 everywhere.  A row that holds a
  * NaN or +inf: accept_prob NaN, the token is not accepted, next token -1; next token -1 too where there is nothing to draw from.
  * T = 0 with a bonus row draws one token per sequence (draft, u_accept and out_accept_prob may be NULL).  B = 0 is
- * allowed and does nothing.  V <= 2^30.  Needs no head and no workspace: calls of one context may overlap. */
+ * allowed and does nothing.  V <= 2^30 and B (T + bonus_row) <= 2^27, else DM_EUNSUPPORTED.  Needs no head and no
+ * workspace: calls of one context may overlap. */
 int dropmatch_verify_lossless(dm_ctx* ctx, const void* target, int dtype, int64_t ld_target, const void* draft_logits,
                               int draft_dtype, int64_t ld_draft, const int32_t* draft, const int32_t* draft_len, int B,
                               int T, int bonus_row, int V, float temperature, float draft_temperature,

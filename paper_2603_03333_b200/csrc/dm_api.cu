@@ -938,7 +938,7 @@ int dropmatch_verify_lossless(dm_ctx* c, const void* target, int dtype, int64_t 
                               int bonus_row, int V, float temperature, float draft_temperature, const float* u_accept,
                               const float* u_next, int32_t* out_accept_len, int32_t* out_next_token, float* out_accept_prob,
                               void* stream) {
-    if (c == nullptr || B < 0 || T < 0 || (bonus_row != 0 && bonus_row != 1) || T + bonus_row < 1) return DM_EINVAL;
+    if (c == nullptr || B < 0 || T < 0 || (bonus_row != 0 && bonus_row != 1) || (T == 0 && bonus_row == 0)) return DM_EINVAL;
     if ((long long)B * ((long long)T + bonus_row) > (1ll << 27)) return DM_EUNSUPPORTED;     // (clusters of one launch)
     RowsParams rp{}, rq{};
     int st = rows_common(&rp, dtype, ld_target, B, V, temperature);
