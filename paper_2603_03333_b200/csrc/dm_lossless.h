@@ -4,8 +4,6 @@
 
 namespace dm {
 
-constexpr int kLosslessMaxV = 1 << 30;
-
 // Constants of exp(x / T) in fp64 (see weight() in dm_lossless.cu).
 struct Exp64 {
     float c16;       // 16 log2(e) / T
