@@ -304,7 +304,7 @@ int dropmatch_distill(dm_ctx* ctx, const void* logits, int dtype, int64_t ld, in
  * next token is drawn from r = max(p - q, 0) of row n (p, if r is 0 everywhere) where a token was rejected, and
  * from p of row n where all were accepted: the smallest v with  r(0) + ... + r(v) > u_next[b] * sum r.
  * Decisions and draws are those of 64-bit arithmetic on the given logits (exponentials to 2^-42; a difference p - q of
- * less than 2^-40 p counts as 0); out_accept_prob is fp32.
+ * less than 2^-41 p counts as 0, of less than 2^-40 p may); out_accept_prob is fp32.
  *   target[B][T + bonus_row][ld_target]   dtype DM_F32 or DM_BF16; row stride ld_target >= V entries, aligned to one
  *                                entry (16-byte aligned rows are the fastest).  bonus_row = 1: one more row per
  *                                sequence, behind the last drafted token
@@ -338,8 +338,9 @@ int dropmatch_verify_lossless(dm_ctx* ctx, const void* target, int dtype, int64_
  * with s = 1 / (1 - p) in fp32; fp32 arithmetic, rounded once to dtype (DM_F32 or DM_BF16).  Dropped entries are +0
  * and add nothing whatever they hold.  Plain dropout of n rows: B = 1, T = n, K = 1.
  *   1 <= K <= 1024, B*T*K < 2^30, 1 <= d <= 2^30, strides >= d entries, pointers aligned to one entry (16-byte aligned
- *   rows are the fastest); entries d..ld_out of a row are left as they are.  The output must not overlap the input,
- *   but for K = 1 may be the input itself (same pointer and stride).  B*T = 0 is allowed and does nothing.
+ *   rows are the fastest); entries d..ld_out of a row are left as they are.  The output must not overlap the input, each
+ *   from its first entry to the last row's last (so not its neighbouring columns either), but for K = 1 may be the
+ *   input itself (same pointer and stride).  B*T = 0 is allowed and does nothing.
  * A row's results do not depend on the other rows of the call.  Needs no head and no workspace: calls of one context
  * may overlap.  dm_set_mask_mode's value is taken at the call (and fixed in a captured graph). */
 int dropmatch_dropout(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int B, int T, int K, int d, float p,
@@ -349,7 +350,8 @@ int dropmatch_dropout_grad(dm_ctx* ctx, const void* grad, int dtype, int64_t ld,
 
 /* ---- a head in 8-bit integers ----------------------------------------------------------------------
  * Projections through a matrix W[V,d] held in 8-bit integers with a scale for each row (vocabulary entry, channel), of
- * rows quantised to 8 bits with a scale for each row (token): half the bytes of a bf16 head, which bound most calls.
+ * rows quantised to 8 bits with a scale for each row (token): half the bytes of a bf16 head, which bound a projection of few
+ * rows.  The calls on a context's head (dm_set_head) take fp32 and bf16 only.
  * The logits go where any logits go (dropmatch_verify_lossless, _logprobs, _distill).
  *   dropmatch_quantize_i8  x[n_rows][ld] (DM_F32 or DM_BF16) -> out_q[n_rows][ld_q], out_scale[n_rows]:
  *                          scale = max(max_j |x[j]| / 127, 2^-126),  q[j] = x[j] / scale rounded to the nearest whole number,
@@ -364,7 +366,7 @@ int dropmatch_dropout_grad(dm_ctx* ctx, const void* grad, int dtype, int64_t ld,
  * 8-bit matrices: any value in [-128, 127], 16-byte aligned, row strides (bytes) a multiple of 16; bytes d..ld of a row are
  * neither read nor written.  x, scales and out are aligned to one entry, strides at least the row's length; columns V..ld_out
  * are left as they are.  Products: d <= 131071, V and n_rows <= 2^30; quantisation: n <= 2^30; else DM_EUNSUPPORTED.  Outputs
- * must not overlap inputs.
+ * must not overlap inputs, each from its first entry to the last row's last.
  * n_rows = 0 is allowed and does nothing.  Need no head and no workspace: calls of one context may overlap (linear's with
  * their own out_q and out_scale).  If a kernel gives up on a wait (dm_device_error), outputs that it did not reach are NaN. */
 int dropmatch_quantize_i8(dm_ctx* ctx, const void* x, int dtype, int64_t ld, int n_rows, int n, int8_t* out_q,

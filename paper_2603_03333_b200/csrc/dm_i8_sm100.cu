@@ -11,7 +11,7 @@
 // under sustained load the power cap in either case (integers of full range toggle every bit of what is streamed).
 // Measured, quantisation included: one token against 128256 x 4096 90-96 us (525 MB, a bare read of which takes 78-86), 61
 // tokens against 151936 x 4096 117-120 us (622 MB; 130-135 back to back), 2047 against 128256 x 8192 1.54-1.6 ms
-// (2.7-2.8 PFLOP/s; back to back 1.78-1.84 ms, 2.35-2.4 PFLOP/s, 0.85 of twice what a bf16 GEMM sustains).
+// (2.7-2.8 PFLOP/s; back to back 1.78-1.86 ms, 2.3-2.4 PFLOP/s, 0.85 of twice what a bf16 GEMM sustains).
 // Tried: two blocks of 256 tokens per piece of W, filling TMEM (a quarter less traffic into shared memory, but read-out that
 // the next tile does not hide: 978 against 826 us at d = 4096, the same at 8192); pairs for few tokens, steps that start at
 // another depth in every CTA (no difference).

@@ -13,7 +13,7 @@
 // can be off, see kBand) is decided again from fp64 sums, and all sums over row n are fp64 with exponentials good to
 // 2^-42 (see weight).  In fp32 a token of the flat tail of 100 thousand would come out one place off in about a
 // draw of ten, and two engines with equal random numbers would drift apart.
-// Measured: 96 sequences of 7 tokens, 151936 bf16 entries, both models (408 MB) 150 us (134 back to back in a graph): 73 + 74,
+// Measured: 96 sequences of 7 tokens, 151936 bf16 entries, both models (408 MB) 150 us (135 back to back in a graph): 73 + 74,
 // where HBM takes 62; one sequence of 5 tokens of 128256 18-20 us (14 in a graph), 4 tokens of 4096 fp32 14 (9).  Rows through registers instead of the ring, per-thread joins and
 // two fp64 passes took 396 and 89; ratios and draws in one kernel, a cluster going through its sequence's rows, 160 and 22.
 #include <math.h>
